@@ -48,7 +48,8 @@ typedef enum {
     SW_ERR_ALIGN = 4,       /* pointer not aligned to its element size                 */
     SW_ERR_ALIAS = 5,       /* y overlaps x or w                                       */
     SW_ERR_LAUNCH = 6,      /* the HIP runtime refused the launch (or no device)       */
-    SW_ERR_JIT = 7          /* the run-time compiler refused a generated kernel        */
+    SW_ERR_JIT = 7,         /* the run-time compiler refused a generated kernel        */
+    SW_ERR_WORKSPACE = 8    /* a caller-owned workspace is missing or too small        */
 } sw_status;
 
 typedef enum { SW_POOL_AVG = 0, SW_POOL_MAX = 1 } sw_pool_mode;
@@ -405,13 +406,108 @@ int sw_conv2d_f16_nhwc(const void* x, const void* w, const float* bias, void* y,
                        int N, int H, int W, int C_in, int C_out, int R, int S,
                        int stride, int pad, int dilation, int relu, void* hip_stream);
 
+/*
+ * ---- Layer norm and linear attention with a decay for each head ------------------------------------------
+ * What stands between the pointwise convolutions (projections) of a sequence model on channel-last rows.  The
+ * attention is a sliding window sum as well: its window is unlimited and fades by a factor a token, so that
+ * everything before a token is one matrix of sums, the state.
+ *
+ * Conventions beside those above: tensors are fp32, bf16 or IEEE half (an sw_type; bit patterns as in the
+ * channel-last calls), products, statistics, sums and states fp32, results rounded once, to nearest even.
+ * Strides are in elements; the innermost dimension is contiguous.  Offsets may pass 2^31.  Calls that need
+ * scratch memory take it from the caller: `workspace`, 16-byte aligned, of at least the bytes that the call's
+ * _workspace_bytes function names (SW_ERR_WORKSPACE otherwise); its contents mean nothing before or after.
+ */
+typedef enum { SW_F32 = 0, SW_BF16 = 1, SW_F16 = 2 } sw_type;
+
+/*
+ * Layer norm of every row of C channels:
+ *     m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps),  y = (x - m) * r * weight + bias
+ * x, y: `rows` rows of C elements, x_stride and y_stride apart (>= C, else SW_ERR_SHAPE); weight, bias: [C] fp32
+ * or NULL (ones, zeros); mean, rstd: [rows] fp32 or NULL: m and r, for the backward pass.  The variance is taken
+ * about the mean (two passes over values held on chip).  y may be x itself (same pointer and stride); any other
+ * overlap is SW_ERR_ALIAS.  1 <= C <= 2^20 (SW_ERR_UNSUPPORTED beyond); eps >= 0 and finite, else SW_ERR_SHAPE.
+ */
+int sw_layer_norm(const void* x, const float* weight, const float* bias, void* y, float* mean, float* rstd,
+                  int64_t rows, int64_t C, int64_t x_stride, int64_t y_stride, float eps, int type, void* hip_stream);
+
+/*
+ * Its backward pass.  With h = (x - mean) * rstd and g = dy * weight,
+ *     dx = rstd * (g - mean(g) - h * mean(g * h)),  dweight = sum over rows of dy * h,  dbias = sum over rows of dy.
+ * mean, rstd: [rows] fp32 as sw_layer_norm wrote them; weight: [C] fp32 or NULL (ones); dx: as x, or NULL;
+ * dweight, dbias: [C] fp32, each or both NULL where they are not wanted.  The sums over rows are added in a fixed
+ * order: equal calls give equal bits.  dx may be dy or x itself (same pointer and stride).
+ */
+int sw_layer_norm_backward(const void* dy, const void* x, const float* weight, const float* mean, const float* rstd,
+                           void* dx, float* dweight, float* dbias, int64_t rows, int64_t C, int64_t dy_stride,
+                           int64_t x_stride, int64_t dx_stride, int type, void* workspace, int64_t workspace_bytes,
+                           void* hip_stream);
+int64_t sw_layer_norm_backward_workspace_bytes(int64_t rows, int64_t C);     /* 0 for invalid extents */
+
+/*
+ * Linear attention.  For every sequence and head h, with l = exp(log_decay[h]) and the state S [dk, dv],
+ *     S_t = l * S_{t-1} + k_t v_t^T,      o_t = scale * S_t^T q_t,      S before the first token: `state` or zero.
+ * q: [B, T, heads, dk], k: [B, T, kv_heads, dk], v: [B, T, kv_heads, dv], o: [B, T, heads, dv], each with strides of
+ * its own; heads is a multiple of kv_heads, and heads/kv_heads neighbouring heads share a row of k and v.
+ * log_decay: [heads] fp32, <= 0; -infinity forgets everything before a token.  It is a constant of the layer.
+ * Sequences of different lengths: starts [B+1] int32 (device), not decreasing, and B = 1 in the strides: sequence b
+ * is the rows starts[b] ... starts[b+1]-1 of T rows in all; rows in no sequence get zeros.  Values out of range are
+ * taken as the nearest in range.  A sequence may be empty: its final state is its first.
+ * state, final_state: [n_states, heads, dk, dv] fp32 or NULL, contiguous; sequence b has entry slots[b] of both, or
+ * entry b where slots is NULL (n_states >= B then, else SW_ERR_SHAPE).  slots: [B] int32 (device), no entry twice; a
+ * sequence with an entry outside 0 ... n_states-1 starts from zero and its final state is not kept.  final_state
+ * may be state.  Extents: 1 <= dk, dv <= 256 (SW_ERR_UNSUPPORTED beyond); all tensors aligned to their elements,
+ * `o` overlapping no input.
+ */
+typedef struct {
+    int64_t batch, token, head;         /* elements from one to the next */
+} sw_strides;
+typedef struct {
+    int64_t T;                          /* tokens of a sequence, or of all packed ones (starts)    */
+    int B, heads, kv_heads, dk, dv;     /* B: sequences                                            */
+    int n_states;                       /* entries of state and final_state (0 where there is neither) */
+    int type;                           /* sw_type of q, k, v, o and their gradients               */
+    float scale;
+} sw_linear_attention_dims;
+
+int sw_linear_attention(const void* q, const void* k, const void* v, void* o, const float* log_decay, const float* state,
+                        float* final_state, const int32_t* slots, const int32_t* starts, const sw_linear_attention_dims* dims,
+                        const sw_strides* q_strides, const sw_strides* k_strides, const sw_strides* v_strides,
+                        const sw_strides* o_strides, void* workspace, int64_t workspace_bytes, void* hip_stream);
+int64_t sw_linear_attention_workspace_bytes(const sw_linear_attention_dims* dims, int packed);   /* packed: starts is given */
+
+/*
+ * Its backward pass: from d_o and, where the final state went on, d_final_state (else NULL), the gradients
+ *     dS_t = scale * q_t do_t^T + l * dS_{t+1},  dq_t = scale * S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t^T k_t,  d_state = l * dS_1
+ * dk and dv of shared rows are sums over the heads that share them.  state as in the forward call; d_final_state and
+ * d_state: [B, heads, dk, dv] (entry b, whatever slots says of state); d_state is NULL where it is not wanted and may be
+ * d_final_state.  dq, dk, dv have q's, k's and v's shapes and strides of their own; rows in no sequence get zeros.
+ */
+int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, const void* v, const float* log_decay,
+                                 const float* state, const float* d_final_state, void* dq, void* dk, void* dv, float* d_state,
+                                 const int32_t* slots, const int32_t* starts, const sw_linear_attention_dims* dims,
+                                 const sw_strides* do_strides, const sw_strides* q_strides, const sw_strides* k_strides,
+                                 const sw_strides* v_strides, const sw_strides* dq_strides, const sw_strides* dk_strides,
+                                 const sw_strides* dv_strides, void* workspace, int64_t workspace_bytes, void* hip_stream);
+int64_t sw_linear_attention_backward_workspace_bytes(const sw_linear_attention_dims* dims, int packed);
+
+/*
+ * Its form for one token of each of B requests (dims->T is 1), on a cache of states that is brought up to date in place:
+ *     S[slots[b]] = l * S[slots[b]] + k_b v_b^T,      o_b = scale * S[slots[b]]^T q_b
+ * q, k, v, o: [B, heads or kv_heads, dk or dv], strides as above (token unused).  state: [n_states, heads, dk, dv] fp32,
+ * 16-byte aligned.  slots as above: a row whose entry is out of range gets zeros and touches no state.
+ */
+int sw_linear_attention_step(const void* q, const void* k, const void* v, void* o, const float* log_decay, float* state,
+                             const int32_t* slots, const sw_linear_attention_dims* dims, const sw_strides* q_strides,
+                             const sw_strides* k_strides, const sw_strides* v_strides, const sw_strides* o_strides, void* hip_stream);
+
 /* Output extent of one axis; <= 0 means the filter does not fit (or bad arguments). */
 int64_t sw_out_dim(int64_t in, int k, int stride, int pad);
 
 /* The same for a filter whose taps are `dilation` input positions apart (span dilation*(k-1)+1). */
 int64_t sw_out_dim_dilated(int64_t in, int k, int stride, int pad, int dilation);
 
-/* Device workspace the library needs: always 0 (paper, sections 1 and 2). */
+/* Device workspace that convolution and pooling need: always 0 (paper, sections 1 and 2). */
 size_t sw_workspace_bytes(void);
 
 /* Static, NUL-terminated description of an sw_status value. */

@@ -14,6 +14,8 @@ LIB_PATH = os.path.join(_PKG, "libswconv.so")
 
 SW_OK = 0
 SW_ERR_NULL, SW_ERR_SHAPE, SW_ERR_UNSUPPORTED, SW_ERR_ALIGN, SW_ERR_ALIAS, SW_ERR_LAUNCH, SW_ERR_JIT = 1, 2, 3, 4, 5, 6, 7
+SW_ERR_WORKSPACE = 8
+SW_F32, SW_BF16, SW_F16 = 0, 1, 2
 SW_POOL_AVG, SW_POOL_MAX = 0, 1
 
 EXPORTS = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2d_depthwise", "sw_conv2d_s8",
@@ -22,9 +24,22 @@ EXPORTS = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2d_depthw
            "sw_conv2d_depthwise_dilated_jit", "sw_jit_prepare_depthwise_dilated", "sw_jit_compile_check_dilated",
            "sw_jit_cached_kernels",
            "sw_s8_packed_filter_bytes", "sw_s8_pack_filter", "sw_conv2d_s8_packed", "sw_conv2d_s8_packed_requant",
+           "sw_layer_norm", "sw_layer_norm_backward", "sw_layer_norm_backward_workspace_bytes",
+           "sw_linear_attention", "sw_linear_attention_workspace_bytes", "sw_linear_attention_backward",
+           "sw_linear_attention_backward_workspace_bytes", "sw_linear_attention_step",
            "sw_probe", "sw_probe_ops", "sw_out_dim", "sw_out_dim_dilated", "sw_workspace_bytes", "sw_status_string", "sw_version", "sw_last_kernel")
 
 _lib = None
+
+
+class SwStrides(ctypes.Structure):
+    """sw_strides of include/swconv.h: elements from one batch entry, token, head to the next."""
+    _fields_ = [("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class SwLinearAttentionDims(ctypes.Structure):
+    """sw_linear_attention_dims of include/swconv.h."""
+    _fields_ = [("T", ctypes.c_int64), *((n, ctypes.c_int) for n in ("B", "heads", "kv_heads", "dk", "dv", "n_states", "type")), ("scale", ctypes.c_float)]
 
 
 class SwError(RuntimeError):
@@ -98,6 +113,22 @@ def lib() -> ctypes.CDLL:
     L.sw_conv2d_s8_packed.argtypes = [vp, vp, vp] + [i32] * 9 + [vp]
     L.sw_conv2d_s8_packed_requant.restype = i32
     L.sw_conv2d_s8_packed_requant.argtypes = [vp, vp, vp, vp, vp] + [i32] * 10 + [vp]
+    f32, dims, strides = ctypes.c_float, ctypes.POINTER(SwLinearAttentionDims), ctypes.POINTER(SwStrides)
+    L.sw_layer_norm.restype = i32
+    L.sw_layer_norm.argtypes = [vp] * 6 + [i64] * 4 + [f32, i32, vp]
+    L.sw_layer_norm_backward.restype = i32
+    L.sw_layer_norm_backward.argtypes = [vp] * 8 + [i64] * 5 + [i32, vp, i64, vp]
+    L.sw_layer_norm_backward_workspace_bytes.restype = i64
+    L.sw_layer_norm_backward_workspace_bytes.argtypes = [i64, i64]
+    L.sw_linear_attention.restype = i32
+    L.sw_linear_attention.argtypes = [vp] * 9 + [dims] + [strides] * 4 + [vp, i64, vp]
+    L.sw_linear_attention_backward.restype = i32
+    L.sw_linear_attention_backward.argtypes = [vp] * 13 + [dims] + [strides] * 7 + [vp, i64, vp]
+    for name in ("sw_linear_attention_workspace_bytes", "sw_linear_attention_backward_workspace_bytes"):
+        getattr(L, name).restype = i64
+        getattr(L, name).argtypes = [dims, i32]
+    L.sw_linear_attention_step.restype = i32
+    L.sw_linear_attention_step.argtypes = [vp] * 7 + [dims] + [strides] * 4 + [vp]
     L.sw_probe.restype = i32
     L.sw_probe.argtypes = [i32, i32, vp]
     L.sw_probe_ops.restype = i64

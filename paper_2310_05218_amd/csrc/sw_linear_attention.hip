@@ -1,0 +1,175 @@
+// Linear attention with a decay for each head, token by token: the recurrence as it stands, for prompts, gradients and single tokens.
+#include "sw_layers.h"
+
+namespace swconv {
+
+namespace {
+
+constexpr int kColumns = 64, kGroups = 4;       // a workgroup has 64 columns of the state, a quarter of its rows a wavefront
+
+__device__ __forceinline__ int64_t clamped(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Rows [lo, hi) of a packed batch's sequence j - 1, j = 1 ... B; j = 0 and B + 1: the rows before the first and after the last one.
+__device__ __forceinline__ void packed_rows(const AttentionBatch& n, int j, int64_t* lo, int64_t* hi)
+{
+    *lo = j == 0 ? 0 : clamped(n.starts[j - 1], 0, n.T);
+    *hi = j == n.B + 1 ? n.T : clamped(n.starts[j], *lo, n.T);
+}
+
+template <int EK, int ROWS>
+__global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel(AttentionSum s, AttentionBatch n)
+{
+    typedef typename ElemOf<EK>::type T;
+    __shared__ float la[2][ROWS * kGroups], lb[2][ROWS * kGroups], sums[2][kGroups][kColumns];
+    const int lane = threadIdx.x % 64, group = threadIdx.x / 64;
+    const int head = blockIdx.y, col = blockIdx.z * kColumns + lane;
+    int64_t lo = 0, hi = n.T;
+    int seq = blockIdx.x;
+    int64_t batch = seq;
+    bool rest = false;
+    if (n.starts) {
+        packed_rows(n, blockIdx.x, &lo, &hi);
+        rest = blockIdx.x == 0 || (int)blockIdx.x == n.B + 1;
+        seq = (int)blockIdx.x - 1;
+        batch = 0;
+    }
+    auto at = [&](const AttentionOperand& o, int64_t t) { return batch * o.batch + t * o.token + head / o.share * o.head; };
+    auto put = [&](int64_t t, float v) {
+        if (s.y_f32)
+            const_cast<float*>(static_cast<const float*>(s.y.p))[at(s.y, t) + col] = v;
+        else
+            const_cast<T*>(static_cast<const T*>(s.y.p))[at(s.y, t) + col] = (T)v;
+    };
+    if (rest) {
+        for (int64_t t = lo + group; t < hi; t += kGroups)
+            if (col < s.DC) put(t, 0.f);
+        return;
+    }
+    const int entry = s.first_slots ? s.first_slots[seq] : seq;
+    const bool kept = !s.first_slots || (entry >= 0 && entry < n.n_states);
+    const float decay = expf(n.log_decay[head]);
+    float state[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int row = group * ROWS + r;
+        state[r] = s.first.p && kept && row < s.DA && col < s.DC
+                       ? s.first.p[entry * s.first.entry + head * s.first.head + row * s.first.row + col * s.first.col]
+                       : 0.f;
+    }
+    for (int64_t i = lo; i < hi; ++i) {
+        const int64_t t = s.reverse ? hi - 1 - (i - lo) : i;
+        const int buf = (int)((i - lo) & 1);
+        for (int d = threadIdx.x; d < ROWS * kGroups; d += kColumns * kGroups) {
+            la[buf][d] = d < s.DA ? (float)static_cast<const T*>(s.a.p)[at(s.a, t) + d] : 0.f;
+            lb[buf][d] = d < s.DA ? (float)static_cast<const T*>(s.b.p)[at(s.b, t) + d] : 0.f;
+        }
+        const float c = col < s.DC ? (float)static_cast<const T*>(s.c.p)[at(s.c, t) + col] * s.alpha_s : 0.f;
+        __syncthreads();
+        float y = 0.f;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const float held = s.reverse ? state[r] : state[r] * decay;
+            state[r] = held + lb[buf][group * ROWS + r] * c;
+            y += state[r] * la[buf][group * ROWS + r];
+            if (s.reverse) state[r] *= decay;
+        }
+        sums[buf][group][lane] = y;
+        __syncthreads();
+        if (group == 0 && col < s.DC) put(t, s.alpha_y * (sums[buf][0][lane] + sums[buf][1][lane] + sums[buf][2][lane] + sums[buf][3][lane]));
+    }
+    if (s.last.p && kept && col < s.DC) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int row = group * ROWS + r;
+            if (row < s.DA) s.last.p[entry * s.last.entry + head * s.last.head + row * s.last.row + col * s.last.col] = state[r];
+        }
+    }
+}
+
+template <int EK>
+__global__ __launch_bounds__(256) void attention_fold_kernel(const float* part, AttentionOperand y, int H, int D, int64_t T, int64_t rows)
+{
+    typedef typename ElemOf<EK>::type E;
+    const int heads = H / y.share;
+    const int64_t all = rows * heads * D;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int d = (int)(i % D);
+        const int u = (int)(i / D % heads);
+        const int64_t row = i / D / heads;
+        float sum = 0.f;
+        for (int g = 0; g < y.share; ++g) sum += part[(row * H + u * y.share + g) * D + d];
+        const_cast<E*>(static_cast<const E*>(y.p))[row / T * y.batch + row % T * y.token + u * y.head + d] = (E)sum;
+    }
+}
+
+template <int EK>
+__global__ __launch_bounds__(256) void attention_step_kernel(AttentionStepArgs p)
+{
+    typedef typename ElemOf<EK>::type T;
+    __shared__ float lq[256], lk[256], sums[4][64];
+    const int lane = threadIdx.x % 64, group = threadIdx.x / 64;
+    const int b = blockIdx.x, head = blockIdx.y, col = blockIdx.z * 64 + lane;
+    const int entry = p.slots ? p.slots[b] : b;
+    T* o = const_cast<T*>(static_cast<const T*>(p.o.p)) + b * p.o.batch + head * p.o.head;
+    if (entry < 0 || entry >= p.n_states) {
+        if (group == 0 && col < p.DV) o[col] = (T)0.f;
+        return;
+    }
+    if ((int)threadIdx.x < p.DK) {
+        lq[threadIdx.x] = (float)static_cast<const T*>(p.q.p)[b * p.q.batch + head * p.q.head + threadIdx.x];
+        lk[threadIdx.x] = (float)static_cast<const T*>(p.k.p)[b * p.k.batch + head / p.k.share * p.k.head + threadIdx.x];
+    }
+    __syncthreads();
+    float y = 0.f;
+    if (col < p.DV) {
+        const float decay = expf(p.log_decay[head]);
+        const float v = (float)static_cast<const T*>(p.v.p)[b * p.v.batch + head / p.v.share * p.v.head + col];
+        float* state = p.state + ((int64_t)entry * p.H + head) * p.DK * p.DV + col;
+        for (int r = group; r < p.DK; r += 4) {
+            const float s = state[(int64_t)r * p.DV] * decay + lk[r] * v;
+            state[(int64_t)r * p.DV] = s;
+            y += s * lq[r];
+        }
+    }
+    sums[group][lane] = y;
+    __syncthreads();
+    if (group == 0 && col < p.DV) o[col] = (T)(p.scale * (sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane]));
+}
+
+}  // namespace
+
+hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatch& n, int ek, hipStream_t st)
+{
+    const dim3 grid((unsigned)(n.starts ? n.B + 2 : n.B), (unsigned)n.H, (unsigned)((s.DC + kColumns - 1) / kColumns));
+    return with_elem(ek, [&](auto e) {
+        note_kernel("attention_recurrent_kernel", ek, s.DA <= 64 ? 16 : s.DA <= 128 ? 32 : 64);
+        if (s.DA <= 64)
+            hipLaunchKernelGGL((attention_recurrent_kernel<e(), 16>), grid, dim3(kColumns * kGroups), 0, st, s, n);
+        else if (s.DA <= 128)
+            hipLaunchKernelGGL((attention_recurrent_kernel<e(), 32>), grid, dim3(kColumns * kGroups), 0, st, s, n);
+        else
+            hipLaunchKernelGGL((attention_recurrent_kernel<e(), 64>), grid, dim3(kColumns * kGroups), 0, st, s, n);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_attention_fold(const float* part, const AttentionOperand& y, const AttentionBatch& n, int kv_heads, int D, int ek, hipStream_t st)
+{
+    const int64_t rows = n.starts ? n.T : n.T * n.B, all = rows * kv_heads * D;
+    const unsigned groups = (unsigned)(all / 256 + 1 < 8192 ? all / 256 + 1 : 8192);
+    return with_elem(ek, [&](auto e) {
+        hipLaunchKernelGGL(attention_fold_kernel<e()>, dim3(groups), dim3(256), 0, st, part, y, n.H, D, n.starts ? rows : n.T, rows);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_attention_step(const AttentionStepArgs& a, int ek, hipStream_t st)
+{
+    const dim3 grid((unsigned)a.B, (unsigned)a.H, (unsigned)((a.DV + 63) / 64));
+    return with_elem(ek, [&](auto e) {
+        SW_NOTED_LAUNCH(note_kernel("attention_step_kernel", ek), attention_step_kernel<e()>, grid, dim3(256), 0, st, a);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace swconv

@@ -187,6 +187,7 @@ const char* sw_status_string(int status)
         case SW_ERR_ALIAS: return "output overlaps an input";
         case SW_ERR_LAUNCH: return "HIP launch failed";
         case SW_ERR_JIT: return "run-time compilation of a generated kernel failed";
+        case SW_ERR_WORKSPACE: return "a workspace is missing, misaligned or too small";
         default: return "unknown status";
     }
 }

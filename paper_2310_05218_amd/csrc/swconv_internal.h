@@ -8,6 +8,7 @@
 
 #include <memory>
 #include <new>
+#include <type_traits>
 
 namespace swconv {
 
