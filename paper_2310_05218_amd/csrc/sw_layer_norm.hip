@@ -1,46 +1,225 @@
 // Layer norm over the channels of channel-last rows, and its backward pass.
+//
+// Both are bound by memory: a row is read once into registers, folded there, and written once.  A row of V 16-byte vectors has the
+// fewest lanes that hold it in a few vectors each: 8, 16 or 32 lanes (several rows a wavefront), a wavefront, 256 to 1024 threads.
+// Workgroups walk over rows a grid apart: a thread's columns never change, so weight and bias stay in its registers (they are 4 bytes an
+// element, twice a 16-bit row), and the next row is on its way while this one is folded.  Rows of more than 2048 vectors are read again from
+// memory instead.
+//
+// Loads are 16 bytes at any element's address: rows of odd length take one vector of single elements at their end, nothing else.
 #include "sw_layers.h"
 
 namespace swconv {
 
 namespace {
 
-constexpr int kThreads = 256;
+// ---- sums over lanes ----------------------------------------------------------------------------------------------------------
 
-// The sum over a workgroup, in every thread.
-__device__ __forceinline__ float block_sum(float v, float* lds)
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int i = 0; i < kThreads / 64; ++i) s += lds[i];
-    return s;
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-template <int EK>
-__global__ __launch_bounds__(kThreads) void layer_norm_kernel(LayerNormArgs p)
+// The sum over groups of LANES neighbouring lanes (8 to 64), in every lane.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
 {
+    v += dpp_move<0xB1>(v);                          // the neighbour
+    v += dpp_move<0x4E>(v);                          // the other pair of four
+    v += dpp_move<0x141>(v);                         // the other four of eight
+    if constexpr (LANES >= 16) v += dpp_move<0x140>(v);
+    if constexpr (LANES >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (LANES >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+
+// The sums over all LANES threads of a row, in every one of them.  `lds` holds a value for each wavefront and sum, and is written again
+// two calls later: one barrier a call, as a thread that is a call ahead of another has passed the barrier that the other's reads precede.
+template <int LANES, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[LANES / 64 + 1], int& turn)
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = lanes_sum<LANES < 64 ? LANES : 64>(v[k]);
+    if constexpr (LANES > 64) {
+        float(*at)[LANES / 64 + 1] = lds + turn * N;
+        turn ^= 1;
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) at[k][threadIdx.x / 64] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = 0.f;
+#pragma unroll
+            for (int i = 0; i < LANES / 64; ++i) v[k] += at[k][i];
+        }
+    }
+}
+
+// ---- vectors of 16 bytes at any element's address --------------------------------------------------------------------------------
+
+template <int EK>
+struct Row {
     typedef typename ElemOf<EK>::type T;
-    __shared__ float lds[kThreads / 64];
+    static constexpr int VEC = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    typedef float floats __attribute__((ext_vector_type(VEC)));
+    struct __attribute__((packed, aligned(sizeof(T)))) loose {
+        vec v;
+    };
+    struct __attribute__((packed, aligned(4))) loose_floats {
+        floats v;
+    };
+    // elements first ... first + VEC - 1 of C, zeros beyond
+    static __device__ __forceinline__ vec load(const T* row, int first, int C)
+    {
+        if (first + VEC <= C) return reinterpret_cast<const loose*>(row + first)->v;
+        vec v = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) v[e] = row[first + e];
+        return v;
+    }
+    static __device__ __forceinline__ void store(T* row, int first, int C, floats f)
+    {
+        const vec v = __builtin_convertvector(f, vec);
+        if (first + VEC <= C) {
+            reinterpret_cast<loose*>(row + first)->v = v;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) row[first + e] = v[e];
+    }
+    static __device__ __forceinline__ floats load_floats(const float* p, int first, int C, float without)
+    {
+        floats f = without;
+        if (!p) return f;
+        if (first + VEC <= C) return reinterpret_cast<const loose_floats*>(p + first)->v;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) f[e] = p[first + e];
+        return f;
+    }
+    static __device__ __forceinline__ void store_floats(float* p, int first, int C, floats f)
+    {
+        if (first + VEC <= C) {
+            reinterpret_cast<loose_floats*>(p + first)->v = f;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) p[first + e] = f[e];
+    }
+    // zeros in place of what is beyond the row
+    static __device__ __forceinline__ floats within(floats f, int first, int C)
+    {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = first + e < C ? f[e] : 0.f;
+        return f;
+    }
+    static __device__ __forceinline__ float sum(floats f)
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += f[e];
+        return s;
+    }
+};
+
+constexpr int threads_of(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+// ---- forward -----------------------------------------------------------------------------------------------------------------------
+
+// TAIL: C is not LANES * NV whole vectors.
+template <int EK, int LANES, int NV, bool TAIL>
+__global__ __launch_bounds__(threads_of(LANES)) void layer_norm_kernel(LayerNormArgs p)
+{
+    typedef Row<EK> R;
+    typedef typename R::T T;
+    typedef typename R::floats floats;
+    constexpr int kRows = threads_of(LANES) / LANES;        // rows that a workgroup has at a time
+    __shared__ float lds[2][LANES / 64 + 1];
+    int turn = 0;
+    const int lane = threadIdx.x % LANES;
+    const int C = TAIL ? p.C : LANES * NV * R::VEC;
+    const float inv = 1.0f / (float)C;
+    auto at = [&](int i) { return (lane + i * LANES) * R::VEC; };
+    floats w[NV], b[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) w[i] = R::load_floats(p.weight, at(i), C, 1.f), b[i] = R::load_floats(p.bias, at(i), C, 0.f);
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    typename R::vec raw[NV];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[i] = R::load(static_cast<const T*>(p.x) + (r < p.rows ? r : p.rows - 1) * p.x_stride, at(i), C);
+    };
+    fetch(row);
+    // (the rows of a workgroup end together: whole wavefronts and, where a row has several, all of them pass every barrier)
+    for (int64_t first = (int64_t)blockIdx.x * kRows; first < p.rows; first += step, row += step) {
+        floats x[NV];
+        float s[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[i] = __builtin_convertvector(raw[i], floats);
+            s[0] += R::sum(x[i]);
+        }
+        fetch(row + step);
+        row_sums<LANES>(s, lds, turn);
+        const float mean = s[0] * inv;
+        s[0] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            x[i] -= mean;
+            if (TAIL) x[i] = R::within(x[i], at(i), C);
+            s[0] += R::sum(x[i] * x[i]);
+        }
+        row_sums<LANES>(s, lds, turn);
+        const float rstd = 1.0f / sqrtf(s[0] * inv + p.eps);
+        if (row < p.rows) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) R::store(static_cast<T*>(p.y) + row * p.y_stride, at(i), C, x[i] * rstd * w[i] + b[i]);
+            if (lane == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+        }
+    }
+}
+
+// Rows beyond what registers hold: a workgroup a row, which is read three times (the second and third from the caches).
+template <int EK>
+__global__ __launch_bounds__(1024) void layer_norm_long_kernel(LayerNormArgs p)
+{
+    typedef Row<EK> R;
+    typedef typename R::T T;
+    __shared__ float lds[2][17];
+    int turn = 0;
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
         const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
-        T* y = static_cast<T*>(p.y) + row * p.y_stride;
-        float s = 0.f;
-        for (int i = threadIdx.x; i < p.C; i += kThreads) s += (float)x[i];
-        const float mean = block_sum(s, lds) / (float)p.C;
-        s = 0.f;
-        for (int i = threadIdx.x; i < p.C; i += kThreads) {
-            const float d = (float)x[i] - mean;
-            s += d * d;
+        float s[1] = {0.f};
+        for (int i = threadIdx.x * R::VEC; i < p.C; i += 1024 * R::VEC) s[0] += R::sum(__builtin_convertvector(R::load(x, i, p.C), typename R::floats));
+        row_sums<1024>(s, lds, turn);
+        const float mean = s[0] / (float)p.C;
+        s[0] = 0.f;
+        for (int i = threadIdx.x * R::VEC; i < p.C; i += 1024 * R::VEC) {
+            const auto d = R::within(__builtin_convertvector(R::load(x, i, p.C), typename R::floats) - mean, i, p.C);
+            s[0] += R::sum(d * d);
         }
-        const float rstd = 1.0f / sqrtf(block_sum(s, lds) / (float)p.C + p.eps);
-        for (int i = threadIdx.x; i < p.C; i += kThreads) {
-            const float h = ((float)x[i] - mean) * rstd;
-            y[i] = (T)(h * (p.weight ? p.weight[i] : 1.0f) + (p.bias ? p.bias[i] : 0.0f));
-        }
+        row_sums<1024>(s, lds, turn);
+        const float rstd = 1.0f / sqrtf(s[0] / (float)p.C + p.eps);
+        for (int i = threadIdx.x * R::VEC; i < p.C; i += 1024 * R::VEC)
+            R::store(static_cast<T*>(p.y) + row * p.y_stride, i, p.C,
+                     (__builtin_convertvector(R::load(x, i, p.C), typename R::floats) - mean) * rstd * R::load_floats(p.weight, i, p.C, 1.f) +
+                         R::load_floats(p.bias, i, p.C, 0.f));
         if (threadIdx.x == 0) {
             if (p.mean) p.mean[row] = mean;
             if (p.rstd) p.rstd[row] = rstd;
@@ -48,38 +227,100 @@ __global__ __launch_bounds__(kThreads) void layer_norm_kernel(LayerNormArgs p)
     }
 }
 
-template <int EK>
-__global__ __launch_bounds__(kThreads) void layer_norm_dx_kernel(LayerNormBackwardArgs p)
+// ---- backward ----------------------------------------------------------------------------------------------------------------------
+
+// A thread adds dy * h and dy of its columns over its rows in registers; the rows of a workgroup meet in LDS, and a workgroup writes its
+// sums as one row {dweight[C], dbias[C]} of `partial`.
+template <int EK, int LANES, int NV, bool TAIL>
+__global__ __launch_bounds__(threads_of(LANES)) void layer_norm_backward_kernel(LayerNormBackwardArgs p)
 {
-    typedef typename ElemOf<EK>::type T;
-    __shared__ float lds[kThreads / 64];
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
-        const T* dy = static_cast<const T*>(p.dy) + row * p.dy_stride;
-        T* dx = static_cast<T*>(p.dx) + row * p.dx_stride;
-        const float mean = p.mean[row], rstd = p.rstd[row];
-        float sg = 0.f, sgh = 0.f;
-        for (int i = threadIdx.x; i < p.C; i += kThreads) {
-            const float g = (float)dy[i] * (p.weight ? p.weight[i] : 1.0f);
-            sg += g;
-            sgh += g * (((float)x[i] - mean) * rstd);
+    typedef Row<EK> R;
+    typedef typename R::T T;
+    constexpr int kRows = threads_of(LANES) / LANES;
+    __shared__ float lds[4][LANES / 64 + 1];
+    int turn = 0;
+    const int lane = threadIdx.x % LANES;
+    const int C = TAIL ? p.C : LANES * NV * R::VEC;
+    const float inv = 1.0f / (float)C;
+    typename R::floats w[NV], sw[NV], sb[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        w[i] = R::load_floats(p.weight, (lane + i * LANES) * R::VEC, C, 1.f);
+        sw[i] = 0.f, sb[i] = 0.f;
+    }
+    int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / LANES;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    typename R::vec raw_x[NV], raw_dy[NV];
+    float next_mean, next_rstd;
+    auto fetch = [&](int64_t r) {
+        r = r < p.rows ? r : p.rows - 1;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            raw_x[i] = R::load(static_cast<const T*>(p.x) + r * p.x_stride, (lane + i * LANES) * R::VEC, C);
+            raw_dy[i] = R::load(static_cast<const T*>(p.dy) + r * p.dy_stride, (lane + i * LANES) * R::VEC, C);
         }
-        sg = block_sum(sg, lds) / (float)p.C;
-        sgh = block_sum(sgh, lds) / (float)p.C;
-        for (int i = threadIdx.x; i < p.C; i += kThreads) {
-            const float g = (float)dy[i] * (p.weight ? p.weight[i] : 1.0f);
-            const float h = ((float)x[i] - mean) * rstd;
-            dx[i] = (T)(rstd * (g - sg - h * sgh));
+        next_mean = p.mean[r], next_rstd = p.rstd[r];
+    };
+    fetch(row);
+    for (int64_t first = (int64_t)blockIdx.x * kRows; first < p.rows; first += step, row += step) {
+        const float mean = next_mean, rstd = next_rstd;
+        const bool mine = row < p.rows;
+        typename R::floats h[NV], g[NV];
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            h[i] = (__builtin_convertvector(raw_x[i], typename R::floats) - mean) * rstd;
+            if (TAIL) h[i] = R::within(h[i], (lane + i * LANES) * R::VEC, C);
+            g[i] = __builtin_convertvector(raw_dy[i], typename R::floats);      // (zeros beyond the row)
+            if (mine) {
+                sw[i] += g[i] * h[i];
+                sb[i] += g[i];
+            }
+            g[i] *= w[i];
+            s[0] += R::sum(g[i]);
+            s[1] += R::sum(g[i] * h[i]);
+        }
+        fetch(row + step);
+        row_sums<LANES>(s, lds, turn);
+        if (mine && p.dx)
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                R::store(static_cast<T*>(p.dx) + row * p.dx_stride, (lane + i * LANES) * R::VEC, C, rstd * (g[i] - s[0] * inv - h[i] * (s[1] * inv)));
+    }
+    if (!p.partial) return;
+    float* out = p.partial + (int64_t)blockIdx.x * 2 * C;
+    if constexpr (kRows > 1) {
+        // (at most 64 lanes a row: their columns' sums of all rows of the workgroup fit 16 KB)
+        __shared__ typename R::floats meet[2][kRows][LANES];
+        static_assert(NV == 1 || kRows * LANES * NV * sizeof(meet[0][0][0]) <= 32768, "LDS");
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            __syncthreads();
+            meet[0][threadIdx.x / LANES][lane] = sw[i];
+            meet[1][threadIdx.x / LANES][lane] = sb[i];
+            __syncthreads();
+            if (threadIdx.x < 2 * LANES) {
+                const int which = threadIdx.x / LANES;
+                typename R::floats s = meet[which][0][lane];
+                for (int r = 1; r < kRows; ++r) s += meet[which][r][lane];
+                R::store_floats(out + which * C, (lane + i * LANES) * R::VEC, C, s);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            R::store_floats(out, (lane + i * LANES) * R::VEC, C, sw[i]);
+            R::store_floats(out + C, (lane + i * LANES) * R::VEC, C, sb[i]);
         }
     }
 }
 
-// sums of a run of rows, a column per thread: partial[run] = {dweight[C], dbias[C]}
+// Rows beyond what registers hold: the sums of a run of rows a column per thread, then dx a workgroup a row (dx may be written over dy or x).
 template <int EK>
-__global__ __launch_bounds__(kThreads) void layer_norm_sums_kernel(LayerNormBackwardArgs p, int64_t run)
+__global__ __launch_bounds__(256) void layer_norm_long_sums_kernel(LayerNormBackwardArgs p, int64_t run)
 {
     typedef typename ElemOf<EK>::type T;
-    const int i = blockIdx.x * kThreads + threadIdx.x;
+    const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= p.C) return;
     const int64_t first = blockIdx.y * run, last = first + run < p.rows ? first + run : p.rows;
     float sw = 0.f, sb = 0.f;
@@ -92,51 +333,148 @@ __global__ __launch_bounds__(kThreads) void layer_norm_sums_kernel(LayerNormBack
     p.partial[(int64_t)blockIdx.y * 2 * p.C + p.C + i] = sb;
 }
 
-__global__ __launch_bounds__(kThreads) void layer_norm_fold_kernel(const float* partial, int parts, int C, float* dweight, float* dbias)
+template <int EK>
+__global__ __launch_bounds__(1024) void layer_norm_long_dx_kernel(LayerNormBackwardArgs p)
 {
-    const int i = blockIdx.x * kThreads + threadIdx.x;
-    if (i >= C) return;
-    float sw = 0.f, sb = 0.f;
-    for (int k = 0; k < parts; ++k) {
-        sw += partial[(int64_t)k * 2 * C + i];
-        sb += partial[(int64_t)k * 2 * C + C + i];
+    typedef Row<EK> R;
+    typedef typename R::T T;
+    __shared__ float lds[4][17];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        const T* x = static_cast<const T*>(p.x) + row * p.x_stride;
+        const T* dy = static_cast<const T*>(p.dy) + row * p.dy_stride;
+        const float mean = p.mean[row], rstd = p.rstd[row];
+        float s[2] = {0.f, 0.f};
+        auto terms = [&](int i, typename R::floats& g, typename R::floats& h) {
+            g = __builtin_convertvector(R::load(dy, i, p.C), typename R::floats) * R::load_floats(p.weight, i, p.C, 1.f);
+            h = R::within((__builtin_convertvector(R::load(x, i, p.C), typename R::floats) - mean) * rstd, i, p.C);
+        };
+        typename R::floats g, h;
+        for (int i = threadIdx.x * R::VEC; i < p.C; i += 1024 * R::VEC) {
+            terms(i, g, h);
+            s[0] += R::sum(g);
+            s[1] += R::sum(g * h);
+        }
+        row_sums<1024>(s, lds, turn);
+        for (int i = threadIdx.x * R::VEC; i < p.C; i += 1024 * R::VEC) {
+            terms(i, g, h);
+            R::store(static_cast<T*>(p.dx) + row * p.dx_stride, i, p.C, rstd * (g - s[0] / (float)p.C - h * (s[1] / (float)p.C)));
+        }
     }
-    if (dweight) dweight[i] = sw;
-    if (dbias) dbias[i] = sb;
 }
 
-unsigned row_groups(int64_t rows) { return (unsigned)(rows < 65536 ? rows : 65536); }
+// The sums over the rows of `partial` ([parts, 2 C]): 64 columns a workgroup, its wavefronts each a share of the rows, in a fixed order.
+constexpr int kFoldWaves = 16;
+__global__ __launch_bounds__(64 * kFoldWaves) void layer_norm_fold_kernel(const float* partial, int parts, int C, float* dweight, float* dbias)
+{
+    __shared__ float lds[kFoldWaves][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int i = blockIdx.x * 64 + lane;
+    float s = 0.f;
+    if (i < 2 * C)
+        for (int k = wave; k < parts; k += kFoldWaves) s += partial[(int64_t)k * 2 * C + i];
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave || i >= 2 * C) return;
+    for (int k = 1; k < kFoldWaves; ++k) s += lds[k][lane];
+    float* out = i < C ? dweight : dbias;
+    if (out) out[i < C ? i : i - C] = s;
+}
+
+// ---- which lanes ---------------------------------------------------------------------------------------------------------------------
+
+// f(lanes, vectors a lane) for rows of C elements: integral constants, 0 lanes where registers do not hold a row.
+template <int EK, bool BACKWARD, class F>
+hipError_t with_lanes(int64_t C, F&& f)
+{
+    const int64_t v = (C + Row<EK>::VEC - 1) / Row<EK>::VEC;
+#define SW_LANES(l, n) \
+    if (v <= (l) * (n)) return f(std::integral_constant<int, l>(), std::integral_constant<int, n>())
+    SW_LANES(8, 1);
+    SW_LANES(16, 1);
+    SW_LANES(32, 1);
+    SW_LANES(64, 1);
+    SW_LANES(64, 2);
+    SW_LANES(256, 1);
+    SW_LANES(256, 2);
+    SW_LANES(512, 2);
+    if constexpr (BACKWARD) {
+        SW_LANES(512, 4);
+    } else {
+        SW_LANES(1024, 2);
+    }
+#undef SW_LANES
+    return f(std::integral_constant<int, 0>(), std::integral_constant<int, 0>());
+}
+
+constexpr int kCUs = 256;
+
+// Workgroups of a launch: `threads` for every CU, or the rows there are.
+unsigned row_groups(int64_t rows, int lanes, int threads)
+{
+    const int64_t want = (rows * lanes + threads_of(lanes) - 1) / threads_of(lanes), most = kCUs * (threads / threads_of(lanes));
+    return (unsigned)(want < most ? want : most);
+}
+
+constexpr int kForwardThreads = 2048, kBackwardThreads = 1024;
+constexpr int kLongParts = 64;
 
 }  // namespace
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, int ek, hipStream_t st)
 {
     return with_elem(ek, [&](auto e) {
-        SW_NOTED_LAUNCH(note_kernel("layer_norm_kernel", ek), layer_norm_kernel<e()>, dim3(row_groups(a.rows)), dim3(kThreads), 0, st, a);
-        return hipGetLastError();
+        return with_lanes<e(), false>(a.C, [&](auto lanes, auto nv) {
+            if constexpr (lanes() == 0) {
+                SW_NOTED_LAUNCH(note_kernel("layer_norm_long_kernel", ek), layer_norm_long_kernel<e()>, dim3(row_groups(a.rows, 1024, kForwardThreads)), dim3(1024), 0, st, a);
+            } else {
+                const dim3 grid(row_groups(a.rows, lanes(), kForwardThreads)), block(threads_of(lanes()));
+                note_kernel("layer_norm_kernel", ek, lanes(), nv());
+                if (a.C == lanes() * nv() * Row<e()>::VEC)
+                    hipLaunchKernelGGL((layer_norm_kernel<e(), lanes(), nv(), false>), grid, block, 0, st, a);
+                else
+                    hipLaunchKernelGGL((layer_norm_kernel<e(), lanes(), nv(), true>), grid, block, 0, st, a);
+            }
+            return hipGetLastError();
+        });
     });
 }
 
-int layer_norm_backward_parts(int64_t rows, int64_t C) { return (int)(rows < 256 ? rows : 256); }
-
-hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& a, int ek, hipStream_t st)
+int layer_norm_backward_parts(int64_t rows, int64_t)
 {
+    const int64_t most = kCUs * (kBackwardThreads / 256);     // of any format and width
+    return (int)(rows < most ? rows : most);
+}
+
+hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek, hipStream_t st)
+{
+    LayerNormBackwardArgs a = args;
+    if (!a.dweight && !a.dbias) a.partial = nullptr;
     return with_elem(ek, [&](auto e) {
-        // (the sums over rows first: dx may be written over dy or x)
-        if (a.dweight || a.dbias) {
-            const int parts = layer_norm_backward_parts(a.rows, a.C);
-            const unsigned columns = (unsigned)((a.C + kThreads - 1) / kThreads);
-            SW_NOTED_LAUNCH(note_kernel("layer_norm_sums_kernel", ek), layer_norm_sums_kernel<e()>, dim3(columns, parts), dim3(kThreads), 0, st, a,
-                            (a.rows + parts - 1) / parts);
+        return with_lanes<e(), true>(a.C, [&](auto lanes, auto nv) {
+            unsigned parts;
+            if constexpr (lanes() == 0) {
+                parts = (unsigned)(a.rows < kLongParts ? a.rows : kLongParts);
+                note_kernel("layer_norm_long_dx_kernel", ek);
+                if (a.partial) {
+                    hipLaunchKernelGGL(layer_norm_long_sums_kernel<e()>, dim3((a.C + 255) / 256, parts), dim3(256), 0, st, a, (a.rows + parts - 1) / parts);
+                    if (const hipError_t err = hipGetLastError()) return err;
+                }
+                if (a.dx) hipLaunchKernelGGL(layer_norm_long_dx_kernel<e()>, dim3(row_groups(a.rows, 1024, kForwardThreads)), dim3(1024), 0, st, a);
+            } else {
+                parts = row_groups(a.rows, lanes(), kBackwardThreads);
+                const dim3 block(threads_of(lanes()));
+                note_kernel("layer_norm_backward_kernel", ek, lanes(), nv());
+                if (a.C == lanes() * nv() * Row<e()>::VEC)
+                    hipLaunchKernelGGL((layer_norm_backward_kernel<e(), lanes(), nv(), false>), dim3(parts), block, 0, st, a);
+                else
+                    hipLaunchKernelGGL((layer_norm_backward_kernel<e(), lanes(), nv(), true>), dim3(parts), block, 0, st, a);
+            }
             if (const hipError_t err = hipGetLastError()) return err;
-            hipLaunchKernelGGL(layer_norm_fold_kernel, dim3(columns), dim3(kThreads), 0, st, a.partial, parts, a.C, a.dweight, a.dbias);
-            if (const hipError_t err = hipGetLastError()) return err;
-        }
-        if (a.dx) {
-            SW_NOTED_LAUNCH(note_kernel("layer_norm_dx_kernel", ek), layer_norm_dx_kernel<e()>, dim3(row_groups(a.rows)), dim3(kThreads), 0, st, a);
+            if (a.partial)
+                hipLaunchKernelGGL(layer_norm_fold_kernel, dim3((2 * a.C + 63) / 64), dim3(64 * kFoldWaves), 0, st, a.partial, (int)parts, a.C, a.dweight, a.dbias);
             return hipGetLastError();
-        }
-        return hipSuccess;
+        });
     });
 }
 
