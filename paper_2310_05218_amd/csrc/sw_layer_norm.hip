@@ -363,22 +363,39 @@ __global__ __launch_bounds__(1024) void layer_norm_long_dx_kernel(LayerNormBackw
     }
 }
 
-// The sums over the rows of `partial` ([parts, 2 C]): 64 columns a workgroup, its wavefronts each a share of the rows, in a fixed order.
-constexpr int kFoldWaves = 16;
-__global__ __launch_bounds__(64 * kFoldWaves) void layer_norm_fold_kernel(const float* partial, int parts, int C, float* dweight, float* dbias)
+// The sums over the rows of `partial` ([parts, 2 C]), in a fixed order: 32 columns a workgroup, a row of eight 16-byte vectors eight lanes, so
+// that a thread has few rows, all on their way at once (1024 rows of 2 x 4096: 20 us with a wavefront's 64 columns, one row after another).
+constexpr int kFoldThreads = 1024, kFoldRows = kFoldThreads / 8;
+__global__ __launch_bounds__(kFoldThreads) void layer_norm_fold_kernel(const float* partial, int parts, int C, float* dweight, float* dbias)
 {
-    __shared__ float lds[kFoldWaves][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int i = blockIdx.x * 64 + lane;
-    float s = 0.f;
-    if (i < 2 * C)
-        for (int k = wave; k < parts; k += kFoldWaves) s += partial[(int64_t)k * 2 * C + i];
-    lds[wave][lane] = s;
+    typedef Row<kElemF32> R;
+    __shared__ R::floats lds[kFoldThreads / 64][8];
+    const int lane = threadIdx.x % 8, first = threadIdx.x / 8;
+    const int i = blockIdx.x * 32 + lane * 4;
+    R::floats s = 0.f;
+    for (int k = first; k < parts; k += 8 * kFoldRows) {
+        R::floats v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = 0.f;
+            if (k + j * kFoldRows < parts && i < 2 * C) v[j] = R::load(partial + (int64_t)(k + j * kFoldRows) * 2 * C, i, 2 * C);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[j];
+    }
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] += __shfl_xor(s[e], d, 64);
+    if (threadIdx.x % 64 < 8) lds[threadIdx.x / 64][lane] = s;
     __syncthreads();
-    if (wave || i >= 2 * C) return;
-    for (int k = 1; k < kFoldWaves; ++k) s += lds[k][lane];
-    float* out = i < C ? dweight : dbias;
-    if (out) out[i < C ? i : i - C] = s;
+    if (threadIdx.x >= 8) return;
+    for (int k = 1; k < kFoldThreads / 64; ++k) s += lds[k][lane];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        float* out = i + e < C ? dweight : dbias;
+        if (i + e < 2 * C && out) out[i + e < C ? i + e : i + e - C] = s[e];
+    }
 }
 
 // ---- which lanes ---------------------------------------------------------------------------------------------------------------------
@@ -416,7 +433,11 @@ unsigned row_groups(int64_t rows, int lanes, int threads)
     return (unsigned)(want < most ? want : most);
 }
 
-constexpr int kForwardThreads = 2048, kBackwardThreads = 1024;
+constexpr int kForwardThreads = 2048;
+// Backward, where every workgroup adds a row of 2 C sums to fold: rows of a workgroup two on a CU (16384 x 4096 bf16 with four: 81 -> 76 us, the
+// fold 7.6 -> 5), rows of a wavefront or less, whose wavefronts wait for nothing but memory, four (70000 x 200 bf16 with two: 19 -> 29).
+constexpr int kBackwardMost = 1024;
+constexpr int backward_threads(int lanes) { return lanes > 64 ? 512 : kBackwardMost; }
 constexpr int kLongParts = 64;
 
 }  // namespace
@@ -442,7 +463,7 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, int ek, hipStream_t st)
 
 int layer_norm_backward_parts(int64_t rows, int64_t)
 {
-    const int64_t most = kCUs * (kBackwardThreads / 256);     // of any format and width
+    const int64_t most = kCUs * (kBackwardMost / 256);      // of any format and width
     return (int)(rows < most ? rows : most);
 }
 
@@ -462,7 +483,7 @@ hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek,
                 }
                 if (a.dx) hipLaunchKernelGGL(layer_norm_long_dx_kernel<e()>, dim3(row_groups(a.rows, 1024, kForwardThreads)), dim3(1024), 0, st, a);
             } else {
-                parts = row_groups(a.rows, lanes(), kBackwardThreads);
+                parts = row_groups(a.rows, lanes(), backward_threads(lanes()));
                 const dim3 block(threads_of(lanes()));
                 note_kernel("layer_norm_backward_kernel", ek, lanes(), nv());
                 if (a.C == lanes() * nv() * Row<e()>::VEC)
@@ -472,7 +493,7 @@ hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek,
             }
             if (const hipError_t err = hipGetLastError()) return err;
             if (a.partial)
-                hipLaunchKernelGGL(layer_norm_fold_kernel, dim3((2 * a.C + 63) / 64), dim3(64 * kFoldWaves), 0, st, a.partial, (int)parts, a.C, a.dweight, a.dbias);
+                hipLaunchKernelGGL(layer_norm_fold_kernel, dim3((2 * a.C + 31) / 32), dim3(kFoldThreads), 0, st, a.partial, (int)parts, a.C, a.dweight, a.dbias);
             return hipGetLastError();
         });
     });
