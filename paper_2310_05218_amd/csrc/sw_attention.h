@@ -1,0 +1,239 @@
+// What the kernels of linear attention in chunks share: a workgroup's place among sequences and segments, the state on its way between
+// memory and accumulators, outputs on theirs to memory.
+#pragma once
+
+#include "sw_layers.h"
+
+namespace swconv {
+namespace attention {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// l^n for n >= 0, from log2(l): 1 for n = 0, whatever l is; below 2^-126 in steps of 2^-149 (what it is multiplied with may be large)
+__device__ __forceinline__ float power(float g2, int n) { return n == 0 ? 1.f : exp2f(g2 * (float)n); }
+
+__device__ __forceinline__ int64_t clamped(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// Rows [lo, hi) of a packed batch's sequence j - 1, j = 1 ... B; j = 0 and B + 1: the rows before the first and after the last one.
+__device__ __forceinline__ int64_t packed_first(const AttentionBatch& n, int j) { return j == 0 ? 0 : clamped(n.starts[j - 1], 0, n.T); }
+__device__ __forceinline__ int64_t packed_end(const AttentionBatch& n, int j, int64_t lo) { return j == n.B + 1 ? n.T : clamped(n.starts[j], lo, n.T); }
+
+// Where a workgroup is: tokens first ... last - 1, in the order they are worked on, of a sequence of `len` rows from row `lo` of `batch`.
+struct Place {
+    int64_t lo, len, first, last, batch, slot;
+    int seq;
+    bool none;          // nothing here
+    bool rest;          // rows in no sequence
+    bool alone;         // the only segment
+    bool ends;          // the last segment
+};
+
+// Segment places of a packed batch: sequence j's first one is lo / length + j, which leaves each at least one and all they need.
+__device__ __forceinline__ int64_t packed_slot(const AttentionSegments& g, int64_t lo, int j) { return lo / g.length + j; }
+
+__device__ __forceinline__ Place locate(const AttentionBatch& n, const AttentionSegments& g)
+{
+    Place p;
+    p.slot = blockIdx.x;
+    int64_t segment;
+    if (n.starts) {
+        // the last j whose first place is not past this one: 64 of them at a time, a lane each
+        int count = 0;
+        for (int base = 0; base < n.B + 2; base += 64) {
+            const int j = base + (int)(threadIdx.x % 64);
+            const bool before = j < n.B + 2 && packed_slot(g, packed_first(n, j), j) <= p.slot;
+            const int found = __popcll(__ballot(before));
+            count += found;
+            if (found < 64) break;
+        }
+        const int j = count - 1;
+        p.lo = packed_first(n, j);
+        p.len = packed_end(n, j, p.lo) - p.lo;
+        p.rest = j == 0 || j == n.B + 1;
+        p.seq = j - 1;
+        p.batch = 0;
+        segment = p.slot - packed_slot(g, p.lo, j);
+    } else {
+        const int64_t segments = (n.T + g.length - 1) / g.length;
+        p.seq = (int)(p.slot / segments);
+        p.batch = p.seq;
+        segment = p.slot % segments;
+        p.lo = 0;
+        p.len = n.T;
+        p.rest = false;
+    }
+    p.first = segment * g.length;
+    p.last = p.first + g.length < p.len ? p.first + g.length : p.len;
+    p.none = segment > 0 && p.first >= p.len;
+    p.alone = p.len <= g.length;
+    p.ends = p.last >= p.len;
+    return p;
+}
+
+// An entry of `first` or `last`, or null: not given, or out of range
+__device__ __forceinline__ float* entry_of(const AttentionState& st, const AttentionSum& s, const AttentionBatch& n, int seq, int head)
+{
+    if (!st.p) return nullptr;
+    const int entry = s.first_slots ? s.first_slots[seq] : seq;
+    if (s.first_slots && (entry < 0 || entry >= n.n_states)) return nullptr;
+    return st.p + entry * st.entry + head * st.head;
+}
+
+// Row of the state that element r of a lane's half holds in a 32 x 32 accumulator tile (its column is lane % 32).
+__device__ __forceinline__ int tile_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+
+// f(tile, element, offset) for the elements of a lane's column that lie within DA rows: offset, their row's place in memory.  (Rows are
+// counted from the lane's own first one: what is added for an element is the same in all lanes.)
+template <int MT, class F>
+__device__ __forceinline__ void each_row(int DA, int64_t row_stride, F&& f)
+{
+    const int half = threadIdx.x % 64 / 32;
+    const int64_t own = 4 * half * row_stride;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int row = 32 * m + 8 * q;
+            if (row + 8 <= DA) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f(m, 4 * q + e, own + (row + e) * row_stride);
+            } else if (row < DA) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (row + 4 * half + e < DA) f(m, 4 * q + e, own + (row + e) * row_stride);
+            }
+        }
+}
+
+// The state before a segment into the accumulators of the column `col`.
+template <int MT>
+__device__ __forceinline__ void load_state(f32x16 (&S)[MT], const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, const Place& at,
+                                           int head, int col, bool turned)
+{
+    const float* p;
+    int64_t row_stride, col_stride;
+    if (at.alone) {
+        p = entry_of(s.first, s, n, at.seq, head);
+        row_stride = s.first.row, col_stride = s.first.col;
+    } else {
+        p = g.states + (at.slot * n.H + head) * s.DA * s.DC;
+        row_stride = turned ? 1 : s.DC, col_stride = turned ? s.DA : 1;
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) S[m] = 0.f;
+    if (!p || col >= s.DC) return;
+    p += col * col_stride;
+    each_row<MT>(s.DA, row_stride, [&](int m, int r, int64_t offset) { S[m][r] = p[offset]; });
+}
+
+template <int MT>
+__device__ __forceinline__ void store_state(const f32x16 (&S)[MT], float* p, int64_t row_stride, int64_t col_stride, const AttentionSum& s, int col)
+{
+    if (col >= s.DC) return;
+    p += col * col_stride;
+    each_row<MT>(s.DA, row_stride, [&](int m, int r, int64_t offset) { p[offset] = S[m][r]; });
+}
+
+// Zeros in `width` columns from col0 of the rows of a place in no sequence.
+template <class T>
+__device__ __forceinline__ void zero_rows(const AttentionSum& s, const Place& at, int head, int col0, int width)
+{
+    const int64_t all = (at.last - at.first) * width;
+    for (int64_t i = threadIdx.x; i < all; i += blockDim.x) {
+        const int64_t to = at.batch * s.y.batch + (at.lo + at.first + i / width) * s.y.token + head / s.y.share * s.y.head + col0 + i % width;
+        if (s.y_f32)
+            const_cast<float*>(static_cast<const float*>(s.y.p))[to] = 0.f;
+        else
+            const_cast<T*>(static_cast<const T*>(s.y.p))[to] = (T)0.f;
+    }
+}
+
+// Four neighbouring columns of one row, those below `width` of them.
+template <class T>
+__device__ __forceinline__ void store_four(T* p, f32x4 v, int width)
+{
+    typedef T vec __attribute__((ext_vector_type(4)));
+    struct __attribute__((packed, aligned(sizeof(T)))) loose {
+        vec v;
+    };
+    const vec w = __builtin_convertvector(v, vec);
+    if (width >= 4) {
+        reinterpret_cast<loose*>(p)->v = w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < width) p[e] = w[e];
+}
+
+// A 32 x 32 tile of outputs, columns of y down and tokens across, into rows `stride` apart from element `offset` of y on.
+template <class T>
+__device__ __forceinline__ void store_outputs(const f32x16& O, const AttentionSum& s, int64_t offset, int64_t stride, int token, int col)
+{
+    const int half = threadIdx.x % 64 / 32;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int c = col + 8 * q + 4 * half;
+        const f32x4 v = {O[4 * q], O[4 * q + 1], O[4 * q + 2], O[4 * q + 3]};
+        if (s.y_f32)
+            store_four(const_cast<float*>(static_cast<const float*>(s.y.p)) + offset + token * stride + c, v, s.DC - c);
+        else
+            store_four(const_cast<T*>(static_cast<const T*>(s.y.p)) + offset + token * stride + c, v, s.DC - c);
+    }
+}
+
+// Whether a wavefront's accumulators hold an infinity or a NaN anywhere.
+template <int N>
+__device__ __forceinline__ bool any_nonfinite(const f32x16 (&v)[N])
+{
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum = fmaf(v[i][r], 0.f, sum);
+    return __any(sum != 0.f);
+}
+
+// The recurrence itself, on rows first ... last - 1 of a chunk in LDS: what a wavefront does where an infinity or a NaN is about.  In the
+// products of whole chunks these would reach the tokens before theirs, as zero times infinity.  With the state in memory: it is
+// rare, and in registers it would be spelled out for every one of them.  S: the lane's rows of its column.  Tiles have rows `pitch` bytes apart.
+template <class T>
+struct TokenByToken {
+    const unsigned char *a, *b, *c;     // c: at the lane's column; a: null without outputs
+    int pitch, pitch_c, first, last, DA;
+    float decay, alpha_s, alpha_y;
+    bool reverse, y_f32, stores;        // stores: the lane's column is one of y's
+    void* y;                            // row 0, at the lane's column
+    int64_t stride;
+};
+template <class T, int MT>
+__device__ __forceinline__ void token_by_token(float* S, TokenByToken<T> p)
+{
+    const int half = threadIdx.x % 64 / 32;
+#pragma unroll 1
+    for (int t = p.first; t < p.last; ++t) {
+        const float c = p.alpha_s * (float)*reinterpret_cast<const T*>(p.c + t * p.pitch_c);
+        const T *a = reinterpret_cast<const T*>(p.a + t * p.pitch), *b = reinterpret_cast<const T*>(p.b + t * p.pitch);
+        float y = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < 16 * MT; ++i) {
+            const int d = i / 16 * 32 + tile_row(i % 16, half);
+            const float v = fmaf((float)b[d], c, p.reverse ? S[i] : S[i] * p.decay);
+            if (p.a && d < p.DA) y = fmaf((float)a[d], v, y);
+            S[i] = p.reverse ? v * p.decay : v;
+        }
+        if (!p.a) continue;
+        y = p.alpha_y * (y + __shfl_xor(y, 32, 64));
+        if (half || !p.stores) continue;
+        if (p.y_f32)
+            static_cast<float*>(p.y)[t * p.stride] = y;
+        else
+            static_cast<T*>(p.y)[t * p.stride] = (T)y;
+    }
+}
+
+}  // namespace attention
+}  // namespace swconv

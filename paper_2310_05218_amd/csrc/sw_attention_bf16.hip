@@ -1,0 +1,16 @@
+// Linear attention in chunks: the kernels of bf16 operands.
+#include "sw_attention_chunk.h"
+
+namespace swconv {
+
+hipError_t launch_attention_states_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
+{
+    return launch_chunk<kElemBF16, false>(s, n, g, false, st);
+}
+
+hipError_t launch_attention_chunks_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st)
+{
+    return launch_chunk<kElemBF16, true>(s, n, g, turned, st);
+}
+
+}  // namespace swconv

@@ -1,0 +1,16 @@
+// Linear attention in chunks: the kernels of half operands.
+#include "sw_attention_chunk.h"
+
+namespace swconv {
+
+hipError_t launch_attention_states_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
+{
+    return launch_chunk<kElemF16, false>(s, n, g, false, st);
+}
+
+hipError_t launch_attention_chunks_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st)
+{
+    return launch_chunk<kElemF16, true>(s, n, g, turned, st);
+}
+
+}  // namespace swconv

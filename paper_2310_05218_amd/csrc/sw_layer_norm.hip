@@ -63,77 +63,6 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*lds)[LANES / 64 
     }
 }
 
-// ---- vectors of 16 bytes at any element's address --------------------------------------------------------------------------------
-
-template <int EK>
-struct Row {
-    typedef typename ElemOf<EK>::type T;
-    static constexpr int VEC = 16 / sizeof(T);
-    typedef T vec __attribute__((ext_vector_type(VEC)));
-    typedef float floats __attribute__((ext_vector_type(VEC)));
-    struct __attribute__((packed, aligned(sizeof(T)))) loose {
-        vec v;
-    };
-    struct __attribute__((packed, aligned(4))) loose_floats {
-        floats v;
-    };
-    // elements first ... first + VEC - 1 of C, zeros beyond
-    static __device__ __forceinline__ vec load(const T* row, int first, int C)
-    {
-        if (first + VEC <= C) return reinterpret_cast<const loose*>(row + first)->v;
-        vec v = {};
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (first + e < C) v[e] = row[first + e];
-        return v;
-    }
-    static __device__ __forceinline__ void store(T* row, int first, int C, floats f)
-    {
-        const vec v = __builtin_convertvector(f, vec);
-        if (first + VEC <= C) {
-            reinterpret_cast<loose*>(row + first)->v = v;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (first + e < C) row[first + e] = v[e];
-    }
-    static __device__ __forceinline__ floats load_floats(const float* p, int first, int C, float without)
-    {
-        floats f = without;
-        if (!p) return f;
-        if (first + VEC <= C) return reinterpret_cast<const loose_floats*>(p + first)->v;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (first + e < C) f[e] = p[first + e];
-        return f;
-    }
-    static __device__ __forceinline__ void store_floats(float* p, int first, int C, floats f)
-    {
-        if (first + VEC <= C) {
-            reinterpret_cast<loose_floats*>(p + first)->v = f;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-            if (first + e < C) p[first + e] = f[e];
-    }
-    // zeros in place of what is beyond the row
-    static __device__ __forceinline__ floats within(floats f, int first, int C)
-    {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = first + e < C ? f[e] : 0.f;
-        return f;
-    }
-    static __device__ __forceinline__ float sum(floats f)
-    {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) s += f[e];
-        return s;
-    }
-};
-
 constexpr int threads_of(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // ---- forward -----------------------------------------------------------------------------------------------------------------------

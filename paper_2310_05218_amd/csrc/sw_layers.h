@@ -33,6 +33,77 @@ hipError_t with_elem(int ek, F&& f)
     }
 }
 
+// ---- vectors of 16 bytes at any element's address --------------------------------------------------------------------------------
+
+template <int EK>
+struct Row {
+    typedef typename ElemOf<EK>::type T;
+    static constexpr int VEC = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(VEC)));
+    typedef float floats __attribute__((ext_vector_type(VEC)));
+    struct __attribute__((packed, aligned(sizeof(T)))) loose {
+        vec v;
+    };
+    struct __attribute__((packed, aligned(4))) loose_floats {
+        floats v;
+    };
+    // elements first ... first + VEC - 1 of C, zeros beyond
+    static __device__ __forceinline__ vec load(const T* row, int first, int C)
+    {
+        if (first + VEC <= C) return reinterpret_cast<const loose*>(row + first)->v;
+        vec v = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) v[e] = row[first + e];
+        return v;
+    }
+    static __device__ __forceinline__ void store(T* row, int first, int C, floats f)
+    {
+        const vec v = __builtin_convertvector(f, vec);
+        if (first + VEC <= C) {
+            reinterpret_cast<loose*>(row + first)->v = v;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) row[first + e] = v[e];
+    }
+    static __device__ __forceinline__ floats load_floats(const float* p, int first, int C, float without)
+    {
+        floats f = without;
+        if (!p) return f;
+        if (first + VEC <= C) return reinterpret_cast<const loose_floats*>(p + first)->v;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) f[e] = p[first + e];
+        return f;
+    }
+    static __device__ __forceinline__ void store_floats(float* p, int first, int C, floats f)
+    {
+        if (first + VEC <= C) {
+            reinterpret_cast<loose_floats*>(p + first)->v = f;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            if (first + e < C) p[first + e] = f[e];
+    }
+    // zeros in place of what is beyond the row
+    static __device__ __forceinline__ floats within(floats f, int first, int C)
+    {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = first + e < C ? f[e] : 0.f;
+        return f;
+    }
+    static __device__ __forceinline__ float sum(floats f)
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += f[e];
+        return s;
+    }
+};
+
 // ---- layer norm ------------------------------------------------------------------------------------------------------------
 struct LayerNormArgs {
     const void* x;
@@ -85,6 +156,20 @@ struct AttentionBatch {
     int64_t T;
     int B, H, n_states;
 };
+// A long sequence is cut into segments of `length` tokens (a multiple of the chunk) that are worked on side by side: their own sums first
+// (attention_states), the state before each from these (attention_scan), then the outputs (attention_chunks).  length 0: whole sequences.
+struct AttentionSegments {
+    float* states;                      // [segments, H, DA, DC]
+    int64_t length, count;              // count: places for segments in all
+};
+constexpr int kAttentionChunk = 64;
+AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed);     // without `states`
+// a segment's own sum for all but the last of a sequence, into `states`
+hipError_t launch_attention_states(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
+// ... from which the state before each segment of a sequence that has several
+hipError_t launch_attention_scan(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+// the outputs and last states (turned: `states` are those of the sum with DA and DC exchanged)
+hipError_t launch_attention_chunks(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, int ek, hipStream_t st);
 hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatch& n, int ek, hipStream_t st);
 // y[row, u] = sum over the heads of group u of part[row, head], rows of D fp32 each, rounded to the format
 hipError_t launch_attention_fold(const float* part, const AttentionOperand& y, const AttentionBatch& n, int kv_heads, int D, int ek, hipStream_t st);

@@ -90,6 +90,18 @@ int check_dims(const sw_linear_attention_dims& d)
 // Packed rows are counted in 32 bits by `starts`.
 bool packed_too_long(const sw_linear_attention_dims& d, const int32_t* starts) { return starts && d.T > 0x7fffffff; }
 
+AttentionSegments segments_of(const sw_linear_attention_dims& d, bool packed)
+{
+    return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed);
+}
+
+// Bytes of the segments' states (0: whole sequences).
+int64_t state_bytes(const sw_linear_attention_dims& d, bool packed)
+{
+    const AttentionSegments g = segments_of(d, packed);
+    return d.type == SW_F32 || g.length > d.T ? 0 : align16(g.count * d.heads * d.dk * d.dv * 4);
+}
+
 // Bytes of the fp32 rows of dk and of dv that heads sharing them are added from (0: not shared).
 int64_t fold_bytes(const sw_linear_attention_dims& d, bool packed, int width)
 {
@@ -160,10 +172,10 @@ int sw_layer_norm_backward(const void* dy, const void* x, const float* weight, c
     return launch_status(launch_layer_norm_backward(a, type, static_cast<hipStream_t>(hip_stream)));
 }
 
-int64_t sw_linear_attention_workspace_bytes(const sw_linear_attention_dims* dims, int)
+int64_t sw_linear_attention_workspace_bytes(const sw_linear_attention_dims* dims, int packed)
 {
     if (!dims || check_dims(*dims) != SW_OK) return 0;
-    return 0;
+    return state_bytes(*dims, packed != 0);
 }
 
 int sw_linear_attention(const void* q, const void* k, const void* v, void* o, const float* log_decay, const float* state, float* final_state,
@@ -201,13 +213,22 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
     const AttentionState first{const_cast<float*>(state), states, per_head, d.dv, 1}, last{final_state, states, per_head, d.dv, 1};
     const AttentionSum s{tq.op, tk.op, tv.op, to.op, first, last, slots, d.dk, d.dv, 1.0f, d.scale, false, false};
     const AttentionBatch n{log_decay, starts, d.T, d.B, d.heads, d.n_states};
-    return launch_status(launch_attention_recurrent(s, n, d.type, static_cast<hipStream_t>(hip_stream)));
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    AttentionSegments g = segments_of(d, starts != nullptr);
+    g.states = static_cast<float*>(workspace);
+    hipError_t e = hipSuccess;
+    if (need) {
+        e = launch_attention_states(s, n, g, d.type, st);
+        if (e == hipSuccess) e = launch_attention_scan(s, n, g, st);
+    }
+    if (e == hipSuccess) e = launch_attention_chunks(s, n, g, false, d.type, st);
+    return launch_status(e);
 }
 
 int64_t sw_linear_attention_backward_workspace_bytes(const sw_linear_attention_dims* dims, int packed)
 {
     if (!dims || check_dims(*dims) != SW_OK) return 0;
-    return fold_bytes(*dims, packed != 0, dims->dk) + fold_bytes(*dims, packed != 0, dims->dv);
+    return fold_bytes(*dims, packed != 0, dims->dk) + fold_bytes(*dims, packed != 0, dims->dv) + 2 * state_bytes(*dims, packed != 0);
 }
 
 int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, const void* v, const float* log_decay, const float* state,
@@ -261,15 +282,24 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     // where heads share rows of k and v their gradients are added from fp32 rows of each head
     float *part_k = static_cast<float*>(workspace), *part_v = part_k + fold_bytes(d, starts != nullptr, d.dk) / 4;
     auto part = [&](float* p, int width) { return AttentionOperand{p, d.T * d.heads * width, (int64_t)d.heads * width, width, 1}; };
-    hipError_t e = launch_attention_recurrent({tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false}, n, d.type, st);
-    if (e == hipSuccess)
-        e = launch_attention_recurrent({tv.op, tdo.op, tq.op, share > 1 ? part(part_k, d.dk) : tdk.op, turned_final, none, nullptr, d.dv, d.dk,
-                                        d.scale, 1.0f, true, share > 1},
-                                       n, d.type, st);
-    if (e == hipSuccess)
-        e = launch_attention_recurrent({tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale,
-                                        1.0f, true, share > 1},
-                                       n, d.type, st);
+    const AttentionSum of_q{tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false};
+    const AttentionSum of_k{tv.op, tdo.op, tq.op, share > 1 ? part(part_k, d.dk) : tdk.op, turned_final, none, nullptr, d.dv, d.dk, d.scale, 1.0f, true, share > 1};
+    const AttentionSum of_v{tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale, 1.0f, true, share > 1};
+    // the states before each segment, forwards (those of the forward call) and backwards in time
+    AttentionSegments ahead = segments_of(d, starts != nullptr), back = ahead;
+    const int64_t bytes = state_bytes(d, starts != nullptr);
+    ahead.states = part_v + fold_bytes(d, starts != nullptr, d.dv) / 4, back.states = ahead.states + bytes / 4;
+    hipError_t e = hipSuccess;
+    if (bytes) {
+        const AttentionSum forward{tq.op, tk.op, tv.op, tdo.op, {const_cast<float*>(state), states, per_head, d.dv, 1}, none, slots, d.dk, d.dv, 1.0f, d.scale, false, false};
+        e = launch_attention_states(forward, n, ahead, d.type, st);
+        if (e == hipSuccess) e = launch_attention_scan(forward, n, ahead, st);
+        if (e == hipSuccess) e = launch_attention_states(of_v, n, back, d.type, st);
+        if (e == hipSuccess) e = launch_attention_scan(of_v, n, back, st);
+    }
+    if (e == hipSuccess) e = launch_attention_chunks(of_q, n, ahead, true, d.type, st);
+    if (e == hipSuccess) e = launch_attention_chunks(of_k, n, back, true, d.type, st);
+    if (e == hipSuccess) e = launch_attention_chunks(of_v, n, back, false, d.type, st);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_k, tdk.op, n, d.kv_heads, d.dk, d.type, st);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_v, tdv.op, n, d.kv_heads, d.dv, d.type, st);
     return launch_status(e);

@@ -1,5 +1,5 @@
 // Linear attention with a decay for each head, token by token: the recurrence as it stands, for prompts, gradients and single tokens.
-#include "sw_layers.h"
+#include "sw_attention.h"
 
 namespace swconv {
 
@@ -86,6 +86,43 @@ __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel
     }
 }
 
+// The state before each segment from the segments' own sums, in place: a thread has one element of a sequence's and head's.
+constexpr int kScanAhead = 8;       // sums on their way at once
+__global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSum s, AttentionBatch n, AttentionSegments g)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
+    if (i >= s.DA * s.DC) return;
+    const float g2 = n.log_decay[head] * 1.44269504088896341f;
+    // (an infinity fades to none: where l is above zero, so is its power)
+    const float decay = g2 > -INFINITY ? fmaxf(__builtin_amdgcn_exp2f(g2 * (float)g.length), 1e-38f) : 0.f;
+    const int64_t step = (int64_t)n.H * s.DA * s.DC;
+    for (int seq = blockIdx.z; seq < n.B; seq += gridDim.z) {
+        int64_t len = n.T, slot;
+        if (n.starts) {
+            const int64_t lo = attention::packed_first(n, seq + 1);
+            len = attention::packed_end(n, seq + 1, lo) - lo;
+            slot = attention::packed_slot(g, lo, seq + 1);
+        } else {
+            slot = seq * ((n.T + g.length - 1) / g.length);
+        }
+        const int64_t segments = (len + g.length - 1) / g.length;
+        if (segments < 2) continue;
+        const float* first = attention::entry_of(s.first, s, n, seq, head);
+        float state = first ? first[i / s.DC * s.first.row + i % s.DC * s.first.col] : 0.f;
+        float* p = g.states + slot * step + (int64_t)head * s.DA * s.DC + i;
+        for (int64_t k = 0; k < segments; k += kScanAhead) {
+            float own[kScanAhead];
+#pragma unroll
+            for (int j = 0; j < kScanAhead; ++j) own[j] = k + j + 1 < segments ? p[(k + j) * step] : 0.f;
+#pragma unroll
+            for (int j = 0; j < kScanAhead; ++j) {
+                if (k + j < segments) p[(k + j) * step] = state;
+                state = fmaf(state, decay, own[j]);
+            }
+        }
+    }
+}
+
 template <int EK>
 __global__ __launch_bounds__(256) void attention_fold_kernel(const float* part, AttentionOperand y, int H, int D, int64_t T, int64_t rows)
 {
@@ -151,6 +188,44 @@ hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatc
             hipLaunchKernelGGL((attention_recurrent_kernel<e(), 64>), grid, dim3(kColumns * kGroups), 0, st, s, n);
         return hipGetLastError();
     });
+}
+
+hipError_t launch_attention_states_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+hipError_t launch_attention_chunks_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st);
+hipError_t launch_attention_states_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+hipError_t launch_attention_chunks_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st);
+
+hipError_t launch_attention_states(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
+{
+    return ek == kElemBF16 ? launch_attention_states_bf16(s, n, g, st) : launch_attention_states_f16(s, n, g, st);
+}
+
+hipError_t launch_attention_chunks(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, int ek, hipStream_t st)
+{
+    if (ek == kElemF32) return launch_attention_recurrent(s, n, ek, st);
+    return ek == kElemBF16 ? launch_attention_chunks_bf16(s, n, g, turned, st) : launch_attention_chunks_f16(s, n, g, turned, st);
+}
+
+AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed)
+{
+    const int64_t rows = packed ? n.T : n.T * n.B, columns = (DC + 127) / 128;
+    AttentionSegments g{nullptr, (int64_t)1 << 62, 0};
+    const int64_t want = 512;          // workgroups
+    if ((packed ? 1 : n.B) * n.H * columns < want) {
+        const int64_t length = (rows * n.H * columns + want - 1) / want;
+        const int64_t chunks = (length + kAttentionChunk - 1) / kAttentionChunk;
+        if (chunks * kAttentionChunk < n.T) g.length = (chunks < 2 ? 2 : chunks) * kAttentionChunk;
+    }
+    if (g.length >= n.T) g.length = (int64_t)1 << 62;
+    g.count = packed ? n.T / g.length + n.B + 2 : n.B * ((n.T + g.length - 1) / g.length);
+    return g;
+}
+
+hipError_t launch_attention_scan(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
+{
+    const dim3 grid((unsigned)((s.DA * s.DC + 255) / 256), (unsigned)n.H, (unsigned)(n.B < 65535 ? n.B : 65535));
+    hipLaunchKernelGGL(attention_scan_kernel, grid, dim3(256), 0, st, s, n, g);
+    return hipGetLastError();
 }
 
 hipError_t launch_attention_fold(const float* part, const AttentionOperand& y, const AttentionBatch& n, int kv_heads, int D, int ek, hipStream_t st)
