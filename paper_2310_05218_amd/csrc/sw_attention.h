@@ -7,7 +7,6 @@
 namespace swconv {
 namespace attention {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -37,7 +36,7 @@ __device__ __forceinline__ int64_t packed_slot(const AttentionSegments& g, int64
 __device__ __forceinline__ Place locate(const AttentionBatch& n, const AttentionSegments& g)
 {
     Place p;
-    p.slot = blockIdx.x;
+    p.slot = blockIdx.x / (unsigned)n.H;
     int64_t segment;
     if (n.starts) {
         // the last j whose first place is not past this one: 64 of them at a time, a lane each
@@ -82,35 +81,30 @@ __device__ __forceinline__ float* entry_of(const AttentionState& st, const Atten
     return st.p + entry * st.entry + head * st.head;
 }
 
-// Row of the state that element r of a lane's half holds in a 32 x 32 accumulator tile (its column is lane % 32).
-__device__ __forceinline__ int tile_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
+// An accumulator tile is 16 x 16: a lane has column lane % 16, rows 4 (lane / 16) ... + 3.
 
 // f(tile, element, offset) for the elements of a lane's column that lie within DA rows: offset, their row's place in memory.  (Rows are
 // counted from the lane's own first one: what is added for an element is the same in all lanes.)
 template <int MT, class F>
 __device__ __forceinline__ void each_row(int DA, int64_t row_stride, F&& f)
 {
-    const int half = threadIdx.x % 64 / 32;
-    const int64_t own = 4 * half * row_stride;
+    const int own = 4 * (threadIdx.x % 64 / 16);
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT; ++m) {
+        if (16 * m + 16 <= DA) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int row = 32 * m + 8 * q;
-            if (row + 8 <= DA) {
+            for (int e = 0; e < 4; ++e) f(m, e, own * row_stride + (16 * m + e) * row_stride);
+        } else if (16 * m < DA) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f(m, 4 * q + e, own + (row + e) * row_stride);
-            } else if (row < DA) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (row + 4 * half + e < DA) f(m, 4 * q + e, own + (row + e) * row_stride);
-            }
+            for (int e = 0; e < 4; ++e)
+                if (16 * m + own + e < DA) f(m, e, own * row_stride + (16 * m + e) * row_stride);
         }
+    }
 }
 
 // The state before a segment into the accumulators of the column `col`.
 template <int MT>
-__device__ __forceinline__ void load_state(f32x16 (&S)[MT], const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, const Place& at,
+__device__ __forceinline__ void load_state(f32x4 (&S)[MT], const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, const Place& at,
                                            int head, int col, bool turned)
 {
     const float* p;
@@ -126,15 +120,15 @@ __device__ __forceinline__ void load_state(f32x16 (&S)[MT], const AttentionSum& 
     for (int m = 0; m < MT; ++m) S[m] = 0.f;
     if (!p || col >= s.DC) return;
     p += col * col_stride;
-    each_row<MT>(s.DA, row_stride, [&](int m, int r, int64_t offset) { S[m][r] = p[offset]; });
+    each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { S[m][e] = p[offset]; });
 }
 
 template <int MT>
-__device__ __forceinline__ void store_state(const f32x16 (&S)[MT], float* p, int64_t row_stride, int64_t col_stride, const AttentionSum& s, int col)
+__device__ __forceinline__ void store_state(const f32x4 (&S)[MT], float* p, int64_t row_stride, int64_t col_stride, const AttentionSum& s, int col)
 {
     if (col >= s.DC) return;
     p += col * col_stride;
-    each_row<MT>(s.DA, row_stride, [&](int m, int r, int64_t offset) { p[offset] = S[m][r]; });
+    each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { p[offset] = S[m][e]; });
 }
 
 // Zeros in `width` columns from col0 of the rows of a place in no sequence.
@@ -169,70 +163,60 @@ __device__ __forceinline__ void store_four(T* p, f32x4 v, int width)
         if (e < width) p[e] = w[e];
 }
 
-// A 32 x 32 tile of outputs, columns of y down and tokens across, into rows `stride` apart from element `offset` of y on.
-template <class T>
-__device__ __forceinline__ void store_outputs(const f32x16& O, const AttentionSum& s, int64_t offset, int64_t stride, int token, int col)
-{
-    const int half = threadIdx.x % 64 / 32;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int c = col + 8 * q + 4 * half;
-        const f32x4 v = {O[4 * q], O[4 * q + 1], O[4 * q + 2], O[4 * q + 3]};
-        if (s.y_f32)
-            store_four(const_cast<float*>(static_cast<const float*>(s.y.p)) + offset + token * stride + c, v, s.DC - c);
-        else
-            store_four(const_cast<T*>(static_cast<const T*>(s.y.p)) + offset + token * stride + c, v, s.DC - c);
-    }
-}
-
 // Whether a wavefront's accumulators hold an infinity or a NaN anywhere.
 template <int N>
-__device__ __forceinline__ bool any_nonfinite(const f32x16 (&v)[N])
+__device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[N])
 {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sum = fmaf(v[i][r], 0.f, sum);
+        for (int e = 0; e < 4; ++e) sum = fmaf(v[i][e], 0.f, sum);
     return __any(sum != 0.f);
 }
 
-// The recurrence itself, on rows first ... last - 1 of a chunk in LDS: what a wavefront does where an infinity or a NaN is about.  In the
-// products of whole chunks these would reach the tokens before theirs, as zero times infinity.  With the state in memory: it is
-// rare, and in registers it would be spelled out for every one of them.  S: the lane's rows of its column.  Tiles have rows `pitch` bytes apart.
+// The recurrence itself, straight from memory: what a wavefront does once more with a segment that has an infinity or a NaN about.  In the
+// products of whole chunks these reach the tokens before theirs, as zero times infinity.  It is rare, and the state lies in (private)
+// memory so that nothing here takes registers from the loop it stands behind.  The operands' row 0 is the segment's first token.
 template <class T>
 struct TokenByToken {
-    const unsigned char *a, *b, *c;     // c: at the lane's column; a: null without outputs
-    int pitch, pitch_c, first, last, DA;
+    const T *a, *b, *c;                 // c: at the lane's column; a: null without outputs
+    int64_t step_a, step_b, step_c, step_y, tokens;
+    int DA;
     float decay, alpha_s, alpha_y;
-    bool reverse, y_f32, stores;        // stores: the lane's column is one of y's
-    void* y;                            // row 0, at the lane's column
-    int64_t stride;
+    bool reverse, y_f32, column;        // column: the lane's is one of c's and y's
+    void* y;                            // at the lane's column
 };
 template <class T, int MT>
-__device__ __forceinline__ void token_by_token(float* S, TokenByToken<T> p)
+__device__ __forceinline__ void token_by_token(f32x4 (&S)[MT], const TokenByToken<T>& p)
 {
-    const int half = threadIdx.x % 64 / 32;
+    const int own = 4 * (threadIdx.x % 64 / 16);
+    float held[4 * MT];
+#pragma unroll
+    for (int i = 0; i < 4 * MT; ++i) held[i] = S[i / 4][i % 4];
 #pragma unroll 1
-    for (int t = p.first; t < p.last; ++t) {
-        const float c = p.alpha_s * (float)*reinterpret_cast<const T*>(p.c + t * p.pitch_c);
-        const T *a = reinterpret_cast<const T*>(p.a + t * p.pitch), *b = reinterpret_cast<const T*>(p.b + t * p.pitch);
+    for (int64_t t = 0; t < p.tokens; ++t) {
+        const float c = p.column ? p.alpha_s * (float)p.c[t * p.step_c] : 0.f;
         float y = 0.f;
 #pragma unroll 1
-        for (int i = 0; i < 16 * MT; ++i) {
-            const int d = i / 16 * 32 + tile_row(i % 16, half);
-            const float v = fmaf((float)b[d], c, p.reverse ? S[i] : S[i] * p.decay);
-            if (p.a && d < p.DA) y = fmaf((float)a[d], v, y);
-            S[i] = p.reverse ? v * p.decay : v;
+        for (int i = 0; i < 4 * MT; ++i) {
+            const int d = i / 4 * 16 + own + i % 4;
+            if (d >= p.DA) continue;
+            const float v = fmaf((float)p.b[t * p.step_b + d], c, p.reverse ? held[i] : held[i] * p.decay);
+            if (p.a) y = fmaf((float)p.a[t * p.step_a + d], v, y);
+            held[i] = p.reverse ? v * p.decay : v;
         }
         if (!p.a) continue;
+        y += __shfl_xor(y, 16, 64);
         y = p.alpha_y * (y + __shfl_xor(y, 32, 64));
-        if (half || !p.stores) continue;
+        if (own || !p.column) continue;
         if (p.y_f32)
-            static_cast<float*>(p.y)[t * p.stride] = y;
+            static_cast<float*>(p.y)[t * p.step_y] = y;
         else
-            static_cast<T*>(p.y)[t * p.stride] = (T)y;
+            static_cast<T*>(p.y)[t * p.step_y] = (T)y;
     }
+#pragma unroll
+    for (int i = 0; i < 4 * MT; ++i) S[i / 4][i % 4] = held[i];
 }
 
 }  // namespace attention

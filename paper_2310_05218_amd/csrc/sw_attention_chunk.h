@@ -2,11 +2,14 @@
 //
 // A chunk of n tokens (rows i, j of a, b, c; state S before it; l the head's decay; e0 = 1 forwards in time, 0 backwards):
 //     y_i = alpha_y [ alpha_s sum_{j<=i} l^(i-j) (a_i . b_j) c_j  +  l^(i+e0) S^T a_i ],   S <- l^n S + alpha_s sum_j l^(n-e0-j) b_j c_j^T
-// A wavefront has 32 columns of c and y and all rows of their state, in its accumulators: the state never leaves registers while a
+// A wavefront has 16 columns of c and y and all rows of their state, in its accumulators: the state never leaves registers while a
 // segment lasts.  Operands are arranged so that results become operands where they are: an accumulator's column is a lane's, its rows
-// {0-3, 8-11, 16-19, 24-27} + 4 (lane / 32); a product's K order is free as long as both operands have the same, so S as it lies is the
-// operand of S^T a, with a's values picked in that order.  Outputs are computed transposed (rows: columns of y), so that a lane holds
-// four neighbouring columns of one token.  Pair products are shared: each 32 x 32 tile is computed by one wavefront and handed round in LDS.
+// 4 (lane / 16) ... + 3 of sixteen; a product's K order is free as long as both operands have the same, so two tiles of S as they lie are
+// the operand of S^T a, with a's values picked in that order.  Outputs are computed transposed (rows: columns of y), so that a lane holds
+// four neighbouring columns of one token.  Pair products are shared: each 16 x 16 tile is computed by one wavefront and handed round in LDS.
+//
+// Why 16 columns: with 32, and half as many wavefronts, the state and what it meets take 250 registers, operands come from LDS one wait
+// after another, and two wavefronts a SIMD hide little of it (4 x 4096 tokens, 16 heads of 128: 105 us an output pass).
 //
 // Operands derived in fp32 enter a product as sums of 16-bit values, and which sums is a choice of precision: pair products two bf16
 // values (17 bits; half, whose range they may leave, meets c as two bf16 values too), the state two bf16 values or one half scaled by a
@@ -28,17 +31,59 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+// c + a b, 16 x 16 over 32: a's row and b's column lane % 16, K 8 (lane / 16) ... + 7
+__device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// v as a sum of N values of a format: v rounded, the rest rounded, ...
+// Two values rounded to 16 bits, packed, and two packed ones widened.
+template <class V>
+__device__ __forceinline__ unsigned pack(float a, float b)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    const f32x2 p = {a, b};
+    if constexpr (__is_same(V, bf16x8))
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(p, bf16x2));
+    else
+        return __builtin_bit_cast(unsigned, __builtin_convertvector(p, f16x2));
+}
+template <class V>
+__device__ __forceinline__ f32x2 widen(unsigned p)
+{
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (__is_same(V, bf16x8))
+        return (f32x2){__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u)};
+    else
+        return __builtin_convertvector(__builtin_bit_cast(f16x2, p), f32x2);
+}
+template <class V>
+__device__ __forceinline__ f32x8 widened(V v)
+{
+    const u32x4 u = __builtin_bit_cast(u32x4, v);
+    f32x8 f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const f32x2 w = widen<V>(u[j]);
+        f[2 * j] = w[0], f[2 * j + 1] = w[1];
+    }
+    return f;
+}
+
+// v as a sum of N values of a format: v rounded, the rest rounded, ...  (In pairs: converted one by one the compiler converts each twice.)
 template <class V, int N>
 __device__ __forceinline__ void parts(f32x8 v, V (&p)[N])
 {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        p[k] = __builtin_convertvector(v, V);
-        if (k + 1 < N) v -= __builtin_convertvector(p[k], f32x8);
+        u32x4 u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = pack<V>(v[2 * j], v[2 * j + 1]);
+        p[k] = __builtin_bit_cast(V, u);
+        if (k + 1 < N) {
+            const f32x8 w = widened<V>(p[k]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] -= w[j];
+        }
     }
 }
 
@@ -75,11 +120,11 @@ __device__ __forceinline__ V joined(u32x2 a, u32x2 b)
     return __builtin_bit_cast(V, (u32x4){a[0], a[1], b[0], b[1]});
 }
 
-// The operand (column m0 + lane % 32, rows k0 + 8 (lane / 32) ... + 7) of a tile that lies row by row, m0 and k0 constants.
+// The operand (column m0 + lane % 16, rows k0 + 8 (lane / 16) ... + 7) of a tile that lies row by row, m0 and k0 constants.
 template <int W>
 __device__ __forceinline__ const unsigned char* turned_base(const unsigned char* tile, int lane)
 {
-    return tile + (8 * (lane / 32) + lane % 16 / 4) * pitch_of(W) + 2 * (16 * (lane / 16 % 2) + 4 * (lane % 4));
+    return tile + (8 * (lane / 16) + lane % 16 / 4) * pitch_of(W) + 8 * (lane % 4);
 }
 template <int W, class V>
 __device__ __forceinline__ V turned(const unsigned char* base, int m0, int k0)
@@ -87,33 +132,58 @@ __device__ __forceinline__ V turned(const unsigned char* base, int m0, int k0)
     return joined<V>(turned_read(base + k0 * pitch_of(W) + 2 * m0), turned_read(base + (k0 + 4) * pitch_of(W) + 2 * m0));
 }
 
+// A lane's number that the compiler takes for new: what is worked out from it is worked out again, not kept in registers from chunk to chunk.
+__device__ __forceinline__ int renewed(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // A tile of kAttentionChunk rows of W values on its way from memory to LDS: rows `from` and on, `width` elements, zeros elsewhere.
+// Whole vectors are loaded by all threads without a branch, those that have none from a place that has one, and become zeros on their way
+// into LDS: with loads in branches the compiler waits for each tile's before it begins the next one's (105 -> 60 us an output pass of
+// 4 x 4096 tokens, 16 heads of 128).  Rows that are no whole number of vectors go element by element, when the tile is written.
 template <int EK, int W, int THREADS>
 struct Staged {
     typedef Row<EK> R;
-    static constexpr int NCH = W / 8, N = kAttentionChunk * NCH / THREADS, STEP = THREADS / NCH;
+    typedef typename R::T T;
+    static constexpr int NCH = W / 8, ALL = kAttentionChunk * NCH, N = (ALL + THREADS - 1) / THREADS, STEP = THREADS / NCH;
+    static_assert(THREADS % NCH == 0 && (ALL % THREADS == 0 || ALL < THREADS), "whole rows, by all threads or each by one");
     typename R::vec v[N];
-    // offset: of row 0, where there is one
-    __device__ __forceinline__ void fetch(const AttentionOperand& o, int64_t offset, int64_t stride, int from, int width)
+    // `tile`: the first of the 64 rows in memory (its last, backwards in time), where there is one; `step`: from one to the next.  An element's
+    // place is a 32-bit distance from it: rows that are further apart than that allows are no case for this kernel.
+    static __device__ __forceinline__ unsigned place(int row, bool reverse, unsigned step) { return (reverse ? kAttentionChunk - 1 - row : row) * step; }
+    __device__ __forceinline__ void fetch(const T* tile, unsigned step, bool reverse, int from, int width)
     {
-        const int c = threadIdx.x % NCH * 8, row = threadIdx.x / NCH;
-        const typename R::T* p = static_cast<const typename R::T*>(o.p) + offset + row * stride;
+        if (width % 8) return;
+        const int thread = renewed(threadIdx.x), c = thread % NCH * 8;
+        int row = thread / NCH;
+        if (ALL < THREADS) row %= kAttentionChunk;
+        const unsigned col = c < width ? c : 0;
 #pragma unroll
-        for (int k = 0; k < N; ++k) v[k] = (typename R::vec){};
-        if (width % 8 == 0) {
-            if (c >= width) return;
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (row + k * STEP >= from) v[k] = reinterpret_cast<const typename R::loose*>(p + k * STEP * stride + c)->v;
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (row + k * STEP >= from && c < width) v[k] = R::load(p + k * STEP * stride, c, width);
+        for (int k = 0; k < N; ++k) {
+            int r = row + k * STEP;
+            if (from > 0) r = r < from ? from : r;
+            v[k] = reinterpret_cast<const typename R::loose*>(reinterpret_cast<const char*>(tile) + (place(r, reverse, step) + col) * (unsigned)sizeof(T))->v;
         }
     }
-    __device__ __forceinline__ void put(unsigned char* tile) const
+    __device__ __forceinline__ void put(unsigned char* to, const T* tile, unsigned step, bool reverse, int from, int width)
     {
-        unsigned char* p = tile + threadIdx.x / NCH * pitch_of(W) + threadIdx.x % NCH * 16;
+        const int thread = renewed(threadIdx.x), c = thread % NCH * 8, row = thread / NCH;
+        if (width % 8) {
+#pragma unroll 1
+            for (int i = thread; i < kAttentionChunk * W; i += THREADS) {
+                const int r = i / W, d = i % W;
+                *reinterpret_cast<T*>(to + r * pitch_of(W) + 2 * d) = r >= from && d < width ? tile[place(r, reverse, step) + d] : (T)0.f;
+            }
+            return;
+        }
+        if (from > 0 || width < W)
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (row + k * STEP < from || c >= width) v[k] = (typename R::vec){};
+        if (ALL < THREADS && thread >= ALL) return;
+        unsigned char* p = to + row * pitch_of(W) + thread % NCH * 16;
 #pragma unroll
         for (int k = 0; k < N; ++k) *reinterpret_cast<typename R::vec*>(p + k * STEP * pitch_of(W)) = v[k];
     }
@@ -121,9 +191,12 @@ struct Staged {
 
 // ---- the state as an operand -----------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float larger_half(float v)
+// The largest of the lanes that have a column.
+__device__ __forceinline__ float column_largest(float v)
 {
-    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
@@ -135,9 +208,9 @@ __device__ __forceinline__ int half_exponent(float largest)
     return (e < -30 ? -30 : e > 100 ? 100 : e) - 14;
 }
 
-// O = S^T a: rows, columns of y; columns, the chunk's tokens.  `a`: row lane % 32 of the tile, at the half's place.
+// O = S^T a: rows, columns of y; columns, the chunk's tokens.  `a`: row lane % 16 of the tile, at the lane's place.
 template <int EK, int MT>
-__device__ __forceinline__ void state_times_a(const f32x16 (&S)[MT], float frame, const unsigned char* a, f32x16 (&O)[2], const float (&reach)[2])
+__device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT], float frame, const unsigned char* a, f32x4 (&O)[4], const float (&reach)[4])
 {
     typedef typename Operand<EK>::vec V;
     float in = 1.f, out = 1.f;
@@ -147,64 +220,72 @@ __device__ __forceinline__ void state_times_a(const f32x16 (&S)[MT], float frame
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) largest = fmaxf(largest, fabsf(S[m][r]));
+            for (int e = 0; e < 4; ++e) largest = fmaxf(largest, fabsf(S[m][e]));
         largest *= frame;
 #pragma unroll
-        for (int d = 1; d < 32; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d, 64));
-        largest = larger_half(largest);
-        const int e = half_exponent(largest);
+        for (int d = 1; d < 16; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d, 64));
+        const int e = half_exponent(column_largest(largest));
         in = frame * __builtin_amdgcn_ldexpf(1.f, -e);
         out = __builtin_amdgcn_ldexpf(1.f, e);
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < MT / 2; ++m) {
+        f32x8 v;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            f32x8 v;
+        for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][e % 4] * in : S[2 * m + e / 4][e % 4];
+        V p[Operand<EK>::kState];
+        parts(v, p);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[m][8 * q + e] * in : S[m][8 * q + e];
-            V p[Operand<EK>::kState];
-            parts(v, p);
+        for (int i = 0; i < 4; ++i) {
+            const unsigned char* at = a + 16 * i * pitch_of(16 * MT) + 64 * m;
+            const V x = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 32));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const unsigned char* at = a + 32 * i * pitch_of(32 * MT) + 64 * m + 32 * q;
-                const V x = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 16));
-#pragma unroll
-                for (int k = Operand<EK>::kState; k-- > 0;) O[i] = multiply(p[k], x, O[i]);
-            }
+            for (int k = Operand<EK>::kState; k-- > 0;) O[i] = multiply(p[k], x, O[i]);
         }
+    }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) O[i] *= reach[i] * out;
+    for (int i = 0; i < 4; ++i) O[i] *= reach[i] * out;
 }
 
-// S <- whole S + sum over the chunk's tokens of b times w (w: weighted c, tokens 16 k + 8 (lane / 32) + e).
+// S <- whole S + sum over the chunk's tokens of b times weighted c (tokens 32 k + 8 (lane / 16) + e: weights in `tables`, those of k = 0 times shift).
 template <int EK, int MT>
-__device__ __forceinline__ void add_products(f32x16 (&S)[MT], float& frame, float whole, f32x8 (&w)[4], const unsigned char* b)
+__device__ __forceinline__ void add_products(f32x4 (&S)[MT], float& frame, float whole, const typename Operand<EK>::vec (&cv)[2], const float* tables,
+                                             float shift, const unsigned char* b)
 {
     typedef typename Operand<EK>::vec V;
+    float in = 1.f;
+    const f32x4 tail[2] = {*reinterpret_cast<const f32x4*>(tables), *reinterpret_cast<const f32x4*>(tables + 256)};
+    auto weighted = [&](int k) {
+        f32x8 w = widened<V>(cv[k]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] *= tail[e / 4][e % 4];
+        if (k == 0) w *= shift;
+        if (EK == kElemF16) w *= in;
+        return w;
+    };
     if constexpr (EK == kElemF16) {
         float largest = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < 2; ++k) {
+            const f32x8 w = weighted(k);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[k][e]));
-        largest = larger_half(largest);
+            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[e]));
+        }
+        largest = column_largest(largest);
         const float next = largest > 0.f ? __builtin_amdgcn_ldexpf(1.f, half_exponent(largest)) : frame;
         whole *= frame / next;
-        const float in = 1.f / next;
+        in = 1.f / next;
         frame = next;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] *= in;
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) S[m] *= whole;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < 2; ++k) {
         V p[Operand<EK>::kTerm];
-        parts(w[k], p);
+        parts(weighted(k), p);
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            const V x = turned<32 * MT, V>(b, 32 * m, 16 * k);
+            const V x = turned<16 * MT, V>(b, 16 * m, 32 * k);
 #pragma unroll
             for (int q = Operand<EK>::kTerm; q-- > 0;) S[m] = multiply(x, p[q], S[m]);
         }
@@ -215,26 +296,28 @@ __device__ __forceinline__ void add_products(f32x16 (&S)[MT], float& frame, floa
 
 constexpr int kPairPitch = pitch_of(kAttentionChunk), kPairs = kAttentionChunk * kPairPitch;       // bytes of one part of the pair products
 
+constexpr int kTables = 64 * 16 * 4;                // ... of the lanes' weights
+
 template <int DAP, int NW, bool OUTPUT>
-constexpr int chunk_lds_bytes() { return kAttentionChunk * ((OUTPUT ? 2 : 1) * pitch_of(DAP) + pitch_of(32 * NW)) + (OUTPUT ? 2 * kPairs : 0); }
+constexpr int chunk_lds_bytes() { return kAttentionChunk * ((OUTPUT ? 2 : 1) * pitch_of(DAP) + pitch_of(16 * NW)) + (OUTPUT ? 2 * kPairs : 0) + kTables; }
 
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 
-// DAP: rows of the state (DA, padded); NW wavefronts of 32 columns each.  OUTPUT false: only a segment's own sum.
+// DAP: rows of the state (DA, padded); NW wavefronts of 16 columns each.  OUTPUT false: only a segment's own sum.
 //
 // A chunk of fewer tokens (a sequence's last) lies in the last rows of its tiles: the weights of tokens are counted from a chunk's end.
 template <int EK, int DAP, int NW, bool OUTPUT>
-__global__ __launch_bounds__(64 * NW, DAP <= 128 ? 2 : 1) void attention_chunk_kernel(AttentionSum s, AttentionBatch n, AttentionSegments g, bool turned_states)
+__global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_kernel(AttentionSum s, AttentionBatch n, AttentionSegments g, bool turned_states)
 {
     typedef typename ElemOf<EK>::type T;
     typedef typename Operand<EK>::vec V;
-    constexpr int CH = kAttentionChunk, WC = 32 * NW, MT = DAP / 32, THREADS = 64 * NW;
-    constexpr bool AHEAD = (OUTPUT ? 2 : 1) * Staged<EK, DAP, THREADS>::N + Staged<EK, WC, THREADS>::N <= 12;    // the next chunk in registers
+    constexpr int CH = kAttentionChunk, WC = 16 * NW, MT = DAP / 16, THREADS = 64 * NW;
+    constexpr bool AHEAD = (OUTPUT ? 2 : 1) * Staged<EK, DAP, THREADS>::N + Staged<EK, WC, THREADS>::N <= 6;    // the next chunk in registers
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *tb = smem, *tc = tb + CH * pitch_of(DAP), *ta = tc + CH * pitch_of(WC), *tp = ta + (OUTPUT ? CH * pitch_of(DAP) : 0);
 
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32, l32 = lane % 32;
-    const int head = blockIdx.y, col0 = blockIdx.z * WC, col = col0 + wave * 32 + l32;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l16 = lane % 16, own = lane / 16;
+    const int head = blockIdx.x % (unsigned)n.H, col0 = blockIdx.y * WC, col = col0 + wave * 16 + l16;
     const int width = s.DC - col0;                  // columns from here on
     const Place at = locate(n, g);
     if (at.none) return;
@@ -246,28 +329,34 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 2 : 1) void attention_chunk_k
 
     const int e0 = s.reverse ? 0 : 1;
     const float g2 = n.log_decay[head] * 1.44269504088896341f;
-    const float chunk_decay = uniform(power(g2, CH));
-    // weights of a chunk's tokens 16 k + 8 half + e: l^(CH - e0 - token) = shift[k] * tail[e]
-    float tail[8], shift[4];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) tail[e] = s.alpha_s * power(g2, 16 - e0 - 8 * half - e);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) shift[k] = uniform(power(g2, 16 * (3 - k)));
-    // pair products: tiles of 32 x 32 (rows j, columns i): (0,0) (1,0) (1,1) of four wavefronts, (0,0) and (1,1), (1,0) of two
-    const int ti = NW >= 4 ? (wave + 1) / 2 : wave, tj = NW >= 4 ? wave / 2 : 0;
-    float fade[16];
-    if constexpr (OUTPUT)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int gap = 32 * (ti - tj) + l32 - tile_row(r, half);
-            fade[r] = gap < 0 ? 0.f : s.alpha_y * s.alpha_s * power(g2, gap);
+    const float chunk_decay = uniform(power(g2, CH)), shift = uniform(power(g2, CH / 2));
+    // The lanes' weights, all wavefronts' the same, sixteen values a lane in fours:
+    // 0, 1: of a chunk's tokens 32 k + 8 own + e, l^(CH - e0 - token) without `shift` for k = 0
+    // 2, 3: of pair products (row j = 4 own + e, column i = l16 of a tile), on the diagonal and with i's tile the next after j's
+    float* tables = reinterpret_cast<float*>(tp + (OUTPUT ? 2 * kPairs : 0)) + 4 * lane;
+    for (int k = wave; k < (OUTPUT ? 4 : 2); k += NW)
+        for (int e = 0; e < 4; ++e) {
+            const int gap = l16 - 4 * own - e;
+            const float v = k < 2 ? power(g2, 32 - e0 - 8 * own - 4 * k - e) : gap < 0 && k == 2 ? 0.f : s.alpha_y * power(g2, k == 2 ? gap : 16 + gap);
+            tables[256 * k + e] = s.alpha_s * v;
         }
+    float further[3];
+    const float near = s.alpha_y * power(g2, l16 + e0);         // ... and of the state in y, of a whole chunk's first tokens
+    if constexpr (OUTPUT) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) further[k] = uniform(power(g2, 16 * (k + 1)));
+        // (tiles above the diagonal that are read with their neighbours and never written)
+        for (int i = threadIdx.x; i < 2 * 2 * 16 * 2; i += THREADS) {
+            const int part = i / 64, tile = i / 32 % 2, row = i / 2 % 16, side = i % 2;
+            *reinterpret_cast<u32x4*>(tp + part * kPairs + (32 * tile + row) * kPairPitch + 64 * tile + 32 + 16 * side) = (u32x4){0, 0, 0, 0};
+        }
+    }
     // places in the tiles
-    const unsigned char *along_b = tb + (32 * tj + l32) * pitch_of(DAP) + 16 * half, *along_a = ta + (32 * ti + l32) * pitch_of(DAP) + 16 * half;
-    const unsigned char *picked_a = ta + l32 * pitch_of(DAP) + 8 * half, *down_b = turned_base<DAP>(tb, lane), *down_c = turned_base<WC>(tc, lane) + 64 * wave;
-    unsigned char* pairs = tp + l32 * kPairPitch;
+    const unsigned char *along_b = tb + l16 * pitch_of(DAP) + 16 * own, *along_a = ta + l16 * pitch_of(DAP) + 16 * own;
+    const unsigned char *picked_a = ta + l16 * pitch_of(DAP) + 8 * own, *down_b = turned_base<DAP>(tb, lane), *down_c = turned_base<WC>(tc, lane) + 32 * wave;
+    unsigned char* pairs = tp + l16 * kPairPitch;
 
-    f32x16 S[MT];
+    f32x4 S[MT];
     if constexpr (OUTPUT)
         load_state(S, s, n, g, at, head, col, turned_states);
     else
@@ -283,85 +372,70 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 2 : 1) void attention_chunk_k
     Staged<EK, WC, THREADS> sc;
     // the first of a chunk's rows that is a token, and the token that row 0 would be
     auto from_of = [&](int64_t t) { return at.last - t < CH ? CH - (int)(at.last - t) : 0; };
+    // the lowest of a chunk's 64 rows in memory
+    auto tile_of = [&](const AttentionOperand& o, int64_t t) { return row_of(o, t - from_of(t) + (s.reverse ? CH - 1 : 0)); };
     auto fetch = [&](int64_t t) {
         const int from = from_of(t);
-        if constexpr (OUTPUT) sa.fetch(s.a, row_of(s.a, t - from), dir * s.a.token, from, s.DA);
-        sb.fetch(s.b, row_of(s.b, t - from), dir * s.b.token, from, s.DA);
-        sc.fetch(s.c, row_of(s.c, t - from) + col0, dir * s.c.token, from, width);
+        if constexpr (OUTPUT) sa.fetch(static_cast<const T*>(s.a.p) + tile_of(s.a, t), (unsigned)s.a.token, s.reverse, from, s.DA);
+        sb.fetch(static_cast<const T*>(s.b.p) + tile_of(s.b, t), (unsigned)s.b.token, s.reverse, from, s.DA);
+        sc.fetch(static_cast<const T*>(s.c.p) + tile_of(s.c, t) + col0, (unsigned)s.c.token, s.reverse, from, width);
     };
-    auto slowly = [&](int64_t t) {
+    auto put = [&](int64_t t) {
         const int from = from_of(t);
-        const int64_t to = row_of(s.y, t - from) + col;
-        float held[16 * MT];
-#pragma unroll
-        for (int i = 0; i < 16 * MT; ++i) held[i] = S[i / 16][i % 16] * frame;
-        void* y = s.y_f32 ? static_cast<void*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to)
-                          : static_cast<void*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to);
-        token_by_token<T, MT>(held, TokenByToken<T>{OUTPUT ? ta : nullptr, tb, tc + (wave * 32 + l32) * 2, pitch_of(DAP), pitch_of(WC), from, CH, s.DA,
-                                                    power(g2, 1), s.alpha_s, s.alpha_y, s.reverse, s.y_f32, col < s.DC, y, dir * s.y.token});
-#pragma unroll
-        for (int i = 0; i < 16 * MT; ++i) S[i / 16][i % 16] = held[i];
-        frame = 1.f;
+        __syncthreads();
+        if constexpr (OUTPUT) sa.put(ta, static_cast<const T*>(s.a.p) + tile_of(s.a, t), (unsigned)s.a.token, s.reverse, from, s.DA);
+        sb.put(tb, static_cast<const T*>(s.b.p) + tile_of(s.b, t), (unsigned)s.b.token, s.reverse, from, s.DA);
+        sc.put(tc, static_cast<const T*>(s.c.p) + tile_of(s.c, t) + col0, (unsigned)s.c.token, s.reverse, from, width);
+        __syncthreads();
     };
+    bool bad = false;
     if (AHEAD && at.first < at.last) fetch(at.first);
     for (int64_t t = at.first; t < at.last; t += CH) {
         const int from = from_of(t);
         if (!AHEAD) fetch(t);
-        __syncthreads();
-        if constexpr (OUTPUT) sa.put(ta);
-        sb.put(tb);
-        sc.put(tc);
-        __syncthreads();
+        put(t);
         if (AHEAD && t + CH < at.last) fetch(t + CH);
         // c: columns a lane, eight tokens each
-        V cv[4];
+        V cv[2];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) cv[k] = turned<WC, V>(down_c, 0, 16 * k);
+        for (int k = 0; k < 2; ++k) cv[k] = turned<WC, V>(down_c, 0, 32 * k);
         if constexpr (OUTPUT) {
-            auto pair_tile = [&](int di, int dj, int i, int j) {
-                f32x16 p = 0.f;
+            // pair products: the ten tiles on and below the diagonal, (0,0) (1,0) (1,1) (2,0) ..., a wavefront after another
+            for (int tile = wave; tile < 10; tile += NW) {
+                const int i = (tile >= 1) + (tile >= 3) + (tile >= 6), j = tile - i * (i + 1) / 2;
+                f32x4 p = 0.f;
 #pragma unroll
-                for (int k = 0; k < DAP / 16; ++k)
-                    p = multiply(*reinterpret_cast<const V*>(along_b + dj * pitch_of(DAP) + 32 * k),
-                                 *reinterpret_cast<const V*>(along_a + di * pitch_of(DAP) + 32 * k), p);
-#pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    f32x8 v;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = p[8 * q + e] * fade[8 * q + e];
-                    bf16x8 w[2];
-                    parts(v, w);
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const u32x4 u = __builtin_bit_cast(u32x4, w[k]);
-                        unsigned char* to = pairs + k * kPairs + 32 * i * kPairPitch + 64 * j + 32 * q + 8 * half;
-                        *reinterpret_cast<u32x2*>(to) = (u32x2){u[0], u[1]};
-                        *reinterpret_cast<u32x2*>(to + 16) = (u32x2){u[2], u[3]};
-                    }
-                }
-            };
-            if (NW < 4 || wave < 3) pair_tile(0, 0, ti, tj);
-            if (NW < 4 && wave == 0) pair_tile(32, 32, 1, 1);
-
-            f32x16 O[2] = {0.f, 0.f};
-            float reach[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int token = 32 * i + l32 - from;
-                reach[i] = s.alpha_y * power(g2, (token < 0 ? 0 : token) + e0);
+                for (int k = 0; k < DAP / 32; ++k)
+                    p = multiply(*reinterpret_cast<const V*>(along_b + 16 * j * pitch_of(DAP) + 64 * k),
+                                 *reinterpret_cast<const V*>(along_a + 16 * i * pitch_of(DAP) + 64 * k), p);
+                p *= *reinterpret_cast<const f32x4*>(tables + (i == j ? 512 : 768)) * (i - j < 2 ? 1.f : further[i - j - 2]);
+                unsigned char* to = pairs + 16 * i * kPairPitch + 32 * j + 8 * own;
+                const u32x2 h = {pack<bf16x8>(p[0], p[1]), pack<bf16x8>(p[2], p[3])};
+                const f32x2 h0 = widen<bf16x8>(h[0]), h1 = widen<bf16x8>(h[1]);
+                *reinterpret_cast<u32x2*>(to) = h;
+                *reinterpret_cast<u32x2*>(to + kPairs) = (u32x2){pack<bf16x8>(p[0] - h0[0], p[1] - h0[1]), pack<bf16x8>(p[2] - h1[0], p[3] - h1[1])};
             }
+
+            f32x4 O[4] = {0.f, 0.f, 0.f, 0.f};
+            float reach[4] = {near, near * further[0], near * further[1], near * further[2]};
+            if (from > 0)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int token = 16 * i + l16 - from;
+                    reach[i] = s.alpha_y * power(g2, (token < 0 ? 0 : token) + e0);
+                }
             state_times_a<EK, MT>(S, frame, picked_a, O, reach);
             __syncthreads();
             // pair products times c
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < 2; ++k) {
                 bf16x8 c2[2];
-                if constexpr (EK == kElemF16) parts(__builtin_convertvector(cv[k], f32x8), c2);
+                if constexpr (EK == kElemF16) parts(widened<V>(cv[k]), c2);
 #pragma unroll
-                for (int i = k / 2; i < 2; ++i) {
+                for (int i = 2 * k; i < 4; ++i) {
                     bf16x8 p[2];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 32 * i * kPairPitch + 32 * k + 16 * half);
+                    for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 16 * i * kPairPitch + 64 * k + 16 * own);
                     if constexpr (EK == kElemF16) {
                         O[i] = multiply(c2[1], p[0], O[i]);
                         O[i] = multiply(c2[0], p[1], O[i]);
@@ -372,44 +446,45 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 2 : 1) void attention_chunk_k
                     }
                 }
             }
-            if (__builtin_expect(any_nonfinite(O), 0)) {
-                slowly(t);
-                continue;
+            bad |= any_nonfinite(O);
+            const int64_t to = tile_of(s.y, t) + col0 + wave * 16;
+            const int now = renewed(lane), c = 4 * (now / 16), left = width - wave * 16 - c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * i + now % 16;
+                const unsigned place = (s.reverse ? CH - 1 - row : row) * (unsigned)s.y.token + c;
+                if (row < from) continue;
+                if (s.y_f32)
+                    store_four(reinterpret_cast<float*>(reinterpret_cast<char*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to) + place * 4u), O[i], left);
+                else
+                    store_four(reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to) + place * (unsigned)sizeof(T)), O[i], left);
             }
-            const int64_t to = row_of(s.y, t - from);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (32 * i + l32 >= from) store_outputs<T>(O[i], s, to, dir * s.y.token, 32 * i + l32, col0 + wave * 32);
         }
-        f32x8 w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            w[k] = __builtin_convertvector(cv[k], f32x8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[k][e] *= tail[e] * shift[k];
-        }
-        add_products<EK, MT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), w, down_b);
+        add_products<EK, MT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
     }
 #pragma unroll
     for (int m = 0; m < MT; ++m) S[m] *= frame;
+    if (!OUTPUT) bad = any_nonfinite(S);
+    if (bad) {
+        if constexpr (OUTPUT) {
+            __builtin_amdgcn_s_waitcnt(0);          // (what has been stored is stored before it is stored again)
+            load_state(S, s, n, g, at, head, col, turned_states);
+        } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) S[m] = 0.f;
+        }
+        const T *a = OUTPUT ? static_cast<const T*>(s.a.p) + row_of(s.a, at.first) : nullptr, *b = static_cast<const T*>(s.b.p) + row_of(s.b, at.first);
+        const T* c = static_cast<const T*>(s.c.p) + row_of(s.c, at.first) + col;
+        const int64_t to = row_of(s.y, at.first) + col;
+        void* y = s.y_f32 ? static_cast<void*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to)
+                          : static_cast<void*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to);
+        token_by_token<T, MT>(S, TokenByToken<T>{a, b, c, dir * s.a.token, dir * s.b.token, dir * s.c.token, dir * s.y.token, at.last - at.first, s.DA,
+                                                 power(g2, 1), s.alpha_s, s.alpha_y, s.reverse, s.y_f32, col < s.DC, y});
+    }
     if constexpr (OUTPUT) {
         float* p = at.ends ? entry_of(s.last, s, n, at.seq, head) : nullptr;
         if (p) store_state(S, p, s.last.row, s.last.col, s, col);
     } else {
-        // a sum with an infinity or a NaN in it: once more, token by token
-        if (__syncthreads_or(any_nonfinite(S))) {
-            frame = 1.f;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) S[m] = 0.f;
-            for (int64_t t = at.first; t < at.last; t += CH) {
-                fetch(t);
-                __syncthreads();
-                sb.put(tb);
-                sc.put(tc);
-                __syncthreads();
-                slowly(t);
-            }
-        }
         store_state(S, g.states + (at.slot * n.H + head) * s.DA * s.DC, s.DC, 1, s, col);
     }
 }
@@ -422,7 +497,7 @@ hipError_t launch_chunk(const AttentionSum& s, const AttentionBatch& n, const At
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_chunk_kernel<EK, dap(), nw(), OUTPUT>),
                                                            hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (attr != hipSuccess) return attr;
-        const dim3 grid((unsigned)g.count, (unsigned)n.H, (unsigned)((s.DC + 32 * nw() - 1) / (32 * nw())));
+        const dim3 grid((unsigned)(g.count * n.H), (unsigned)((s.DC + 16 * nw() - 1) / (16 * nw())));
         note_kernel("attention_chunk_kernel", EK, dap(), nw(), OUTPUT);
         hipLaunchKernelGGL((attention_chunk_kernel<EK, dap(), nw(), OUTPUT>), grid, dim3(64 * nw()), lds, st, s, n, g, turned);
         return hipGetLastError();
@@ -433,7 +508,7 @@ hipError_t launch_chunk(const AttentionSum& s, const AttentionBatch& n, const At
         if (s.DA <= 128) return with(std::integral_constant<int, 128>(), nw);
         return with(std::integral_constant<int, 256>(), nw);
     };
-    return s.DC <= 64 ? rows(std::integral_constant<int, 2>()) : rows(std::integral_constant<int, 4>());
+    return s.DC <= 64 ? rows(std::integral_constant<int, 4>()) : rows(std::integral_constant<int, 8>());
 }
 
 }  // namespace

@@ -3,6 +3,7 @@
 #include "../../include/swconv.h"
 
 #include <cmath>
+#include <initializer_list>
 
 #include "sw_layers.h"
 
@@ -83,6 +84,8 @@ int check_dims(const sw_linear_attention_dims& d)
         return SW_ERR_SHAPE;
     if (d.T > kMaxExtent / d.B || (int64_t)d.B + 2 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.dk > kMaxHead || d.dv > kMaxHead || d.heads > 65535) return SW_ERR_UNSUPPORTED;
+    // (a place for every 128 tokens and two a sequence, every head one: workgroups of a launch)
+    if ((d.T / 128 * d.B + 2 * ((int64_t)d.B + 2)) * d.heads > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.type != SW_F32 && d.type != SW_BF16 && d.type != SW_F16) return SW_ERR_UNSUPPORTED;
     return SW_OK;
 }
@@ -93,6 +96,14 @@ bool packed_too_long(const sw_linear_attention_dims& d, const int32_t* starts) {
 AttentionSegments segments_of(const sw_linear_attention_dims& d, bool packed)
 {
     return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed);
+}
+
+// Whether the chunk kernels' 32-bit distances within a chunk reach its rows; tensors that lie further apart go token by token.
+bool near_rows(std::initializer_list<const Tensor4*> tensors)
+{
+    for (const Tensor4* t : tensors)
+        if (t->op.token > ((int64_t)1 << 30) / kAttentionChunk) return false;
+    return true;
 }
 
 // Bytes of the segments' states (0: whole sequences).
@@ -216,6 +227,7 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     AttentionSegments g = segments_of(d, starts != nullptr);
     g.states = static_cast<float*>(workspace);
+    if (!near_rows({&tq, &tk, &tv, &to})) return launch_status(launch_attention_recurrent(s, n, d.type, st));
     hipError_t e = hipSuccess;
     if (need) {
         e = launch_attention_states(s, n, g, d.type, st);
@@ -290,16 +302,20 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     const int64_t bytes = state_bytes(d, starts != nullptr);
     ahead.states = part_v + fold_bytes(d, starts != nullptr, d.dv) / 4, back.states = ahead.states + bytes / 4;
     hipError_t e = hipSuccess;
-    if (bytes) {
+    const bool chunks = near_rows({&tdo, &tq, &tk, &tv, &tdq, &tdk, &tdv});
+    if (bytes && chunks) {
         const AttentionSum forward{tq.op, tk.op, tv.op, tdo.op, {const_cast<float*>(state), states, per_head, d.dv, 1}, none, slots, d.dk, d.dv, 1.0f, d.scale, false, false};
         e = launch_attention_states(forward, n, ahead, d.type, st);
         if (e == hipSuccess) e = launch_attention_scan(forward, n, ahead, st);
         if (e == hipSuccess) e = launch_attention_states(of_v, n, back, d.type, st);
         if (e == hipSuccess) e = launch_attention_scan(of_v, n, back, st);
     }
-    if (e == hipSuccess) e = launch_attention_chunks(of_q, n, ahead, true, d.type, st);
-    if (e == hipSuccess) e = launch_attention_chunks(of_k, n, back, true, d.type, st);
-    if (e == hipSuccess) e = launch_attention_chunks(of_v, n, back, false, d.type, st);
+    auto run = [&](const AttentionSum& sum, const AttentionSegments& g, bool turned_states) {
+        return chunks ? launch_attention_chunks(sum, n, g, turned_states, d.type, st) : launch_attention_recurrent(sum, n, d.type, st);
+    };
+    if (e == hipSuccess) e = run(of_q, ahead, true);
+    if (e == hipSuccess) e = run(of_k, back, true);
+    if (e == hipSuccess) e = run(of_v, back, false);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_k, tdk.op, n, d.kv_heads, d.dk, d.type, st);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_v, tdv.op, n, d.kv_heads, d.dv, d.type, st);
     return launch_status(e);
