@@ -33,10 +33,11 @@ struct Place {
 // Segment places of a packed batch: sequence j's first one is lo / length + j, which leaves each at least one and all they need.
 __device__ __forceinline__ int64_t packed_slot(const AttentionSegments& g, int64_t lo, int j) { return lo / g.length + j; }
 
-__device__ __forceinline__ Place locate(const AttentionBatch& n, const AttentionSegments& g)
+// place: of a segment, in the rows' order; backwards in time a sequence's segments are worked on from its end, the first place is the last one's.
+__device__ __forceinline__ Place locate(const AttentionBatch& n, const AttentionSegments& g, int64_t place, bool reverse)
 {
     Place p;
-    p.slot = blockIdx.x / (unsigned)n.H;
+    p.slot = place;
     int64_t segment;
     if (n.starts) {
         // the last j whose first place is not past this one: 64 of them at a time, a lane each
@@ -64,9 +65,14 @@ __device__ __forceinline__ Place locate(const AttentionBatch& n, const Attention
         p.len = n.T;
         p.rest = false;
     }
+    const int64_t segments = p.len <= g.length ? 1 : (p.len + g.length - 1) / g.length;
+    p.none = segment >= segments;
+    if (reverse && !p.none && !p.rest) {
+        p.slot += segments - 1 - 2 * segment;
+        segment = segments - 1 - segment;
+    }
     p.first = segment * g.length;
     p.last = p.first + g.length < p.len ? p.first + g.length : p.len;
-    p.none = segment > 0 && p.first >= p.len;
     p.alone = p.len <= g.length;
     p.ends = p.last >= p.len;
     return p;
@@ -83,7 +89,7 @@ __device__ __forceinline__ float* entry_of(const AttentionState& st, const Atten
 
 // An accumulator tile is 16 x 16: a lane has column lane % 16, rows 4 (lane / 16) ... + 3.
 
-// f(tile, element, offset) for the elements of a lane's column that lie within DA rows: offset, their row's place in memory.  (Rows are
+// f(tile, element, offset) for the elements of a column of a lane that lie within DA rows: offset, their row's place in memory.  (Rows are
 // counted from the lane's own first one: what is added for an element is the same in all lanes.)
 template <int MT, class F>
 __device__ __forceinline__ void each_row(int DA, int64_t row_stride, F&& f)
@@ -102,10 +108,9 @@ __device__ __forceinline__ void each_row(int DA, int64_t row_stride, F&& f)
     }
 }
 
-// The state before a segment into the accumulators of the column `col`.
-template <int MT>
-__device__ __forceinline__ void load_state(f32x4 (&S)[MT], const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, const Place& at,
-                                           int head, int col, bool turned)
+// The state before a segment into the accumulators of the columns `col` and 16 further each.
+template <int MT, int CT>
+__device__ __forceinline__ void load_state(f32x4 (&S)[MT][CT], const AttentionSum& s, const AttentionBatch& n, const Place& at, int head, int col)
 {
     const float* p;
     int64_t row_stride, col_stride;
@@ -113,22 +118,28 @@ __device__ __forceinline__ void load_state(f32x4 (&S)[MT], const AttentionSum& s
         p = entry_of(s.first, s, n, at.seq, head);
         row_stride = s.first.row, col_stride = s.first.col;
     } else {
-        p = g.states + (at.slot * n.H + head) * s.DA * s.DC;
-        row_stride = turned ? 1 : s.DC, col_stride = turned ? s.DA : 1;
+        p = s.states + (at.slot * n.H + head) * s.DA * s.DC;
+        row_stride = s.turned ? 1 : s.DC, col_stride = s.turned ? s.DA : 1;
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m) S[m] = 0.f;
-    if (!p || col >= s.DC) return;
-    p += col * col_stride;
-    each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { S[m][e] = p[offset]; });
+    for (int c = 0; c < CT; ++c) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) S[m][c] = 0.f;
+        if (!p || col + 16 * c >= s.DC) continue;
+        const float* own = p + (col + 16 * c) * col_stride;
+        each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { S[m][c][e] = own[offset]; });
+    }
 }
 
-template <int MT>
-__device__ __forceinline__ void store_state(const f32x4 (&S)[MT], float* p, int64_t row_stride, int64_t col_stride, const AttentionSum& s, int col)
+template <int MT, int CT>
+__device__ __forceinline__ void store_state(const f32x4 (&S)[MT][CT], float* p, int64_t row_stride, int64_t col_stride, const AttentionSum& s, int col)
 {
-    if (col >= s.DC) return;
-    p += col * col_stride;
-    each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { p[offset] = S[m][e]; });
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+        if (col + 16 * c >= s.DC) continue;
+        float* own = p + (col + 16 * c) * col_stride;
+        each_row<MT>(s.DA, row_stride, [&](int m, int e, int64_t offset) { own[offset] = S[m][c][e]; });
+    }
 }
 
 // Zeros in `width` columns from col0 of the rows of a place in no sequence.
@@ -164,14 +175,16 @@ __device__ __forceinline__ void store_four(T* p, f32x4 v, int width)
 }
 
 // Whether a wavefront's accumulators hold an infinity or a NaN anywhere.
-template <int N>
-__device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[N])
+template <int N, int CT>
+__device__ __forceinline__ bool any_nonfinite(const f32x4 (&v)[N][CT])
 {
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum = fmaf(v[i][e], 0.f, sum);
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fmaf(v[i][c][e], 0.f, sum);
     return __any(sum != 0.f);
 }
 
@@ -187,13 +200,13 @@ struct TokenByToken {
     bool reverse, y_f32, column;        // column: the lane's is one of c's and y's
     void* y;                            // at the lane's column
 };
-template <class T, int MT>
-__device__ __forceinline__ void token_by_token(f32x4 (&S)[MT], const TokenByToken<T>& p)
+template <class T, int MT, int CT>
+__device__ __forceinline__ void token_by_token(f32x4 (&S)[MT][CT], int tile, const TokenByToken<T>& p)
 {
     const int own = 4 * (threadIdx.x % 64 / 16);
     float held[4 * MT];
 #pragma unroll
-    for (int i = 0; i < 4 * MT; ++i) held[i] = S[i / 4][i % 4];
+    for (int i = 0; i < 4 * MT; ++i) held[i] = S[i / 4][tile][i % 4];
 #pragma unroll 1
     for (int64_t t = 0; t < p.tokens; ++t) {
         const float c = p.column ? p.alpha_s * (float)p.c[t * p.step_c] : 0.f;
@@ -216,7 +229,7 @@ __device__ __forceinline__ void token_by_token(f32x4 (&S)[MT], const TokenByToke
             static_cast<T*>(p.y)[t * p.step_y] = (T)y;
     }
 #pragma unroll
-    for (int i = 0; i < 4 * MT; ++i) S[i / 4][i % 4] = held[i];
+    for (int i = 0; i < 4 * MT; ++i) S[i / 4][tile][i % 4] = held[i];
 }
 
 }  // namespace attention

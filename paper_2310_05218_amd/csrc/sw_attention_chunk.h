@@ -2,19 +2,17 @@
 //
 // A chunk of n tokens (rows i, j of a, b, c; state S before it; l the head's decay; e0 = 1 forwards in time, 0 backwards):
 //     y_i = alpha_y [ alpha_s sum_{j<=i} l^(i-j) (a_i . b_j) c_j  +  l^(i+e0) S^T a_i ],   S <- l^n S + alpha_s sum_j l^(n-e0-j) b_j c_j^T
-// A wavefront has 16 columns of c and y and all rows of their state, in its accumulators: the state never leaves registers while a
+// A wavefront has 16 or 32 columns of c and y and all rows of their state, in its accumulators: the state never leaves registers while a
 // segment lasts.  Operands are arranged so that results become operands where they are: an accumulator's column is a lane's, its rows
 // 4 (lane / 16) ... + 3 of sixteen; a product's K order is free as long as both operands have the same, so two tiles of S as they lie are
 // the operand of S^T a, with a's values picked in that order.  Outputs are computed transposed (rows: columns of y), so that a lane holds
 // four neighbouring columns of one token.  Pair products are shared: each 16 x 16 tile is computed by one wavefront and handed round in LDS.
 //
-// Why 16 columns: with 32, and half as many wavefronts, the state and what it meets take 250 registers, operands come from LDS one wait
-// after another, and two wavefronts a SIMD hide little of it (4 x 4096 tokens, 16 heads of 128: 105 us an output pass).
-//
-// Operands derived in fp32 enter a product as sums of 16-bit values, and which sums is a choice of precision: pair products two bf16
-// values (17 bits; half, whose range they may leave, meets c as two bf16 values too), the state two bf16 values or one half scaled by a
-// power of two (both finer than y's own rounding), the state's new terms three bf16 or two scaled half values (22 bits and more: the
-// state is an fp32 result).
+// Operands derived in fp32 enter a product as sums of 16-bit values, and which sums is a choice of precision.  Pair products: two bf16
+// values (17 bits; half, whose range they may leave, meets c as two bf16 values too).  The state: one value of the format, in half scaled
+// by a power of two; its rounding is y's own, on the part of y that comes from before the chunk (y's error against 64 bits at most 1.4 times
+// what its last rounding gives; with two values 10 % more time).  The state's new terms: three bf16 or two scaled half values, 22 bits and
+// more, as the state is an fp32 result.
 #pragma once
 
 #include "sw_attention.h"
@@ -92,7 +90,7 @@ struct Operand;
 template <>
 struct Operand<kElemBF16> {
     typedef bf16x8 vec;
-    static constexpr int kState = 2, kTerm = 3;
+    static constexpr int kState = 1, kTerm = 3;
 };
 template <>
 struct Operand<kElemF16> {
@@ -209,85 +207,109 @@ __device__ __forceinline__ int half_exponent(float largest)
 }
 
 // O = S^T a: rows, columns of y; columns, the chunk's tokens.  `a`: row lane % 16 of the tile, at the lane's place.
-template <int EK, int MT>
-__device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT], float frame, const unsigned char* a, f32x4 (&O)[4], const float (&reach)[4])
+template <int EK, int MT, int CT>
+__device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const float (&frame)[CT], const unsigned char* a, f32x4 (&O)[4][CT], const float (&reach)[4])
 {
     typedef typename Operand<EK>::vec V;
-    float in = 1.f, out = 1.f;
+    float in[CT], out = 1.f;
     if constexpr (EK == kElemF16) {
         // one scale for the wavefront's columns: they are the rows of what is computed
         float largest = 0.f;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int c = 0; c < CT; ++c) {
+            float of = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) largest = fmaxf(largest, fabsf(S[m][e]));
-        largest *= frame;
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) of = fmaxf(of, fabsf(S[m][c][e]));
+            largest = fmaxf(largest, of * frame[c]);
+        }
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d, 64));
         const int e = half_exponent(column_largest(largest));
-        in = frame * __builtin_amdgcn_ldexpf(1.f, -e);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) in[c] = frame[c] * __builtin_amdgcn_ldexpf(1.f, -e);
         out = __builtin_amdgcn_ldexpf(1.f, e);
     }
 #pragma unroll
     for (int m = 0; m < MT / 2; ++m) {
-        f32x8 v;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][e % 4] * in : S[2 * m + e / 4][e % 4];
-        V p[Operand<EK>::kState];
-        parts(v, p);
+        V x[4], p[CT][Operand<EK>::kState];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const unsigned char* at = a + 16 * i * pitch_of(16 * MT) + 64 * m;
-            const V x = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 32));
-#pragma unroll
-            for (int k = Operand<EK>::kState; k-- > 0;) O[i] = multiply(p[k], x, O[i]);
+            x[i] = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 32));
         }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            f32x8 v;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][c][e % 4] * in[c] : S[2 * m + e / 4][c][e % 4];
+            parts(v, p[c]);
+        }
+#pragma unroll
+        for (int k = Operand<EK>::kState; k-- > 0;)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) O[i][c] = multiply(p[c][k], x[i], O[i][c]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) O[i] *= reach[i] * out;
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) O[i][c] *= reach[i] * out;
 }
 
 // S <- whole S + sum over the chunk's tokens of b times weighted c (tokens 32 k + 8 (lane / 16) + e: weights in `tables`, those of k = 0 times shift).
-template <int EK, int MT>
-__device__ __forceinline__ void add_products(f32x4 (&S)[MT], float& frame, float whole, const typename Operand<EK>::vec (&cv)[2], const float* tables,
-                                             float shift, const unsigned char* b)
+template <int EK, int MT, int CT>
+__device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[CT], float whole, const typename Operand<EK>::vec (&cv)[2][CT],
+                                             const float* tables, float shift, const unsigned char* b)
 {
     typedef typename Operand<EK>::vec V;
-    float in = 1.f;
     const f32x4 tail[2] = {*reinterpret_cast<const f32x4*>(tables), *reinterpret_cast<const f32x4*>(tables + 256)};
-    auto weighted = [&](int k) {
-        f32x8 w = widened<V>(cv[k]);
+    auto weighted = [&](int k, int c) {
+        f32x8 w = widened<V>(cv[k][c]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] *= tail[e / 4][e % 4];
         if (k == 0) w *= shift;
-        if (EK == kElemF16) w *= in;
         return w;
     };
-    if constexpr (EK == kElemF16) {
-        float largest = 0.f;
+    float in[CT];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const f32x8 w = weighted(k);
+    for (int c = 0; c < CT; ++c) {
+        float fades = whole;
+        if constexpr (EK == kElemF16) {
+            float largest = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[e]));
+            for (int k = 0; k < 2; ++k) {
+                const f32x8 w = weighted(k, c);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[e]));
+            }
+            largest = column_largest(largest);
+            const float next = largest > 0.f ? __builtin_amdgcn_ldexpf(1.f, half_exponent(largest)) : frame[c];
+            fades *= frame[c] / next;
+            in[c] = 1.f / next;
+            frame[c] = next;
         }
-        largest = column_largest(largest);
-        const float next = largest > 0.f ? __builtin_amdgcn_ldexpf(1.f, half_exponent(largest)) : frame;
-        whole *= frame / next;
-        in = 1.f / next;
-        frame = next;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) S[m][c] *= fades;
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m) S[m] *= whole;
-#pragma unroll
     for (int k = 0; k < 2; ++k) {
-        V p[Operand<EK>::kTerm];
-        parts(weighted(k), p);
+        V p[CT][Operand<EK>::kTerm];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+            f32x8 w = weighted(k, c);
+            if (EK == kElemF16) w *= in[c];
+            parts(w, p[c]);
+        }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const V x = turned<16 * MT, V>(b, 16 * m, 32 * k);
 #pragma unroll
-            for (int q = Operand<EK>::kTerm; q-- > 0;) S[m] = multiply(x, p[q], S[m]);
+            for (int q = Operand<EK>::kTerm; q-- > 0;)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, p[c][q], S[m][c]);
         }
     }
 }
@@ -298,28 +320,31 @@ constexpr int kPairPitch = pitch_of(kAttentionChunk), kPairs = kAttentionChunk *
 
 constexpr int kTables = 64 * 16 * 4;                // ... of the lanes' weights
 
-template <int DAP, int NW, bool OUTPUT>
-constexpr int chunk_lds_bytes() { return kAttentionChunk * ((OUTPUT ? 2 : 1) * pitch_of(DAP) + pitch_of(16 * NW)) + (OUTPUT ? 2 * kPairs : 0) + kTables; }
+template <int DAP, int WC, bool OUTPUT>
+constexpr int chunk_lds_bytes() { return kAttentionChunk * ((OUTPUT ? 2 : 1) * pitch_of(DAP) + pitch_of(WC)) + (OUTPUT ? 2 * kPairs : 0) + kTables; }
 
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 
-// DAP: rows of the state (DA, padded); NW wavefronts of 16 columns each.  OUTPUT false: only a segment's own sum.
+// DAP: rows of the state (DA, padded); four wavefronts of CT tiles of 16 columns each.  OUTPUT false: only a segment's own sum.
 //
 // A chunk of fewer tokens (a sequence's last) lies in the last rows of its tiles: the weights of tokens are counted from a chunk's end.
-template <int EK, int DAP, int NW, bool OUTPUT>
-__global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_kernel(AttentionSum s, AttentionBatch n, AttentionSegments g, bool turned_states)
+template <int EK, int DAP, int CT, bool OUTPUT>
+__global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kernel(AttentionSums sums, AttentionBatch n, AttentionSegments g)
 {
     typedef typename ElemOf<EK>::type T;
     typedef typename Operand<EK>::vec V;
-    constexpr int CH = kAttentionChunk, WC = 16 * NW, MT = DAP / 16, THREADS = 64 * NW;
-    constexpr bool AHEAD = (OUTPUT ? 2 : 1) * Staged<EK, DAP, THREADS>::N + Staged<EK, WC, THREADS>::N <= 6;    // the next chunk in registers
+    constexpr int CH = kAttentionChunk, NW = 4, WC = 16 * CT * NW, MT = DAP / 16, THREADS = 64 * NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *tb = smem, *tc = tb + CH * pitch_of(DAP), *ta = tc + CH * pitch_of(WC), *tp = ta + (OUTPUT ? CH * pitch_of(DAP) : 0);
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l16 = lane % 16, own = lane / 16;
-    const int head = blockIdx.x % (unsigned)n.H, col0 = blockIdx.y * WC, col = col0 + wave * 16 + l16;
+    // Workgroups side by side: the sums of one segment and head, then its heads, whose rows lie side by side in memory.  The outputs go
+    // through the segments from the last one, which the caches saw last.
+    const unsigned block = OUTPUT ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const AttentionSum& s = sums.of[block % (unsigned)sums.count];
+    const int head = block / (unsigned)sums.count % (unsigned)n.H, col0 = blockIdx.y * WC, col = col0 + wave * 16 * CT + l16;
     const int width = s.DC - col0;                  // columns from here on
-    const Place at = locate(n, g);
+    const Place at = locate(n, g, block / (unsigned)sums.count / (unsigned)n.H, s.reverse);
     if (at.none) return;
     if (at.rest) {
         if (OUTPUT) zero_rows<T>(s, at, head, col0, width < WC ? width : WC);
@@ -353,16 +378,21 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_k
     }
     // places in the tiles
     const unsigned char *along_b = tb + l16 * pitch_of(DAP) + 16 * own, *along_a = ta + l16 * pitch_of(DAP) + 16 * own;
-    const unsigned char *picked_a = ta + l16 * pitch_of(DAP) + 8 * own, *down_b = turned_base<DAP>(tb, lane), *down_c = turned_base<WC>(tc, lane) + 32 * wave;
+    const unsigned char *picked_a = ta + l16 * pitch_of(DAP) + 8 * own, *down_b = turned_base<DAP>(tb, lane), *down_c = turned_base<WC>(tc, lane) + 32 * CT * wave;
     unsigned char* pairs = tp + l16 * kPairPitch;
 
-    f32x4 S[MT];
-    if constexpr (OUTPUT)
-        load_state(S, s, n, g, at, head, col, turned_states);
-    else
+    f32x4 S[MT][CT];
+    float frame[CT];                                // half: S is in units of `frame`, a power of two a column
+    auto begin = [&] {
+        if constexpr (OUTPUT)
+            load_state(S, s, n, at, head, col);
+        else
 #pragma unroll
-        for (int m = 0; m < MT; ++m) S[m] = 0.f;
-    float frame = 1.f;                              // half: S is in units of `frame`, a power of two a column
+            for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) frame[c] = 1.f;
+    };
+    begin();
 
     const int64_t dir = s.reverse ? -1 : 1;
     auto row_of = [&](const AttentionOperand& o, int64_t t) {
@@ -389,16 +419,16 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_k
         __syncthreads();
     };
     bool bad = false;
-    if (AHEAD && at.first < at.last) fetch(at.first);
     for (int64_t t = at.first; t < at.last; t += CH) {
         const int from = from_of(t);
-        if (!AHEAD) fetch(t);
+        fetch(t);
         put(t);
-        if (AHEAD && t + CH < at.last) fetch(t + CH);
         // c: columns a lane, eight tokens each
-        V cv[2];
+        V cv[2][CT];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) cv[k] = turned<WC, V>(down_c, 0, 32 * k);
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) cv[k][c] = turned<WC, V>(down_c, 16 * c, 32 * k);
         if constexpr (OUTPUT) {
             // pair products: the ten tiles on and below the diagonal, (0,0) (1,0) (1,1) (2,0) ..., a wavefront after another
             for (int tile = wave; tile < 10; tile += NW) {
@@ -416,7 +446,9 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_k
                 *reinterpret_cast<u32x2*>(to + kPairs) = (u32x2){pack<bf16x8>(p[0] - h0[0], p[1] - h0[1]), pack<bf16x8>(p[2] - h1[0], p[3] - h1[1])};
             }
 
-            f32x4 O[4] = {0.f, 0.f, 0.f, 0.f};
+            f32x4 O[4][CT];
+#pragma unroll
+            for (int i = 0; i < 4 * CT; ++i) O[i / CT][i % CT] = 0.f;
             float reach[4] = {near, near * further[0], near * further[1], near * further[2]};
             if (from > 0)
 #pragma unroll
@@ -424,91 +456,114 @@ __global__ __launch_bounds__(64 * NW, DAP <= 128 ? 4 : 2) void attention_chunk_k
                     const int token = 16 * i + l16 - from;
                     reach[i] = s.alpha_y * power(g2, (token < 0 ? 0 : token) + e0);
                 }
-            state_times_a<EK, MT>(S, frame, picked_a, O, reach);
+            state_times_a<EK, MT, CT>(S, frame, picked_a, O, reach);
             __syncthreads();
             // pair products times c
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                bf16x8 c2[2];
-                if constexpr (EK == kElemF16) parts(widened<V>(cv[k]), c2);
+                bf16x8 c2[CT][2];
+                if constexpr (EK == kElemF16)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) parts(widened<V>(cv[k][c]), c2[c]);
 #pragma unroll
                 for (int i = 2 * k; i < 4; ++i) {
                     bf16x8 p[2];
 #pragma unroll
                     for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 16 * i * kPairPitch + 64 * k + 16 * own);
-                    if constexpr (EK == kElemF16) {
-                        O[i] = multiply(c2[1], p[0], O[i]);
-                        O[i] = multiply(c2[0], p[1], O[i]);
-                        O[i] = multiply(c2[0], p[0], O[i]);
-                    } else {
-                        O[i] = multiply(cv[k], p[1], O[i]);
-                        O[i] = multiply(cv[k], p[0], O[i]);
-                    }
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        if constexpr (EK == kElemF16) {
+                            O[i][c] = multiply(c2[c][1], p[0], O[i][c]);
+                            O[i][c] = multiply(c2[c][0], p[1], O[i][c]);
+                            O[i][c] = multiply(c2[c][0], p[0], O[i][c]);
+                        } else {
+                            O[i][c] = multiply(cv[k][c], p[1], O[i][c]);
+                            O[i][c] = multiply(cv[k][c], p[0], O[i][c]);
+                        }
                 }
             }
             bad |= any_nonfinite(O);
-            const int64_t to = tile_of(s.y, t) + col0 + wave * 16;
-            const int now = renewed(lane), c = 4 * (now / 16), left = width - wave * 16 - c;
+            const int64_t to = tile_of(s.y, t) + col0 + wave * 16 * CT;
+            const int now = renewed(lane);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = 16 * i + now % 16;
-                const unsigned place = (s.reverse ? CH - 1 - row : row) * (unsigned)s.y.token + c;
                 if (row < from) continue;
-                if (s.y_f32)
-                    store_four(reinterpret_cast<float*>(reinterpret_cast<char*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to) + place * 4u), O[i], left);
-                else
-                    store_four(reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to) + place * (unsigned)sizeof(T)), O[i], left);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    const int first = 16 * c + 4 * (now / 16), left = width - wave * 16 * CT - first;
+                    const unsigned place = (s.reverse ? CH - 1 - row : row) * (unsigned)s.y.token + first;
+                    if (s.y_f32)
+                        store_four(reinterpret_cast<float*>(reinterpret_cast<char*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to) + place * 4u), O[i][c], left);
+                    else
+                        store_four(reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to) + place * (unsigned)sizeof(T)), O[i][c], left);
+                }
             }
         }
-        add_products<EK, MT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
+        add_products<EK, MT, CT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m) S[m] *= frame;
+    for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] *= frame[i % CT];
     if (!OUTPUT) bad = any_nonfinite(S);
     if (bad) {
-        if constexpr (OUTPUT) {
-            __builtin_amdgcn_s_waitcnt(0);          // (what has been stored is stored before it is stored again)
-            load_state(S, s, n, g, at, head, col, turned_states);
-        } else {
-#pragma unroll
-            for (int m = 0; m < MT; ++m) S[m] = 0.f;
-        }
+        __builtin_amdgcn_s_waitcnt(0);              // (what has been stored is stored before it is stored again)
+        begin();
         const T *a = OUTPUT ? static_cast<const T*>(s.a.p) + row_of(s.a, at.first) : nullptr, *b = static_cast<const T*>(s.b.p) + row_of(s.b, at.first);
-        const T* c = static_cast<const T*>(s.c.p) + row_of(s.c, at.first) + col;
-        const int64_t to = row_of(s.y, at.first) + col;
-        void* y = s.y_f32 ? static_cast<void*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to)
-                          : static_cast<void*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to);
-        token_by_token<T, MT>(S, TokenByToken<T>{a, b, c, dir * s.a.token, dir * s.b.token, dir * s.c.token, dir * s.y.token, at.last - at.first, s.DA,
-                                                 power(g2, 1), s.alpha_s, s.alpha_y, s.reverse, s.y_f32, col < s.DC, y});
+#pragma unroll
+        for (int i = 0; i < CT; ++i) {
+            const T* c = static_cast<const T*>(s.c.p) + row_of(s.c, at.first) + col + 16 * i;
+            const int64_t to = row_of(s.y, at.first) + col + 16 * i;
+            void* y = s.y_f32 ? static_cast<void*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to)
+                              : static_cast<void*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to);
+            token_by_token(S, i, TokenByToken<T>{a, b, c, dir * s.a.token, dir * s.b.token, dir * s.c.token, dir * s.y.token, at.last - at.first, s.DA,
+                                                 power(g2, 1), s.alpha_s, s.alpha_y, s.reverse, s.y_f32, col + 16 * i < s.DC, y});
+        }
     }
     if constexpr (OUTPUT) {
         float* p = at.ends ? entry_of(s.last, s, n, at.seq, head) : nullptr;
         if (p) store_state(S, p, s.last.row, s.last.col, s, col);
     } else {
-        store_state(S, g.states + (at.slot * n.H + head) * s.DA * s.DC, s.DC, 1, s, col);
+        store_state(S, s.states + (at.slot * n.H + head) * s.DA * s.DC, s.DC, 1, s, col);
     }
 }
 
+// The sums of one size in one launch.
 template <int EK, bool OUTPUT>
-hipError_t launch_chunk(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st)
+hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
-    auto with = [&](auto dap, auto nw) {
-        constexpr int lds = chunk_lds_bytes<dap(), nw(), OUTPUT>();
-        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_chunk_kernel<EK, dap(), nw(), OUTPUT>),
-                                                           hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-        if (attr != hipSuccess) return attr;
-        const dim3 grid((unsigned)(g.count * n.H), (unsigned)((s.DC + 16 * nw() - 1) / (16 * nw())));
-        note_kernel("attention_chunk_kernel", EK, dap(), nw(), OUTPUT);
-        hipLaunchKernelGGL((attention_chunk_kernel<EK, dap(), nw(), OUTPUT>), grid, dim3(64 * nw()), lds, st, s, n, g, turned);
-        return hipGetLastError();
-    };
-    auto rows = [&](auto nw) {
-        if (s.DA <= 32) return with(std::integral_constant<int, 32>(), nw);
-        if (s.DA <= 64) return with(std::integral_constant<int, 64>(), nw);
-        if (s.DA <= 128) return with(std::integral_constant<int, 128>(), nw);
-        return with(std::integral_constant<int, 256>(), nw);
-    };
-    return s.DC <= 64 ? rows(std::integral_constant<int, 4>()) : rows(std::integral_constant<int, 8>());
+    auto padded = [](int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; };
+    auto columns = [](int d) { return d <= 64 ? 0 : (d + 127) / 128; };
+    bool done[3] = {false, false, false};
+    for (int i = 0; i < all.count; ++i) {
+        if (done[i]) continue;
+        AttentionSums s;
+        s.count = 0;
+        const int da = padded(all.of[i].DA), dc = all.of[i].DC;
+        for (int j = i; j < all.count; ++j)
+            if (!done[j] && padded(all.of[j].DA) == da && columns(all.of[j].DC) == columns(dc))
+                s.of[s.count++] = all.of[j], done[j] = true;
+        auto with = [&](auto dap, auto ct) {
+            constexpr int lds = chunk_lds_bytes<dap(), 64 * ct(), OUTPUT>();
+            static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_chunk_kernel<EK, dap(), ct(), OUTPUT>),
+                                                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+            if (attr != hipSuccess) return attr;
+            const dim3 grid((unsigned)(g.count * n.H * s.count), (unsigned)((dc + 64 * ct() - 1) / (64 * ct())));
+            note_kernel("attention_chunk_kernel", EK, dap(), ct(), OUTPUT);
+            hipLaunchKernelGGL((attention_chunk_kernel<EK, dap(), ct(), OUTPUT>), grid, dim3(256), lds, st, s, n, g);
+            return hipGetLastError();
+        };
+        auto rows = [&](auto ct) {
+            switch (da) {
+            case 32: return with(std::integral_constant<int, 32>(), ct);
+            case 64: return with(std::integral_constant<int, 64>(), ct);
+            case 128: return with(std::integral_constant<int, 128>(), ct);
+            default: return with(std::integral_constant<int, 256>(), ct);
+            }
+        };
+        const hipError_t e = dc <= 64 ? rows(std::integral_constant<int, 1>()) : rows(std::integral_constant<int, 2>());
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

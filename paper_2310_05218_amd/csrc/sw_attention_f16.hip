@@ -3,14 +3,14 @@
 
 namespace swconv {
 
-hipError_t launch_attention_states_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
+hipError_t launch_attention_states_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
-    return launch_chunk<kElemF16, false>(s, n, g, false, st);
+    return launch_chunk<kElemF16, false>(s, n, g, st);
 }
 
-hipError_t launch_attention_chunks_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st)
+hipError_t launch_attention_chunks_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
-    return launch_chunk<kElemF16, true>(s, n, g, turned, st);
+    return launch_chunk<kElemF16, true>(s, n, g, st);
 }
 
 }  // namespace swconv

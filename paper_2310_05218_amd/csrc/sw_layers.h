@@ -149,6 +149,12 @@ struct AttentionSum {
     int DA, DC;
     float alpha_s, alpha_y;
     bool reverse, y_f32;
+    float* states = nullptr;            // [segments, H, DA, DC]: the state before each segment
+    bool turned = false;                // ... of the sum with a's and c's widths exchanged: [segments, H, DC, DA]
+};
+struct AttentionSums {                  // that are worked on side by side
+    AttentionSum of[3];
+    int count;
 };
 struct AttentionBatch {
     const float* log_decay;
@@ -159,17 +165,16 @@ struct AttentionBatch {
 // A long sequence is cut into segments of `length` tokens (a multiple of the chunk) that are worked on side by side: their own sums first
 // (attention_states), the state before each from these (attention_scan), then the outputs (attention_chunks).  length 0: whole sequences.
 struct AttentionSegments {
-    float* states;                      // [segments, H, DA, DC]
     int64_t length, count;              // count: places for segments in all
 };
 constexpr int kAttentionChunk = 64;
-AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed);     // without `states`
+AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed);
 // a segment's own sum for all but the last of a sequence, into `states`
-hipError_t launch_attention_states(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
+hipError_t launch_attention_states(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
 // ... from which the state before each segment of a sequence that has several
-hipError_t launch_attention_scan(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-// the outputs and last states (turned: `states` are those of the sum with DA and DC exchanged)
-hipError_t launch_attention_chunks(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, int ek, hipStream_t st);
+hipError_t launch_attention_scan(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+// the outputs and last states
+hipError_t launch_attention_chunks(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
 hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatch& n, int ek, hipStream_t st);
 // y[row, u] = sum over the heads of group u of part[row, head], rows of D fp32 each, rounded to the format
 hipError_t launch_attention_fold(const float* part, const AttentionOperand& y, const AttentionBatch& n, int kv_heads, int D, int ek, hipStream_t st);

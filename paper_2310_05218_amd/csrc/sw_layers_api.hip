@@ -84,8 +84,8 @@ int check_dims(const sw_linear_attention_dims& d)
         return SW_ERR_SHAPE;
     if (d.T > kMaxExtent / d.B || (int64_t)d.B + 2 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.dk > kMaxHead || d.dv > kMaxHead || d.heads > 65535) return SW_ERR_UNSUPPORTED;
-    // (a place for every 128 tokens and two a sequence, every head one: workgroups of a launch)
-    if ((d.T / 128 * d.B + 2 * ((int64_t)d.B + 2)) * d.heads > 0x7fffffff) return SW_ERR_SHAPE;
+    // (a place for every 128 tokens and two a sequence, every head one, three sums: workgroups of a launch)
+    if ((d.T / 128 * d.B + 2 * ((int64_t)d.B + 2)) * d.heads * 3 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.type != SW_F32 && d.type != SW_BF16 && d.type != SW_F16) return SW_ERR_UNSUPPORTED;
     return SW_OK;
 }
@@ -222,18 +222,17 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
             if (meet(out[p], out[r])) return SW_ERR_ALIAS;
     }
     const AttentionState first{const_cast<float*>(state), states, per_head, d.dv, 1}, last{final_state, states, per_head, d.dv, 1};
-    const AttentionSum s{tq.op, tk.op, tv.op, to.op, first, last, slots, d.dk, d.dv, 1.0f, d.scale, false, false};
+    AttentionSums s;
+    s.count = 1;
+    s.of[0] = AttentionSum{tq.op, tk.op, tv.op, to.op, first, last, slots, d.dk, d.dv, 1.0f, d.scale, false, false, static_cast<float*>(workspace)};
     const AttentionBatch n{log_decay, starts, d.T, d.B, d.heads, d.n_states};
+    const AttentionSegments g = segments_of(d, starts != nullptr);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    AttentionSegments g = segments_of(d, starts != nullptr);
-    g.states = static_cast<float*>(workspace);
-    if (!near_rows({&tq, &tk, &tv, &to})) return launch_status(launch_attention_recurrent(s, n, d.type, st));
+    if (!near_rows({&tq, &tk, &tv, &to})) return launch_status(launch_attention_recurrent(s.of[0], n, d.type, st));
     hipError_t e = hipSuccess;
-    if (need) {
-        e = launch_attention_states(s, n, g, d.type, st);
-        if (e == hipSuccess) e = launch_attention_scan(s, n, g, st);
-    }
-    if (e == hipSuccess) e = launch_attention_chunks(s, n, g, false, d.type, st);
+    if (need) e = launch_attention_states(s, n, g, d.type, st);
+    if (need && e == hipSuccess) e = launch_attention_scan(s, n, g, st);
+    if (e == hipSuccess) e = launch_attention_chunks(s, n, g, d.type, st);
     return launch_status(e);
 }
 
@@ -294,28 +293,29 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     // where heads share rows of k and v their gradients are added from fp32 rows of each head
     float *part_k = static_cast<float*>(workspace), *part_v = part_k + fold_bytes(d, starts != nullptr, d.dk) / 4;
     auto part = [&](float* p, int width) { return AttentionOperand{p, d.T * d.heads * width, (int64_t)d.heads * width, width, 1}; };
-    const AttentionSum of_q{tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false};
-    const AttentionSum of_k{tv.op, tdo.op, tq.op, share > 1 ? part(part_k, d.dk) : tdk.op, turned_final, none, nullptr, d.dv, d.dk, d.scale, 1.0f, true, share > 1};
-    const AttentionSum of_v{tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale, 1.0f, true, share > 1};
     // the states before each segment, forwards (those of the forward call) and backwards in time
-    AttentionSegments ahead = segments_of(d, starts != nullptr), back = ahead;
     const int64_t bytes = state_bytes(d, starts != nullptr);
-    ahead.states = part_v + fold_bytes(d, starts != nullptr, d.dv) / 4, back.states = ahead.states + bytes / 4;
+    float *ahead = part_v + fold_bytes(d, starts != nullptr, d.dv) / 4, *back = ahead + bytes / 4;
+    const AttentionSum of_q{tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false, ahead, true};
+    const AttentionSum of_k{tv.op, tdo.op, tq.op, share > 1 ? part(part_k, d.dk) : tdk.op, turned_final, none, nullptr, d.dv, d.dk, d.scale, 1.0f, true,
+                            share > 1, back, true};
+    const AttentionSum of_v{tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale, 1.0f, true,
+                            share > 1, back, false};
+    const AttentionSums gradients{{of_q, of_k, of_v}, 3};
+    const AttentionSegments g = segments_of(d, starts != nullptr);
     hipError_t e = hipSuccess;
-    const bool chunks = near_rows({&tdo, &tq, &tk, &tv, &tdq, &tdk, &tdv});
-    if (bytes && chunks) {
-        const AttentionSum forward{tq.op, tk.op, tv.op, tdo.op, {const_cast<float*>(state), states, per_head, d.dv, 1}, none, slots, d.dk, d.dv, 1.0f, d.scale, false, false};
-        e = launch_attention_states(forward, n, ahead, d.type, st);
-        if (e == hipSuccess) e = launch_attention_scan(forward, n, ahead, st);
-        if (e == hipSuccess) e = launch_attention_states(of_v, n, back, d.type, st);
-        if (e == hipSuccess) e = launch_attention_scan(of_v, n, back, st);
+    if (near_rows({&tdo, &tq, &tk, &tv, &tdq, &tdk, &tdv})) {
+        if (bytes) {
+            const AttentionSum forward{tq.op, tk.op, tv.op, tdo.op, {const_cast<float*>(state), states, per_head, d.dv, 1}, none, slots, d.dk, d.dv, 1.0f,
+                                       d.scale, false, false, ahead, false};
+            const AttentionSums both{{forward, of_v, of_v}, 2};
+            e = launch_attention_states(both, n, g, d.type, st);
+            if (e == hipSuccess) e = launch_attention_scan(both, n, g, st);
+        }
+        if (e == hipSuccess) e = launch_attention_chunks(gradients, n, g, d.type, st);
+    } else {
+        for (int i = 0; i < 3 && e == hipSuccess; ++i) e = launch_attention_recurrent(gradients.of[i], n, d.type, st);
     }
-    auto run = [&](const AttentionSum& sum, const AttentionSegments& g, bool turned_states) {
-        return chunks ? launch_attention_chunks(sum, n, g, turned_states, d.type, st) : launch_attention_recurrent(sum, n, d.type, st);
-    };
-    if (e == hipSuccess) e = run(of_q, ahead, true);
-    if (e == hipSuccess) e = run(of_k, back, true);
-    if (e == hipSuccess) e = run(of_v, back, false);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_k, tdk.op, n, d.kv_heads, d.dk, d.type, st);
     if (e == hipSuccess && share > 1) e = launch_attention_fold(part_v, tdv.op, n, d.kv_heads, d.dv, d.type, st);
     return launch_status(e);

@@ -88,9 +88,10 @@ __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel
 
 // The state before each segment from the segments' own sums, in place: a thread has one element of a sequence's and head's.
 constexpr int kScanAhead = 8;       // sums on their way at once
-__global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSum s, AttentionBatch n, AttentionSegments g)
+__global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSums sums, AttentionBatch n, AttentionSegments g)
 {
-    const int i = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y;
+    const AttentionSum& s = sums.of[blockIdx.y / (unsigned)n.H];
+    const int i = blockIdx.x * 256 + threadIdx.x, head = blockIdx.y % (unsigned)n.H;
     if (i >= s.DA * s.DC) return;
     const float g2 = n.log_decay[head] * 1.44269504088896341f;
     // (an infinity fades to none: where l is above zero, so is its power)
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSum s, Att
         if (segments < 2) continue;
         const float* first = attention::entry_of(s.first, s, n, seq, head);
         float state = first ? first[i / s.DC * s.first.row + i % s.DC * s.first.col] : 0.f;
-        float* p = g.states + slot * step + (int64_t)head * s.DA * s.DC + i;
+        float* p = s.states + slot * step + (int64_t)head * s.DA * s.DC + i;
         for (int64_t k = 0; k < segments; k += kScanAhead) {
             float own[kScanAhead];
 #pragma unroll
@@ -190,26 +191,30 @@ hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatc
     });
 }
 
-hipError_t launch_attention_states_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-hipError_t launch_attention_chunks_bf16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st);
-hipError_t launch_attention_states_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-hipError_t launch_attention_chunks_f16(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, hipStream_t st);
+hipError_t launch_attention_states_bf16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+hipError_t launch_attention_chunks_bf16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+hipError_t launch_attention_states_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
+hipError_t launch_attention_chunks_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
 
-hipError_t launch_attention_states(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
+hipError_t launch_attention_states(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
 {
     return ek == kElemBF16 ? launch_attention_states_bf16(s, n, g, st) : launch_attention_states_f16(s, n, g, st);
 }
 
-hipError_t launch_attention_chunks(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, bool turned, int ek, hipStream_t st)
+hipError_t launch_attention_chunks(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
 {
-    if (ek == kElemF32) return launch_attention_recurrent(s, n, ek, st);
-    return ek == kElemBF16 ? launch_attention_chunks_bf16(s, n, g, turned, st) : launch_attention_chunks_f16(s, n, g, turned, st);
+    if (ek == kElemF32) {
+        for (int i = 0; i < s.count; ++i)
+            if (const hipError_t e = launch_attention_recurrent(s.of[i], n, ek, st)) return e;
+        return hipSuccess;
+    }
+    return ek == kElemBF16 ? launch_attention_chunks_bf16(s, n, g, st) : launch_attention_chunks_f16(s, n, g, st);
 }
 
 AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed)
 {
     const int64_t rows = packed ? n.T : n.T * n.B, columns = (DC + 127) / 128;
-    AttentionSegments g{nullptr, (int64_t)1 << 62, 0};
+    AttentionSegments g{(int64_t)1 << 62, 0};
     const int64_t want = 512;          // workgroups
     if ((packed ? 1 : n.B) * n.H * columns < want) {
         const int64_t length = (rows * n.H * columns + want - 1) / want;
@@ -221,9 +226,9 @@ AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bo
     return g;
 }
 
-hipError_t launch_attention_scan(const AttentionSum& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
+hipError_t launch_attention_scan(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
-    const dim3 grid((unsigned)((s.DA * s.DC + 255) / 256), (unsigned)n.H, (unsigned)(n.B < 65535 ? n.B : 65535));
+    const dim3 grid((unsigned)((s.of[0].DA * s.of[0].DC + 255) / 256), (unsigned)(n.H * s.count), (unsigned)(n.B < 65535 ? n.B : 65535));
     hipLaunchKernelGGL(attention_scan_kernel, grid, dim3(256), 0, st, s, n, g);
     return hipGetLastError();
 }
