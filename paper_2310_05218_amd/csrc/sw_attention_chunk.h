@@ -1,4 +1,4 @@
-// Linear attention in chunks of 64 tokens on the matrix cores: bf16 and half.
+// Linear attention in chunks of tokens on the matrix cores: 64 of bf16 and half, 32 of fp32.
 //
 // A chunk of n tokens (rows i, j of a, b, c; state S before it; l the head's decay; e0 = 1 forwards in time, 0 backwards):
 //     y_i = alpha_y [ alpha_s sum_{j<=i} l^(i-j) (a_i . b_j) c_j  +  l^(i+e0) S^T a_i ],   S <- l^n S + alpha_s sum_j l^(n-e0-j) b_j c_j^T
@@ -12,7 +12,7 @@
 // values (17 bits; half, whose range they may leave, meets c as two bf16 values too).  The state: one value of the format, in half scaled
 // by a power of two; its rounding is y's own, on the part of y that comes from before the chunk (y's error against 64 bits at most 1.4 times
 // what its last rounding gives; with two values 10 % more time).  The state's new terms: three bf16 or two scaled half values, 22 bits and
-// more, as the state is an fp32 result.
+// more, as the state is an fp32 result.  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
 #pragma once
 
 #include "sw_attention.h"
@@ -97,11 +97,27 @@ struct Operand<kElemF16> {
     typedef f16x8 vec;
     static constexpr int kState = 1, kTerm = 2;
 };
+// fp32: K is 4, a value a lane; a vector holds the operands of four instructions, K in the order 4 (lane / 16) + element.
+template <>
+struct Operand<kElemF32> {
+    typedef f32x4 vec;
+};
+__device__ __forceinline__ f32x4 multiply(f32x4 a, f32x4 b, f32x4 c)
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+// Tokens of a chunk, and how many tiles of 16 and operand vectors of them there are.
+constexpr int chunk_of(int ek) { return ek == kElemF32 ? kAttentionChunk / 2 : kAttentionChunk; }
+constexpr int tiles_of(int ek) { return chunk_of(ek) / 16; }
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------------------------------------
-// Rows of W 16-bit values and 16 bytes more: sixteen rows' same 16 bytes (operands along a row) lie in different banks; the transposing
-// reads meet in twos, which costs less than an exchange of pieces, whose addresses are no constant apart.
-constexpr int pitch_of(int W) { return 2 * W + 16; }
+// Rows of W values and 16 bytes more: sixteen rows' same 16 bytes (operands along a row) lie in different banks; the transposing reads of
+// 16-bit values meet in twos, which costs less than an exchange of pieces, whose addresses are no constant apart.
+template <int EK>
+constexpr int pitch_of(int W) { return elem_size(EK) * W + 16; }
 
 // Four rows' values of one column, from the addresses of four neighbouring columns of one row each: lane i of sixteen gives row i / 4, columns
 // 4 (i % 4) ..., and gets column i.
@@ -118,16 +134,29 @@ __device__ __forceinline__ V joined(u32x2 a, u32x2 b)
     return __builtin_bit_cast(V, (u32x4){a[0], a[1], b[0], b[1]});
 }
 
-// The operand (column m0 + lane % 16, rows k0 + 8 (lane / 16) ... + 7) of a tile that lies row by row, m0 and k0 constants.
-template <int W>
+// The operand of a tile that lies row by row: column m0 + lane % 16, of the rows k0 and on those that are the lane's (8 (lane / 16) ... + 7;
+// fp32: 4 (lane / 16) ... + 3), m0 and k0 constants.
+template <int EK, int W>
 __device__ __forceinline__ const unsigned char* turned_base(const unsigned char* tile, int lane)
 {
-    return tile + (8 * (lane / 16) + lane % 16 / 4) * pitch_of(W) + 8 * (lane % 4);
+    if constexpr (EK == kElemF32)
+        return tile + 4 * (lane / 16) * pitch_of<EK>(W) + 4 * (lane % 16);
+    else
+        return tile + (8 * (lane / 16) + lane % 16 / 4) * pitch_of<EK>(W) + 8 * (lane % 4);
 }
-template <int W, class V>
-__device__ __forceinline__ V turned(const unsigned char* base, int m0, int k0)
+template <int EK, int W>
+__device__ __forceinline__ typename Operand<EK>::vec turned(const unsigned char* base, int m0, int k0)
 {
-    return joined<V>(turned_read(base + k0 * pitch_of(W) + 2 * m0), turned_read(base + (k0 + 4) * pitch_of(W) + 2 * m0));
+    typedef typename Operand<EK>::vec V;
+    const unsigned char* p = base + k0 * pitch_of<EK>(W) + elem_size(EK) * m0;
+    if constexpr (EK == kElemF32) {
+        V v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = *reinterpret_cast<const float*>(p + e * pitch_of<EK>(W));
+        return v;
+    } else {
+        return joined<V>(turned_read(p), turned_read(p + 4 * pitch_of<EK>(W)));
+    }
 }
 
 // A lane's number that the compiler takes for new: what is worked out from it is worked out again, not kept in registers from chunk to chunk.
@@ -137,26 +166,26 @@ __device__ __forceinline__ int renewed(int v)
     return v;
 }
 
-// A tile of kAttentionChunk rows of W values on its way from memory to LDS: rows `from` and on, `width` elements, zeros elsewhere.
+// A tile of a chunk's rows of W values on its way from memory to LDS: rows `from` and on, `width` elements, zeros elsewhere.
 // Whole vectors are loaded by all threads without a branch, those that have none from a place that has one, and become zeros on their way
-// into LDS: with loads in branches the compiler waits for each tile's before it begins the next one's (105 -> 60 us an output pass of
-// 4 x 4096 tokens, 16 heads of 128).  Rows that are no whole number of vectors go element by element, when the tile is written.
+// into LDS: with loads in branches the compiler waits for each tile's before it begins the next one's.  Rows that are no whole number of
+// vectors go element by element, when the tile is written.
 template <int EK, int W, int THREADS>
 struct Staged {
     typedef Row<EK> R;
     typedef typename R::T T;
-    static constexpr int NCH = W / 8, ALL = kAttentionChunk * NCH, N = (ALL + THREADS - 1) / THREADS, STEP = THREADS / NCH;
+    static constexpr int CH = chunk_of(EK), VEC = R::VEC, NCH = W / VEC, ALL = CH * NCH, N = (ALL + THREADS - 1) / THREADS, STEP = THREADS / NCH;
     static_assert(THREADS % NCH == 0 && (ALL % THREADS == 0 || ALL < THREADS), "whole rows, by all threads or each by one");
     typename R::vec v[N];
-    // `tile`: the first of the 64 rows in memory (its last, backwards in time), where there is one; `step`: from one to the next.  An element's
+    // `tile`: the first of the rows in memory (its last, backwards in time), where there is one; `step`: from one to the next.  An element's
     // place is a 32-bit distance from it: rows that are further apart than that allows are no case for this kernel.
-    static __device__ __forceinline__ unsigned place(int row, bool reverse, unsigned step) { return (reverse ? kAttentionChunk - 1 - row : row) * step; }
+    static __device__ __forceinline__ unsigned place(int row, bool reverse, unsigned step) { return (reverse ? CH - 1 - row : row) * step; }
     __device__ __forceinline__ void fetch(const T* tile, unsigned step, bool reverse, int from, int width)
     {
-        if (width % 8) return;
-        const int thread = renewed(threadIdx.x), c = thread % NCH * 8;
+        if (width % VEC) return;
+        const int thread = renewed(threadIdx.x), c = thread % NCH * VEC;
         int row = thread / NCH;
-        if (ALL < THREADS) row %= kAttentionChunk;
+        if (ALL < THREADS) row %= CH;
         const unsigned col = c < width ? c : 0;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
@@ -167,12 +196,12 @@ struct Staged {
     }
     __device__ __forceinline__ void put(unsigned char* to, const T* tile, unsigned step, bool reverse, int from, int width)
     {
-        const int thread = renewed(threadIdx.x), c = thread % NCH * 8, row = thread / NCH;
-        if (width % 8) {
+        const int thread = renewed(threadIdx.x), c = thread % NCH * VEC, row = thread / NCH;
+        if (width % VEC) {
 #pragma unroll 1
-            for (int i = thread; i < kAttentionChunk * W; i += THREADS) {
+            for (int i = thread; i < CH * W; i += THREADS) {
                 const int r = i / W, d = i % W;
-                *reinterpret_cast<T*>(to + r * pitch_of(W) + 2 * d) = r >= from && d < width ? tile[place(r, reverse, step) + d] : (T)0.f;
+                *reinterpret_cast<T*>(to + r * pitch_of<EK>(W) + (int)sizeof(T) * d) = r >= from && d < width ? tile[place(r, reverse, step) + d] : (T)0.f;
             }
             return;
         }
@@ -181,9 +210,9 @@ struct Staged {
             for (int k = 0; k < N; ++k)
                 if (row + k * STEP < from || c >= width) v[k] = (typename R::vec){};
         if (ALL < THREADS && thread >= ALL) return;
-        unsigned char* p = to + row * pitch_of(W) + thread % NCH * 16;
+        unsigned char* p = to + row * pitch_of<EK>(W) + thread % NCH * 16;
 #pragma unroll
-        for (int k = 0; k < N; ++k) *reinterpret_cast<typename R::vec*>(p + k * STEP * pitch_of(W)) = v[k];
+        for (int k = 0; k < N; ++k) *reinterpret_cast<typename R::vec*>(p + k * STEP * pitch_of<EK>(W)) = v[k];
     }
 };
 
@@ -208,9 +237,11 @@ __device__ __forceinline__ int half_exponent(float largest)
 
 // O = S^T a: rows, columns of y; columns, the chunk's tokens.  `a`: row lane % 16 of the tile, at the lane's place.
 template <int EK, int MT, int CT>
-__device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const float (&frame)[CT], const unsigned char* a, f32x4 (&O)[4][CT], const float (&reach)[4])
+__device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const float (&frame)[CT], const unsigned char* a, f32x4 (&O)[tiles_of(EK)][CT],
+                                              const float (&reach)[tiles_of(EK)])
 {
     typedef typename Operand<EK>::vec V;
+    constexpr int TI = tiles_of(EK);
     float in[CT], out = 1.f;
     if constexpr (EK == kElemF16) {
         // one scale for the wavefront's columns: they are the rows of what is computed
@@ -231,97 +262,134 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
         for (int c = 0; c < CT; ++c) in[c] = frame[c] * __builtin_amdgcn_ldexpf(1.f, -e);
         out = __builtin_amdgcn_ldexpf(1.f, e);
     }
+    if constexpr (EK == kElemF32) {
 #pragma unroll
-    for (int m = 0; m < MT / 2; ++m) {
-        V x[4], p[CT][Operand<EK>::kState];
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned char* at = a + 16 * i * pitch_of(16 * MT) + 64 * m;
-            x[i] = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 32));
+            for (int i = 0; i < TI; ++i) {
+                const V x = *reinterpret_cast<const V*>(a + 16 * i * pitch_of<EK>(16 * MT) + 64 * m);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) O[i][c] = multiply(S[m][c], x, O[i][c]);
+            }
+    } else {
+#pragma unroll
+        for (int m = 0; m < MT / 2; ++m) {
+            V x[TI], p[CT][Operand<EK>::kState];
+#pragma unroll
+            for (int i = 0; i < TI; ++i) {
+                const unsigned char* at = a + 16 * i * pitch_of<EK>(16 * MT) + 64 * m;
+                x[i] = joined<V>(*reinterpret_cast<const u32x2*>(at), *reinterpret_cast<const u32x2*>(at + 32));
+            }
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                f32x8 v;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][c][e % 4] * in[c] : S[2 * m + e / 4][c][e % 4];
+                parts(v, p[c]);
+            }
+#pragma unroll
+            for (int k = Operand<EK>::kState; k-- > 0;)
+#pragma unroll
+                for (int i = 0; i < TI; ++i)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) O[i][c] = multiply(p[c][k], x[i], O[i][c]);
         }
-#pragma unroll
-        for (int c = 0; c < CT; ++c) {
-            f32x8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][c][e % 4] * in[c] : S[2 * m + e / 4][c][e % 4];
-            parts(v, p[c]);
-        }
-#pragma unroll
-        for (int k = Operand<EK>::kState; k-- > 0;)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) O[i][c] = multiply(p[c][k], x[i], O[i][c]);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < TI; ++i)
 #pragma unroll
         for (int c = 0; c < CT; ++c) O[i][c] *= reach[i] * out;
 }
 
-// S <- whole S + sum over the chunk's tokens of b times weighted c (tokens 32 k + 8 (lane / 16) + e: weights in `tables`, those of k = 0 times shift).
+// S <- whole S + sum over the chunk's tokens of b times weighted c (an operand vector's tokens: weights in `tables`, those of
+// the first vector times shift).
 template <int EK, int MT, int CT>
 __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[CT], float whole, const typename Operand<EK>::vec (&cv)[2][CT],
                                              const float* tables, float shift, const unsigned char* b)
 {
     typedef typename Operand<EK>::vec V;
     const f32x4 tail[2] = {*reinterpret_cast<const f32x4*>(tables), *reinterpret_cast<const f32x4*>(tables + 256)};
-    auto weighted = [&](int k, int c) {
-        f32x8 w = widened<V>(cv[k][c]);
+    if constexpr (EK == kElemF32) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] *= tail[e / 4][e % 4];
-        if (k == 0) w *= shift;
-        return w;
-    };
-    float in[CT];
+        for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] *= whole;
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        float fades = whole;
-        if constexpr (EK == kElemF16) {
-            float largest = 0.f;
+        for (int k = 0; k < 2; ++k) {
+            V w[CT];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const f32x8 w = weighted(k, c);
+            for (int c = 0; c < CT; ++c) w[c] = cv[k][c] * tail[0] * (k == 0 ? shift : 1.f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[e]));
+            for (int m = 0; m < MT; ++m) {
+                const V x = turned<EK, 16 * MT>(b, 16 * m, 16 * k);
+#pragma unroll
+                for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, w[c], S[m][c]);
             }
-            largest = column_largest(largest);
-            const float next = largest > 0.f ? __builtin_amdgcn_ldexpf(1.f, half_exponent(largest)) : frame[c];
-            fades *= frame[c] / next;
-            in[c] = 1.f / next;
-            frame[c] = next;
         }
+    } else {
+        auto weighted = [&](int k, int c) {
+            f32x8 w = widened<V>(cv[k][c]);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) S[m][c] *= fades;
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        V p[CT][Operand<EK>::kTerm];
+            for (int e = 0; e < 8; ++e) w[e] *= tail[e / 4][e % 4];
+            if (k == 0) w *= shift;
+            return w;
+        };
+        float in[CT];
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-            f32x8 w = weighted(k, c);
-            if (EK == kElemF16) w *= in[c];
-            parts(w, p[c]);
+            float fades = whole;
+            if constexpr (EK == kElemF16) {
+                float largest = 0.f;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f32x8 w = weighted(k, c);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(w[e]));
+                }
+                largest = column_largest(largest);
+                const float next = largest > 0.f ? __builtin_amdgcn_ldexpf(1.f, half_exponent(largest)) : frame[c];
+                fades *= frame[c] / next;
+                in[c] = 1.f / next;
+                frame[c] = next;
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) S[m][c] *= fades;
         }
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const V x = turned<16 * MT, V>(b, 16 * m, 32 * k);
+        for (int k = 0; k < 2; ++k) {
+            V p[CT][Operand<EK>::kTerm];
 #pragma unroll
-            for (int q = Operand<EK>::kTerm; q-- > 0;)
+            for (int c = 0; c < CT; ++c) {
+                f32x8 w = weighted(k, c);
+                if (EK == kElemF16) w *= in[c];
+                parts(w, p[c]);
+            }
 #pragma unroll
-                for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, p[c][q], S[m][c]);
+            for (int m = 0; m < MT; ++m) {
+                const V x = turned<EK, 16 * MT>(b, 16 * m, 32 * k);
+#pragma unroll
+                for (int q = Operand<EK>::kTerm; q-- > 0;)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, p[c][q], S[m][c]);
+            }
         }
     }
 }
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------------
 
-constexpr int kPairPitch = pitch_of(kAttentionChunk), kPairs = kAttentionChunk * kPairPitch;       // bytes of one part of the pair products
+// Pair products in LDS: row i, column j; two bf16 parts, or fp32.
+template <int EK>
+constexpr int pair_pitch() { return pitch_of<EK>(chunk_of(EK)); }
+template <int EK>
+constexpr int pair_bytes() { return chunk_of(EK) * pair_pitch<EK>(); }      // of one part
+template <int EK>
+constexpr int pair_parts() { return EK == kElemF32 ? 1 : 2; }
+constexpr int kTables = 64 * 16 * 4;                // bytes of the lanes' weights
 
-constexpr int kTables = 64 * 16 * 4;                // ... of the lanes' weights
-
-template <int DAP, int WC, bool OUTPUT>
-constexpr int chunk_lds_bytes() { return kAttentionChunk * ((OUTPUT ? 2 : 1) * pitch_of(DAP) + pitch_of(WC)) + (OUTPUT ? 2 * kPairs : 0) + kTables; }
+template <int EK, int DAP, int WC, bool OUTPUT>
+constexpr int chunk_lds_bytes()
+{
+    return chunk_of(EK) * ((OUTPUT ? 2 : 1) * pitch_of<EK>(DAP) + pitch_of<EK>(WC)) + (OUTPUT ? pair_parts<EK>() * pair_bytes<EK>() : 0) + kTables;
+}
 
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
 
@@ -333,9 +401,9 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
 {
     typedef typename ElemOf<EK>::type T;
     typedef typename Operand<EK>::vec V;
-    constexpr int CH = kAttentionChunk, NW = 4, WC = 16 * CT * NW, MT = DAP / 16, THREADS = 64 * NW;
+    constexpr int CH = chunk_of(EK), TI = tiles_of(EK), ES = elem_size(EK), kPairPitch = pair_pitch<EK>(), kPairs = pair_bytes<EK>(), NW = 4, WC = 16 * CT * NW, MT = DAP / 16, THREADS = 64 * NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    unsigned char *tb = smem, *tc = tb + CH * pitch_of(DAP), *ta = tc + CH * pitch_of(WC), *tp = ta + (OUTPUT ? CH * pitch_of(DAP) : 0);
+    unsigned char *tb = smem, *tc = tb + CH * pitch_of<EK>(DAP), *ta = tc + CH * pitch_of<EK>(WC), *tp = ta + (OUTPUT ? CH * pitch_of<EK>(DAP) : 0);
 
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), l16 = lane % 16, own = lane / 16;
     // Workgroups side by side: the sums of one segment and head, then its heads, whose rows lie side by side in memory.  The outputs go
@@ -356,13 +424,14 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     const float g2 = n.log_decay[head] * 1.44269504088896341f;
     const float chunk_decay = uniform(power(g2, CH)), shift = uniform(power(g2, CH / 2));
     // The lanes' weights, all wavefronts' the same, sixteen values a lane in fours:
-    // 0, 1: of a chunk's tokens 32 k + 8 own + e, l^(CH - e0 - token) without `shift` for k = 0
+    // 0, 1: of a chunk's tokens, the second operand vector's 8 own + e (fp32: 4 own + e): l^(CH - e0 - token)
     // 2, 3: of pair products (row j = 4 own + e, column i = l16 of a tile), on the diagonal and with i's tile the next after j's
-    float* tables = reinterpret_cast<float*>(tp + (OUTPUT ? 2 * kPairs : 0)) + 4 * lane;
+    float* tables = reinterpret_cast<float*>(tp + (OUTPUT ? pair_parts<EK>() * kPairs : 0)) + 4 * lane;
     for (int k = wave; k < (OUTPUT ? 4 : 2); k += NW)
         for (int e = 0; e < 4; ++e) {
             const int gap = l16 - 4 * own - e;
-            const float v = k < 2 ? power(g2, 32 - e0 - 8 * own - 4 * k - e) : gap < 0 && k == 2 ? 0.f : s.alpha_y * power(g2, k == 2 ? gap : 16 + gap);
+            const int after = CH / 2 - e0 - (EK == kElemF32 ? 4 : 8) * own - 4 * k - e;
+            const float v = k < 2 ? power(g2, after < 0 ? 0 : after) : gap < 0 && k == 2 ? 0.f : s.alpha_y * power(g2, k == 2 ? gap : 16 + gap);
             tables[256 * k + e] = s.alpha_s * v;
         }
     float further[3];
@@ -371,14 +440,15 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
 #pragma unroll
         for (int k = 0; k < 3; ++k) further[k] = uniform(power(g2, 16 * (k + 1)));
         // (tiles above the diagonal that are read with their neighbours and never written)
-        for (int i = threadIdx.x; i < 2 * 2 * 16 * 2; i += THREADS) {
+        for (int i = threadIdx.x; EK != kElemF32 && i < 2 * 2 * 16 * 2; i += THREADS) {
             const int part = i / 64, tile = i / 32 % 2, row = i / 2 % 16, side = i % 2;
             *reinterpret_cast<u32x4*>(tp + part * kPairs + (32 * tile + row) * kPairPitch + 64 * tile + 32 + 16 * side) = (u32x4){0, 0, 0, 0};
         }
     }
     // places in the tiles
-    const unsigned char *along_b = tb + l16 * pitch_of(DAP) + 16 * own, *along_a = ta + l16 * pitch_of(DAP) + 16 * own;
-    const unsigned char *picked_a = ta + l16 * pitch_of(DAP) + 8 * own, *down_b = turned_base<DAP>(tb, lane), *down_c = turned_base<WC>(tc, lane) + 32 * CT * wave;
+    const unsigned char *along_b = tb + l16 * pitch_of<EK>(DAP) + 16 * own, *along_a = ta + l16 * pitch_of<EK>(DAP) + 16 * own;
+    const unsigned char* picked_a = ta + l16 * pitch_of<EK>(DAP) + 4 * ES * own;
+    const unsigned char *down_b = turned_base<EK, DAP>(tb, lane), *down_c = turned_base<EK, WC>(tc, lane) + 16 * ES * CT * wave;
     unsigned char* pairs = tp + l16 * kPairPitch;
 
     f32x4 S[MT][CT];
@@ -428,31 +498,37 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
-            for (int c = 0; c < CT; ++c) cv[k][c] = turned<WC, V>(down_c, 16 * c, 32 * k);
+            for (int c = 0; c < CT; ++c) cv[k][c] = turned<EK, WC>(down_c, 16 * c, CH / 2 * k);
         if constexpr (OUTPUT) {
-            // pair products: the ten tiles on and below the diagonal, (0,0) (1,0) (1,1) (2,0) ..., a wavefront after another
-            for (int tile = wave; tile < 10; tile += NW) {
+            // pair products: the tiles on and below the diagonal, (0,0) (1,0) (1,1) (2,0) ..., a wavefront after another
+            for (int tile = wave; tile < TI * (TI + 1) / 2; tile += NW) {
                 const int i = (tile >= 1) + (tile >= 3) + (tile >= 6), j = tile - i * (i + 1) / 2;
                 f32x4 p = 0.f;
 #pragma unroll
-                for (int k = 0; k < DAP / 32; ++k)
-                    p = multiply(*reinterpret_cast<const V*>(along_b + 16 * j * pitch_of(DAP) + 64 * k),
-                                 *reinterpret_cast<const V*>(along_a + 16 * i * pitch_of(DAP) + 64 * k), p);
+                for (int k = 0; k < DAP * ES / 64; ++k)
+                    p = multiply(*reinterpret_cast<const V*>(along_b + 16 * j * pitch_of<EK>(DAP) + 64 * k),
+                                 *reinterpret_cast<const V*>(along_a + 16 * i * pitch_of<EK>(DAP) + 64 * k), p);
                 p *= *reinterpret_cast<const f32x4*>(tables + (i == j ? 512 : 768)) * (i - j < 2 ? 1.f : further[i - j - 2]);
-                unsigned char* to = pairs + 16 * i * kPairPitch + 32 * j + 8 * own;
-                const u32x2 h = {pack<bf16x8>(p[0], p[1]), pack<bf16x8>(p[2], p[3])};
-                const f32x2 h0 = widen<bf16x8>(h[0]), h1 = widen<bf16x8>(h[1]);
-                *reinterpret_cast<u32x2*>(to) = h;
-                *reinterpret_cast<u32x2*>(to + kPairs) = (u32x2){pack<bf16x8>(p[0] - h0[0], p[1] - h0[1]), pack<bf16x8>(p[2] - h1[0], p[3] - h1[1])};
+                unsigned char* to = pairs + 16 * i * kPairPitch + 16 * ES * j + 4 * ES * own;
+                if constexpr (EK == kElemF32) {
+                    *reinterpret_cast<f32x4*>(to) = p;
+                } else {
+                    const u32x2 h = {pack<bf16x8>(p[0], p[1]), pack<bf16x8>(p[2], p[3])};
+                    const f32x2 h0 = widen<bf16x8>(h[0]), h1 = widen<bf16x8>(h[1]);
+                    *reinterpret_cast<u32x2*>(to) = h;
+                    *reinterpret_cast<u32x2*>(to + kPairs) = (u32x2){pack<bf16x8>(p[0] - h0[0], p[1] - h0[1]), pack<bf16x8>(p[2] - h1[0], p[3] - h1[1])};
+                }
             }
 
-            f32x4 O[4][CT];
+            f32x4 O[TI][CT];
 #pragma unroll
-            for (int i = 0; i < 4 * CT; ++i) O[i / CT][i % CT] = 0.f;
-            float reach[4] = {near, near * further[0], near * further[1], near * further[2]};
+            for (int i = 0; i < TI * CT; ++i) O[i / CT][i % CT] = 0.f;
+            float reach[TI];
+#pragma unroll
+            for (int i = 0; i < TI; ++i) reach[i] = i == 0 ? near : near * further[i - 1];
             if (from > 0)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < TI; ++i) {
                     const int token = 16 * i + l16 - from;
                     reach[i] = s.alpha_y * power(g2, (token < 0 ? 0 : token) + e0);
                 }
@@ -461,32 +537,41 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
             // pair products times c
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                bf16x8 c2[CT][2];
-                if constexpr (EK == kElemF16)
+                if constexpr (EK == kElemF32) {
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) parts(widened<V>(cv[k][c]), c2[c]);
+                    for (int i = k; i < TI; ++i) {
+                        const f32x4 p = *reinterpret_cast<const f32x4*>(pairs + 16 * i * kPairPitch + 64 * k + 16 * own);
 #pragma unroll
-                for (int i = 2 * k; i < 4; ++i) {
-                    bf16x8 p[2];
+                        for (int c = 0; c < CT; ++c) O[i][c] = multiply(cv[k][c], p, O[i][c]);
+                    }
+                } else {
+                    bf16x8 c2[CT][2];
+                    if constexpr (EK == kElemF16)
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 16 * i * kPairPitch + 64 * k + 16 * own);
+                        for (int c = 0; c < CT; ++c) parts(widened<V>(cv[k][c]), c2[c]);
 #pragma unroll
-                    for (int c = 0; c < CT; ++c)
-                        if constexpr (EK == kElemF16) {
-                            O[i][c] = multiply(c2[c][1], p[0], O[i][c]);
-                            O[i][c] = multiply(c2[c][0], p[1], O[i][c]);
-                            O[i][c] = multiply(c2[c][0], p[0], O[i][c]);
-                        } else {
-                            O[i][c] = multiply(cv[k][c], p[1], O[i][c]);
-                            O[i][c] = multiply(cv[k][c], p[0], O[i][c]);
-                        }
+                    for (int i = 2 * k; i < TI; ++i) {
+                        bf16x8 p[2];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 16 * i * kPairPitch + 64 * k + 16 * own);
+#pragma unroll
+                        for (int c = 0; c < CT; ++c)
+                            if constexpr (EK == kElemF16) {
+                                O[i][c] = multiply(c2[c][1], p[0], O[i][c]);
+                                O[i][c] = multiply(c2[c][0], p[1], O[i][c]);
+                                O[i][c] = multiply(c2[c][0], p[0], O[i][c]);
+                            } else {
+                                O[i][c] = multiply(cv[k][c], p[1], O[i][c]);
+                                O[i][c] = multiply(cv[k][c], p[0], O[i][c]);
+                            }
+                    }
                 }
             }
             bad |= any_nonfinite(O);
             const int64_t to = tile_of(s.y, t) + col0 + wave * 16 * CT;
             const int now = renewed(lane);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < TI; ++i) {
                 const int row = 16 * i + now % 16;
                 if (row < from) continue;
 #pragma unroll
@@ -543,7 +628,7 @@ hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const
             if (!done[j] && padded(all.of[j].DA) == da && columns(all.of[j].DC) == columns(dc))
                 s.of[s.count++] = all.of[j], done[j] = true;
         auto with = [&](auto dap, auto ct) {
-            constexpr int lds = chunk_lds_bytes<dap(), 64 * ct(), OUTPUT>();
+            constexpr int lds = chunk_lds_bytes<EK, dap(), 64 * ct(), OUTPUT>();
             static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(attention_chunk_kernel<EK, dap(), ct(), OUTPUT>),
                                                                hipFuncAttributeMaxDynamicSharedMemorySize, lds);
             if (attr != hipSuccess) return attr;

@@ -110,7 +110,7 @@ bool near_rows(std::initializer_list<const Tensor4*> tensors)
 int64_t state_bytes(const sw_linear_attention_dims& d, bool packed)
 {
     const AttentionSegments g = segments_of(d, packed);
-    return d.type == SW_F32 || g.length > d.T ? 0 : align16(g.count * d.heads * d.dk * d.dv * 4);
+    return g.length > d.T ? 0 : align16(g.count * d.heads * d.dk * d.dv * 4);
 }
 
 // Bytes of the fp32 rows of dk and of dv that heads sharing them are added from (0: not shared).

@@ -191,25 +191,20 @@ hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatc
     });
 }
 
-hipError_t launch_attention_states_bf16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-hipError_t launch_attention_chunks_bf16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-hipError_t launch_attention_states_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-hipError_t launch_attention_chunks_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);
-
-hipError_t launch_attention_states(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
-{
-    return ek == kElemBF16 ? launch_attention_states_bf16(s, n, g, st) : launch_attention_states_f16(s, n, g, st);
-}
-
-hipError_t launch_attention_chunks(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st)
-{
-    if (ek == kElemF32) {
-        for (int i = 0; i < s.count; ++i)
-            if (const hipError_t e = launch_attention_recurrent(s.of[i], n, ek, st)) return e;
-        return hipSuccess;
+// (a translation unit for each format's kernels)
+#define SW_ATTENTION_UNITS(what)                                                                                                        \
+    hipError_t launch_attention_##what##_f32(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);  \
+    hipError_t launch_attention_##what##_bf16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st); \
+    hipError_t launch_attention_##what##_f16(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st);  \
+    hipError_t launch_attention_##what(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st) \
+    {                                                                                                                                   \
+        return ek == kElemF32    ? launch_attention_##what##_f32(s, n, g, st)                                                              \
+               : ek == kElemBF16 ? launch_attention_##what##_bf16(s, n, g, st)                                                             \
+                                 : launch_attention_##what##_f16(s, n, g, st);                                                             \
     }
-    return ek == kElemBF16 ? launch_attention_chunks_bf16(s, n, g, st) : launch_attention_chunks_f16(s, n, g, st);
-}
+SW_ATTENTION_UNITS(states)
+SW_ATTENTION_UNITS(chunks)
+#undef SW_ATTENTION_UNITS
 
 AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed)
 {
