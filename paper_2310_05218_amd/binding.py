@@ -312,10 +312,13 @@ def _bind_current_stream():
 
 # operations of the native short way (csrc/binding/sw_binding.cpp), in its order
 (_CONV1D, _POOL1D, _POOL2D, _CONV2D, _BIAS_RELU, _DILATED, _DEPTHWISE, _DEPTHWISE_BIAS_RELU, _DEPTHWISE_BF16, _S8, _S8_REQUANT, _S8_NHWC,
- _NHWC) = range(13)
+ _NHWC, _LAYER_NORM, _LAYER_NORM_BACKWARD, _ATTENTION, _ATTENTION_BACKWARD, _ATTENTION_STEP) = range(18)
 _NATIVE_ENTRIES = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2d_bias_relu", "sw_conv2d_dilated", "sw_conv2d_depthwise",
                    "sw_conv2d_depthwise_bias_relu", "sw_conv2d_depthwise_bf16", "sw_conv2d_s8", "sw_conv2d_s8_requant", "sw_conv2d_s8_nhwc",
-                   "sw_conv2d_s8_nhwc_requant", "sw_conv2d_nhwc", "sw_conv2d_bf16_nhwc", "sw_conv2d_f16_nhwc")
+                   "sw_conv2d_s8_nhwc_requant", "sw_conv2d_nhwc", "sw_conv2d_bf16_nhwc", "sw_conv2d_f16_nhwc",
+                   "sw_layer_norm", "sw_layer_norm_backward", "sw_layer_norm_backward_workspace_bytes", "sw_linear_attention",
+                   "sw_linear_attention_workspace_bytes", "sw_linear_attention_backward", "sw_linear_attention_backward_workspace_bytes",
+                   "sw_linear_attention_step")
 
 
 def _bind_native(*args):

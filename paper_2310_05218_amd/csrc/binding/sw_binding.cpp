@@ -1,22 +1,26 @@
 // The short way from a Python call to the C ABI: checks, output extents, the output tensor and the call in one native function.
 //
-// run(op, x, w, bias, scale, integers and flags ...) returns the output tensor, a status code other than SW_OK, or None for whatever
+// run(op, x, w, bias, scale, integers and flags ...; layer norm and attention: their own arguments) returns the output tensor or a tuple of
+// them, a status code other than SW_OK, or None for whatever
 // it does not take (other types, layouts, devices, arguments out of range): the caller then goes the long way, which takes it or says
 // why not.  Nothing is kept between calls but the entry points' addresses.
 //
 // Measured on one 256 x 256 image under a 3 x 3 filter, whose kernel takes 3.7 us in a graph, calls one after the other: 4.4 to 4.9 us a call,
-// 7.05 in Python through ctypes (2.3 of which the checks, 1.4 torch.empty, 0.6 ctypes).
+// 7.05 in Python through ctypes (2.3 of which the checks, 1.4 torch.empty, 0.6 ctypes).  A layer norm of 4 rows of 2048, whose kernel takes 2.3:
+// 5.0 us a call, 8.2 in Python; one token of linear attention on 16 heads of 128 x 128, whose kernel takes 4.1: 5.1.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
+#include <cmath>
 
 #include "../../../include/swconv.h"
 
 namespace {
 
-enum Op { kConv1d, kPool1d, kPool2d, kConv2d, kBiasRelu, kDilated, kDepthwise, kDepthwiseBiasRelu, kDepthwiseBf16, kS8, kS8Requant, kS8Nhwc, kNhwc, kOps };
+enum Op { kConv1d, kPool1d, kPool2d, kConv2d, kBiasRelu, kDilated, kDepthwise, kDepthwiseBiasRelu, kDepthwiseBf16, kS8, kS8Requant, kS8Nhwc, kNhwc, kLayerNorm, kLayerNormBackward,
+          kAttention, kAttentionBackward, kAttentionStep };
 
 struct Entries {
     decltype(&sw_conv1d) conv1d;
@@ -35,6 +39,14 @@ struct Entries {
     decltype(&sw_conv2d_nhwc) nhwc;
     decltype(&sw_conv2d_bf16_nhwc) bf16_nhwc;
     decltype(&sw_conv2d_f16_nhwc) f16_nhwc;
+    decltype(&sw_layer_norm) layer_norm;
+    decltype(&sw_layer_norm_backward) layer_norm_backward;
+    decltype(&sw_layer_norm_backward_workspace_bytes) layer_norm_backward_workspace;
+    decltype(&sw_linear_attention) attention;
+    decltype(&sw_linear_attention_workspace_bytes) attention_workspace;
+    decltype(&sw_linear_attention_backward) attention_backward;
+    decltype(&sw_linear_attention_backward_workspace_bytes) attention_backward_workspace;
+    decltype(&sw_linear_attention_step) attention_step;
 };
 Entries g_entry;
 constexpr int kEntries = sizeof(Entries) / sizeof(void*);
@@ -238,12 +250,254 @@ PyObject* run_op(int op, PyObject* const* a, Py_ssize_t n)
     return nullptr;
 }
 
+// ---- layer norm and linear attention: several outputs, strided tensors, workspaces --------------------------------------------------
+
+// the sw_type of a tensor on the GPU; false: none
+bool type_of(const at::Tensor& t, int* type)
+{
+    const auto k = t.scalar_type();
+    *type = k == at::kFloat ? SW_F32 : k == at::kBFloat16 ? SW_BF16 : SW_F16;
+    return (g_host ? t.is_cpu() : t.is_cuda()) && (k == at::kFloat || k == at::kBFloat16 || k == at::kHalf);
+}
+
+const at::Tensor* any_tensor(PyObject* o) { return THPVariable_CheckExact(o) ? &THPVariable_Unpack(o) : nullptr; }
+
+// a contiguous tensor of that type and shape, or None where that may be (*t null then)
+bool plain(PyObject* o, at::ScalarType type, at::IntArrayRef shape, bool none, const at::Tensor** t)
+{
+    *t = nullptr;
+    if (o == Py_None) return none;
+    *t = tensor(o, type, (int)shape.size());
+    return *t && (*t)->sizes() == shape;
+}
+
+// a Python number that a float holds, `none` for None
+bool number(PyObject* o, double none, float* v)
+{
+    double d = none;
+    if (PyFloat_CheckExact(o))
+        d = PyFloat_AS_DOUBLE(o);
+    else if (o != Py_None)
+        return false;
+    if (!(d >= -3e38 && d <= 3e38)) return false;
+    *v = (float)d;
+    return true;
+}
+
+// rows of the last dimension, evenly apart
+struct Rows {
+    int64_t rows, width, stride;
+    bool set(const at::Tensor& t)
+    {
+        if (t.dim() < 1 || t.numel() == 0) return false;
+        const auto n = t.sizes(), s = t.strides();
+        const int last = (int)t.dim() - 1;
+        width = n[last];
+        rows = t.numel() / width, stride = width;
+        if (t.is_contiguous()) return true;
+        if (s[last] != 1 && width > 1) return false;
+        int64_t done = 1;
+        for (int i = last - 1; i >= 0; --i) {
+            if (n[i] == 1) continue;
+            if (done == 1)
+                stride = s[i];
+            else if (s[i] != done * stride)
+                return false;
+            done *= n[i];
+        }
+        return true;
+    }
+};
+
+// f(stream) without the lock; then `count` tensors as a tuple (one as it is), or the status
+template <class F>
+PyObject* call_into(at::Tensor* const* out, int count, F&& f)
+{
+    void* const stream = g_host ? nullptr : static_cast<void*>(c10::hip::getCurrentHIPStream().stream());
+    int rc;
+    {
+        const Unlocked unlocked;
+        rc = f(stream);
+    }
+    if (rc != SW_OK) return PyLong_FromLong(rc);
+    if (count == 1) return THPVariable_Wrap(*out[0]);
+    PyObject* all = PyTuple_New(count);
+    for (int i = 0; all && i < count; ++i) {
+        PyObject* one = Py_None;
+        if (out[i])
+            one = THPVariable_Wrap(*out[i]);
+        else
+            Py_INCREF(one);
+        if (!one) {
+            Py_DECREF(all);
+            return nullptr;
+        }
+        PyTuple_SET_ITEM(all, i, one);
+    }
+    return all;
+}
+
+float* floats(const at::Tensor* t) { return t ? static_cast<float*>(t->mutable_data_ptr()) : nullptr; }
+
+// (x, weight, bias, eps, stats), (dy, x, weight, mean, rstd, params)
+PyObject* run_norm(bool backward, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != (backward ? 6 : 5)) return nullptr;
+    const at::Tensor *x = any_tensor(a[backward ? 1 : 0]), *w, *b = nullptr;
+    int type, flags;
+    Rows rx;
+    if (!x || !type_of(*x, &type) || !rx.set(*x)) return nullptr;
+    const int64_t width[1] = {rx.width};
+    if (!flag(a[n - 1], &flags) || !plain(a[backward ? 2 : 1], at::kFloat, width, true, &w)) return nullptr;
+    const auto stats = x->sizes().slice(0, x->dim() - 1);
+    const auto f32 = x->options().dtype(at::kFloat);
+    if (!backward) {
+        float eps;
+        if (!plain(a[2], at::kFloat, width, true, &b) || a[3] == Py_None || !number(a[3], 0, &eps)) return nullptr;
+        const Address xa(x), wa(w), ba(b);
+        at::Tensor y = at::empty(x->sizes(), x->options()), mean, rstd;
+        if (flags) mean = at::empty(stats, f32), rstd = at::empty(stats, f32);
+        void* const yp = y.mutable_data_ptr();
+        float *const mp = flags ? floats(&mean) : nullptr, *const rp = flags ? floats(&rstd) : nullptr;
+        at::Tensor* const out[3] = {&y, &mean, &rstd};
+        return call_into(out, flags ? 3 : 1, [&](void* st) {
+            return g_entry.layer_norm(xa.p, wa, ba, yp, mp, rp, rx.rows, rx.width, rx.stride, rx.width, eps, type, st);
+        });
+    }
+    const at::Tensor *dy = any_tensor(a[0]), *mean, *rstd;
+    Rows rdy;
+    int dtype;
+    if (!dy || !type_of(*dy, &dtype) || dtype != type || dy->sizes() != x->sizes() || !rdy.set(*dy) || !plain(a[3], at::kFloat, stats, false, &mean) ||
+        !plain(a[4], at::kFloat, stats, false, &rstd))
+        return nullptr;
+    const Address da(dy), xa(x), wa(w), ma(mean), ra(rstd);
+    at::Tensor dx = at::empty(x->sizes(), x->options()), dw, db, work;
+    int64_t need = 0;
+    if (flags) {
+        need = g_entry.layer_norm_backward_workspace(rx.rows, rx.width);
+        dw = at::empty(width, f32), db = at::empty(width, f32), work = at::empty({need}, x->options().dtype(at::kByte));
+    }
+    void *const dxp = dx.mutable_data_ptr(), *const wp = need ? work.mutable_data_ptr() : nullptr;
+    float *const dwp = flags ? floats(&dw) : nullptr, *const dbp = flags ? floats(&db) : nullptr;
+    at::Tensor* const out[3] = {&dx, flags ? &dw : nullptr, flags ? &db : nullptr};
+    return call_into(out, 3, [&](void* st) {
+        return g_entry.layer_norm_backward(da.p, xa.p, wa, ma, ra, dxp, dwp, dbp, rx.rows, rx.width, rdy.stride, rx.stride, rx.width, type, wp, need, st);
+    });
+}
+
+// [..., heads, width] of that type and shape, the innermost dimension contiguous
+bool heads_of(PyObject* o, const at::Tensor& like, at::IntArrayRef shape, const at::Tensor** t, sw_strides* s)
+{
+    *t = any_tensor(o);
+    if (!*t || (*t)->is_cuda() != like.is_cuda() || (*t)->scalar_type() != like.scalar_type() || (*t)->sizes() != shape) return false;
+    const auto st = (*t)->strides();
+    const size_t d = st.size();
+    if (st[d - 1] != 1 && shape[d - 1] > 1) return false;
+    *s = sw_strides{d == 4 ? st[0] : 0, st[d - 3], st[d - 2]};
+    return true;
+}
+
+sw_strides strides_of(at::IntArrayRef shape)
+{
+    const size_t d = shape.size();
+    return sw_strides{d == 4 ? shape[1] * shape[2] * shape[3] : 0, shape[d - 2] * shape[d - 1], shape[d - 1]};
+}
+
+// (q, k, v, log_decay, scale, starts, state, slots, final_state), (do, q, k, v, log_decay, scale, starts, state, slots, d_final_state, d_state)
+// and (q, k, v, log_decay, scale, state, slots)
+PyObject* run_attention(int op, PyObject* const* a, Py_ssize_t n)
+{
+    const bool step = op == kAttentionStep, backward = op == kAttentionBackward;
+    if (n != (step ? 7 : backward ? 11 : 9)) return nullptr;
+    PyObject* const pdo = backward ? *a++ : nullptr;
+    PyObject *const pstarts = step ? Py_None : a[5], *const pstate = a[step ? 5 : 6], *const pslots = a[step ? 6 : 7];
+    const at::Tensor *q = any_tensor(a[0]), *k = any_tensor(a[1]), *v = any_tensor(a[2]), *starts = nullptr, *slots, *decay;
+    const bool packed = pstarts != Py_None;
+    const int64_t dim = step || packed ? 3 : 4;
+    sw_linear_attention_dims d{};
+    if (!q || !k || !v || !type_of(*q, &d.type) || q->dim() != dim || k->dim() != dim || v->dim() != dim || q->numel() == 0 || k->numel() == 0 ||
+        v->numel() == 0 || !fits(*q) || !fits(*k) || !fits(*v))
+        return nullptr;
+    if (packed && (!(starts = tensor(pstarts, at::kInt, 1)) || starts->size(0) < 2 || starts->size(0) > INT32_MAX)) return nullptr;
+    d.heads = (int)q->size(dim - 2), d.kv_heads = (int)v->size(dim - 2), d.dk = (int)q->size(dim - 1), d.dv = (int)v->size(dim - 1);
+    d.B = packed ? (int)starts->size(0) - 1 : (int)q->size(0);
+    d.T = step ? 1 : q->size(dim - 3);
+    if (d.heads % d.kv_heads || !number(a[4], std::pow((double)d.dk, -0.5), &d.scale)) return nullptr;
+    // shapes [..., heads, width] on q's first dimensions
+    int64_t sq[4], sk[4], sv[4], so[4];
+    for (int i = 0; i < dim - 2; ++i) sq[i] = sk[i] = sv[i] = so[i] = q->size(i);
+    sq[dim - 2] = so[dim - 2] = d.heads, sk[dim - 2] = sv[dim - 2] = d.kv_heads;
+    sq[dim - 1] = sk[dim - 1] = d.dk, sv[dim - 1] = so[dim - 1] = d.dv;
+    const at::IntArrayRef nq(sq, dim), nk(sk, dim), nv(sv, dim), no(so, dim);
+    sw_strides tq, tk, tv, tdo;
+    const int64_t heads[1] = {d.heads}, sequences[1] = {d.B};
+    const at::Tensor* d_o = nullptr;
+    if (!heads_of(a[0], *q, nq, &q, &tq) || !heads_of(a[1], *q, nk, &k, &tk) || !heads_of(a[2], *q, nv, &v, &tv) ||
+        (backward && !heads_of(pdo, *q, no, &d_o, &tdo)) || !plain(a[3], at::kFloat, heads, false, &decay) ||
+        !plain(pslots, at::kInt, sequences, true, &slots))
+        return nullptr;
+    auto states = [&](PyObject* o, int64_t count, const at::Tensor** t) {
+        const int64_t shape[4] = {count, d.heads, d.dk, d.dv};
+        return plain(o, at::kFloat, shape, true, t);
+    };
+    PyObject* const pfinal = step ? Py_None : a[8];         // (backward: d_final_state)
+    const at::Tensor *held = any_tensor(pstate != Py_None || backward ? pstate : pfinal), *state, *last, *d_state = nullptr;
+    if (held && (held->dim() != 4 || held->size(0) > INT32_MAX)) return nullptr;
+    d.n_states = held ? (int)held->size(0) : 0;
+    if (!states(pstate, d.n_states, &state) || !states(pfinal, backward ? d.B : d.n_states, &last) || (step && !state) ||
+        (backward && !states(a[9], d.B, &d_state)))
+        return nullptr;
+    const Address qa(q), ka(k), va(v), ga(decay), sa(slots), ca(starts);
+    const auto options = q->options();
+    if (step) {
+        float* const sp = floats(state);
+        at::Tensor o = at::empty(no, options);
+        void* const op = o.mutable_data_ptr();
+        auto as_rows = [](sw_strides s) { return sw_strides{s.token, 0, s.head}; };
+        tq = as_rows(tq), tk = as_rows(tk), tv = as_rows(tv);
+        const sw_strides to = as_rows(strides_of(no));
+        at::Tensor* const out[1] = {&o};
+        return call_into(out, 1, [&](void* st) { return g_entry.attention_step(qa.p, ka.p, va.p, op, ga, sp, sa, &d, &tq, &tk, &tv, &to, st); });
+    }
+    at::Tensor work;
+    const int64_t need = backward ? g_entry.attention_backward_workspace(&d, packed) : g_entry.attention_workspace(&d, packed);
+    if (need) work = at::empty({need}, options.dtype(at::kByte));
+    void* const wp = need ? work.mutable_data_ptr() : nullptr;
+    const Address first(state);
+    if (!backward) {
+        float* const lp = floats(last);
+        at::Tensor o = at::empty(no, options);
+        void* const op = o.mutable_data_ptr();
+        const sw_strides to = strides_of(no);
+        at::Tensor* const out[1] = {&o};
+        return call_into(out, 1, [&](void* st) {
+            return g_entry.attention(qa.p, ka.p, va.p, op, ga, first, lp, sa, ca, &d, &tq, &tk, &tv, &to, wp, need, st);
+        });
+    }
+    const Address da(d_o), fa(last);
+    float* const gs = floats(d_state);
+    at::Tensor dq = at::empty(nq, options), dk = at::empty(nk, options), dv = at::empty(nv, options);
+    void *const gq = dq.mutable_data_ptr(), *const gk = dk.mutable_data_ptr(), *const gv = dv.mutable_data_ptr();
+    const sw_strides uq = strides_of(nq), uk = strides_of(nk), uv = strides_of(nv);
+    at::Tensor* const out[3] = {&dq, &dk, &dv};
+    return call_into(out, 3, [&](void* st) {
+        return g_entry.attention_backward(da.p, qa.p, ka.p, va.p, ga, first, fa, gq, gk, gv, gs, sa, ca, &d, &tdo, &tq, &tk, &tv, &uq, &uk, &uv, wp, need, st);
+    });
+}
+
 PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     int op;
     if (g_bound && n >= 1 && integer(a[0], &op)) {
         try {
-            if (PyObject* y = run_op(op, a + 1, n - 1)) return y;
+            PyObject* y;
+            if (op == kLayerNorm || op == kLayerNormBackward)
+                y = run_norm(op == kLayerNormBackward, a + 1, n - 1);
+            else if (op >= kAttention && op <= kAttentionStep)
+                y = run_attention(op, a + 1, n - 1);
+            else
+                y = run_op(op, a + 1, n - 1);
+            if (y) return y;
         } catch (...) {
             // (a tensor without storage, memory that is not there: the long way says it as it always has)
         }

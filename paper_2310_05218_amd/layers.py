@@ -3,12 +3,15 @@
 Tensors may have any strides as long as the innermost dimension is contiguous (a slice of a fused projection, heads before
 tokens).  Outputs that are not given, and the scratch memory of a call, are allocated on the stream that the call runs on, so
 that the caching allocator hands them to nothing else before the call's kernels are done with them.
+
+Calls on the current stream without `out` go the native short way of `binding`, which takes them or leaves them to the checks here.
 """
 from __future__ import annotations
 
 import contextlib
 
-from .binding import SW_BF16, SW_ERR_SHAPE, SW_F16, SW_F32, SwError, SwLinearAttentionDims, SwStrides, _check, _stream, lib
+from . import binding
+from .binding import SW_BF16, SW_ERR_SHAPE, SW_F16, SW_F32, SwError, SwLinearAttentionDims, SwStrides, _check, _done, _stream, lib
 
 _types = None
 
@@ -74,6 +77,10 @@ def _rows(t, like, name):
 def sw_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stats: bool = False, out=None, stream=None):
     """Layer norm over the last dimension: x [..., C] fp32, bf16 or half, weight and bias [C] fp32 or None -> y as x;
     with `stats` (y, mean, rstd), the statistics [...] fp32 that sw_layer_norm_backward takes."""
+    if out is None and stream is None:
+        y = binding._native(binding._LAYER_NORM, x, weight, bias, eps, stats)
+        if y is not None:
+            return _done(y, "sw_layer_norm")
     import torch
 
     code = _type(x, "x")
@@ -95,6 +102,10 @@ def sw_layer_norm(x, weight=None, bias=None, eps: float = 1e-5, stats: bool = Fa
 def sw_layer_norm_backward(dy, x, weight, mean, rstd, params: bool = True, out=None, stream=None):
     """Gradients of sw_layer_norm: dy and x [..., C], weight [C] fp32 or None, mean and rstd [...] as the forward call returned
     them -> (dx, dweight, dbias), dx as x (`out` where given), dweight and dbias [C] fp32, or None with `params` False."""
+    if out is None and stream is None:
+        y = binding._native(binding._LAYER_NORM_BACKWARD, dy, x, weight, mean, rstd, params)
+        if y is not None:
+            return _done(y, "sw_layer_norm_backward")
     import torch
 
     code = _type(x, "x")
@@ -172,6 +183,10 @@ def sw_linear_attention(q, k, v, log_decay, scale=None, starts=None, state=None,
     Packed sequences of different lengths: starts [B+1] int32, and q, k, v, o without the first dimension.
     state [n,heads,dk,dv] fp32: what the sequences start from (None: zeros); final_state, as state: where their last states are
     written (may be `state`; None: not kept); slots [B] int32: the sequences' entries of both (None: in order)."""
+    if out is None and stream is None:
+        y = binding._native(binding._ATTENTION, q, k, v, log_decay, scale, starts, state, slots, final_state)
+        if y is not None:
+            return _done(y, "sw_linear_attention")
     import torch
 
     dims, front, g, s, at = _attention(q, k, v, log_decay, scale, starts, slots, "sw_linear_attention")
@@ -199,6 +214,10 @@ def sw_linear_attention_backward(do, q, k, v, log_decay, scale=None, starts=None
     """Gradients of sw_linear_attention, from do (as o) and, where the final states went on, d_final_state [B,heads,dk,dv] fp32
     -> (dq, dk, dv) as q, k, v (`out`: the three to write into); d_state [B,heads,dk,dv] fp32 is filled where given (it may be
     d_final_state).  The other arguments are the forward call's."""
+    if out is None and stream is None:
+        y = binding._native(binding._ATTENTION_BACKWARD, do, q, k, v, log_decay, scale, starts, state, slots, d_final_state, d_state)
+        if y is not None:
+            return _done(y, "sw_linear_attention_backward")
     import torch
 
     dims, front, g, s, at = _attention(q, k, v, log_decay, scale, starts, slots, "sw_linear_attention_backward")
@@ -226,6 +245,10 @@ def sw_linear_attention_step(q, k, v, log_decay, state, slots=None, scale=None, 
     """One token of each of B requests on a cache of states, brought up to date in place: q [B,heads,dk], k [B,kv_heads,dk],
     v [B,kv_heads,dv], state [n,heads,dk,dv] fp32, slots [B] int32 (None: in order) -> o [B,heads,dv].  A row whose slot is
     out of range (-1: unused) gets zeros and touches no state."""
+    if out is None and stream is None:
+        y = binding._native(binding._ATTENTION_STEP, q, k, v, log_decay, scale, state, slots)
+        if y is not None:
+            return _done(y, "sw_linear_attention_step")
     import torch
 
     if q.dim() != 3 or k.dim() != 3 or v.dim() != 3:
