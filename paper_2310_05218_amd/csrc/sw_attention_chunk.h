@@ -187,10 +187,18 @@ struct Staged {
         int row = thread / NCH;
         if (ALL < THREADS) row %= CH;
         const unsigned col = c < width ? c : 0;
+        if (from == 0) {
+            // (one distance for all of a thread's rows: what they are apart is the same for all threads)
+            const unsigned own = (place(row, reverse, step) + col) * (unsigned)sizeof(T);
+            const int64_t apart = (int64_t)STEP * (int)sizeof(T) * (reverse ? -(int64_t)step : (int64_t)step);
+            const char* at = reinterpret_cast<const char*>(tile);
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = reinterpret_cast<const typename R::loose*>(at + k * apart + own)->v;
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            int r = row + k * STEP;
-            if (from > 0) r = r < from ? from : r;
+            const int r = row + k * STEP < from ? from : row + k * STEP;
             v[k] = reinterpret_cast<const typename R::loose*>(reinterpret_cast<const char*>(tile) + (place(r, reverse, step) + col) * (unsigned)sizeof(T))->v;
         }
     }
@@ -470,29 +478,31 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     };
     Staged<EK, DAP, THREADS> sa, sb;
     Staged<EK, WC, THREADS> sc;
-    // the first of a chunk's rows that is a token, and the token that row 0 would be
+    // the first of a chunk's rows that is a token
     auto from_of = [&](int64_t t) { return at.last - t < CH ? CH - (int)(at.last - t) : 0; };
-    // the lowest of a chunk's 64 rows in memory
-    auto tile_of = [&](const AttentionOperand& o, int64_t t) { return row_of(o, t - from_of(t) + (s.reverse ? CH - 1 : 0)); };
-    auto fetch = [&](int64_t t) {
-        const int from = from_of(t);
-        if constexpr (OUTPUT) sa.fetch(static_cast<const T*>(s.a.p) + tile_of(s.a, t), (unsigned)s.a.token, s.reverse, from, s.DA);
-        sb.fetch(static_cast<const T*>(s.b.p) + tile_of(s.b, t), (unsigned)s.b.token, s.reverse, from, s.DA);
-        sc.fetch(static_cast<const T*>(s.c.p) + tile_of(s.c, t) + col0, (unsigned)s.c.token, s.reverse, from, width);
-    };
-    auto put = [&](int64_t t) {
-        const int from = from_of(t);
-        __syncthreads();
-        if constexpr (OUTPUT) sa.put(ta, static_cast<const T*>(s.a.p) + tile_of(s.a, t), (unsigned)s.a.token, s.reverse, from, s.DA);
-        sb.put(tb, static_cast<const T*>(s.b.p) + tile_of(s.b, t), (unsigned)s.b.token, s.reverse, from, s.DA);
-        sc.put(tc, static_cast<const T*>(s.c.p) + tile_of(s.c, t) + col0, (unsigned)s.c.token, s.reverse, from, width);
-        __syncthreads();
-    };
+    // Where a chunk's tiles begin in memory, at the lowest of their rows: the first chunk's, moved on by `dir` CH rows with each chunk.
+    auto begins = [&](const AttentionOperand& o) { return row_of(o, at.first + (s.reverse ? CH - 1 : 0)); };
+    const T *pa = OUTPUT ? static_cast<const T*>(s.a.p) + begins(s.a) : nullptr, *pb = static_cast<const T*>(s.b.p) + begins(s.b),
+            *pc = static_cast<const T*>(s.c.p) + begins(s.c) + col0;
+    const int ys = s.y_f32 ? 4 : ES;
+    char* py = OUTPUT ? static_cast<char*>(const_cast<void*>(s.y.p)) + (begins(s.y) + col0 + wave * 16 * CT) * ys : nullptr;
     bool bad = false;
     for (int64_t t = at.first; t < at.last; t += CH) {
         const int from = from_of(t);
-        fetch(t);
-        put(t);
+        {
+            // (a chunk of fewer rows: `from` of its tile's are before its first token)
+            const int64_t back = dir * from;
+            const T *xa = pa - back * s.a.token, *xb = pb - back * s.b.token, *xc = pc - back * s.c.token;
+            if constexpr (OUTPUT) sa.fetch(xa, (unsigned)s.a.token, s.reverse, from, s.DA);
+            sb.fetch(xb, (unsigned)s.b.token, s.reverse, from, s.DA);
+            sc.fetch(xc, (unsigned)s.c.token, s.reverse, from, width);
+            __syncthreads();
+            if constexpr (OUTPUT) sa.put(ta, xa, (unsigned)s.a.token, s.reverse, from, s.DA);
+            sb.put(tb, xb, (unsigned)s.b.token, s.reverse, from, s.DA);
+            sc.put(tc, xc, (unsigned)s.c.token, s.reverse, from, width);
+            __syncthreads();
+            pa += dir * CH * s.a.token, pb += dir * CH * s.b.token, pc += dir * CH * s.c.token;
+        }
         // c: columns a lane, eight tokens each
         V cv[2][CT];
 #pragma unroll
@@ -568,22 +578,32 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                 }
             }
             bad |= any_nonfinite(O);
-            const int64_t to = tile_of(s.y, t) + col0 + wave * 16 * CT;
             const int now = renewed(lane);
+            auto place = [&](int row) { return (unsigned)((s.reverse ? CH - 1 - row : row) * (unsigned)s.y.token + 4 * (now / 16)) * (unsigned)ys; };
+            auto put_all = [&](auto* as) {
+                typedef std::remove_pointer_t<decltype(as)> Y;
+                if (from == 0 && width - wave * 16 * CT >= 16 * CT) {
+                    const unsigned mine = place(now % 16);
+                    const int64_t apart = dir * 16 * (int)sizeof(Y) * s.y.token;
 #pragma unroll
-            for (int i = 0; i < TI; ++i) {
-                const int row = 16 * i + now % 16;
-                if (row < from) continue;
+                    for (int i = 0; i < TI; ++i)
 #pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    const int first = 16 * c + 4 * (now / 16), left = width - wave * 16 * CT - first;
-                    const unsigned place = (s.reverse ? CH - 1 - row : row) * (unsigned)s.y.token + first;
-                    if (s.y_f32)
-                        store_four(reinterpret_cast<float*>(reinterpret_cast<char*>(const_cast<float*>(static_cast<const float*>(s.y.p)) + to) + place * 4u), O[i][c], left);
-                    else
-                        store_four(reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<T*>(static_cast<const T*>(s.y.p)) + to) + place * (unsigned)sizeof(T)), O[i][c], left);
+                        for (int c = 0; c < CT; ++c) store_four(reinterpret_cast<Y*>(py + i * apart + mine) + 16 * c, O[i][c], 4);
+                    return;
                 }
-            }
+                char* to = py - dir * from * s.y.token * (int)sizeof(Y);
+#pragma unroll
+                for (int i = 0; i < TI; ++i)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+                        if (16 * i + now % 16 >= from)
+                            store_four(reinterpret_cast<Y*>(to + place(16 * i + now % 16)) + 16 * c, O[i][c], width - wave * 16 * CT - 4 * (now / 16) - 16 * c);
+            };
+            if (s.y_f32)
+                put_all(static_cast<float*>(nullptr));
+            else
+                put_all(static_cast<T*>(nullptr));
+            py += dir * CH * s.y.token * ys;
         }
         add_products<EK, MT, CT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
     }
