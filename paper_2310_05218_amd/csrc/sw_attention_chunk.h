@@ -12,7 +12,8 @@
 // values (17 bits; half, whose range they may leave, meets c as two bf16 values too).  The state: one value of the format, in half scaled
 // by a power of two; its rounding is y's own, on the part of y that comes from before the chunk (y's error against 64 bits at most 1.4 times
 // what its last rounding gives; with two values 10 % more time).  The state's new terms: three bf16 or two scaled half values, 22 bits and
-// more, as the state is an fp32 result.  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
+// more, as the state is an fp32 result; two bf16 values, 16 bits, where it is none and only later rows of the segment come from it, as operand
+// of 8 bits.  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
 #pragma once
 
 #include "sw_attention.h"
@@ -67,9 +68,10 @@ __device__ __forceinline__ f32x8 widened(V v)
     return f;
 }
 
-// v as a sum of N values of a format: v rounded, the rest rounded, ...  (In pairs: converted one by one the compiler converts each twice.)
+// v as a sum of N values of a format: v rounded, the rest rounded, ...; what is left.  (In pairs: converted one by one the compiler converts
+// each twice.)
 template <class V, int N>
-__device__ __forceinline__ void parts(f32x8 v, V (&p)[N])
+__device__ __forceinline__ f32x8 parts(f32x8 v, V (&p)[N])
 {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -77,12 +79,11 @@ __device__ __forceinline__ void parts(f32x8 v, V (&p)[N])
 #pragma unroll
         for (int j = 0; j < 4; ++j) u[j] = pack<V>(v[2 * j], v[2 * j + 1]);
         p[k] = __builtin_bit_cast(V, u);
-        if (k + 1 < N) {
-            const f32x8 w = widened<V>(p[k]);
+        const f32x8 w = widened<V>(p[k]);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] -= w[j];
-        }
+        for (int j = 0; j < 8; ++j) v[j] -= w[j];
     }
+    return v;
 }
 
 template <int EK>
@@ -90,12 +91,12 @@ struct Operand;
 template <>
 struct Operand<kElemBF16> {
     typedef bf16x8 vec;
-    static constexpr int kState = 1, kTerm = 3;
+    static constexpr int kState = 1, kTerm = 3, kPassing = 2;
 };
 template <>
 struct Operand<kElemF16> {
     typedef f16x8 vec;
-    static constexpr int kState = 1, kTerm = 2;
+    static constexpr int kState = 1, kTerm = 2, kPassing = 2;
 };
 // fp32: K is 4, a value a lane; a vector holds the operands of four instructions, K in the order 4 (lane / 16) + element.
 template <>
@@ -310,10 +311,10 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
 }
 
 // S <- whole S + sum over the chunk's tokens of b times weighted c (an operand vector's tokens: weights in `tables`, those of
-// the first vector times shift).
-template <int EK, int MT, int CT>
+// the first vector times shift).  FIRST parts of the weighted c, and the others where `all`.
+template <int EK, int MT, int CT, int FIRST>
 __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[CT], float whole, const typename Operand<EK>::vec (&cv)[2][CT],
-                                             const float* tables, float shift, const unsigned char* b)
+                                             const float* tables, float shift, const unsigned char* b, bool all)
 {
     typedef typename Operand<EK>::vec V;
     const f32x4 tail[2] = {*reinterpret_cast<const f32x4*>(tables), *reinterpret_cast<const f32x4*>(tables + 256)};
@@ -363,18 +364,33 @@ __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            V p[CT][Operand<EK>::kTerm];
+            V p[CT][FIRST];
+            f32x8 rest[CT];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 f32x8 w = weighted(k, c);
                 if (EK == kElemF16) w *= in[c];
-                parts(w, p[c]);
+                rest[c] = parts(w, p[c]);
+            }
+            constexpr int MORE = Operand<EK>::kTerm - FIRST;
+            if (MORE && all) {
+                V r[CT][MORE ? MORE : 1];
+#pragma unroll
+                for (int c = 0; c < CT; ++c) parts(rest[c], r[c]);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const V x = turned<EK, 16 * MT>(b, 16 * m, 32 * k);
+#pragma unroll
+                    for (int q = MORE; q-- > 0;)
+#pragma unroll
+                        for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, r[c][q], S[m][c]);
+                }
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const V x = turned<EK, 16 * MT>(b, 16 * m, 32 * k);
 #pragma unroll
-                for (int q = Operand<EK>::kTerm; q-- > 0;)
+                for (int q = FIRST; q-- > 0;)
 #pragma unroll
                     for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, p[c][q], S[m][c]);
             }
@@ -397,6 +413,15 @@ template <int EK, int DAP, int WC, bool OUTPUT>
 constexpr int chunk_lds_bytes()
 {
     return chunk_of(EK) * ((OUTPUT ? 2 : 1) * pitch_of<EK>(DAP) + pitch_of<EK>(WC)) + (OUTPUT ? pair_parts<EK>() * pair_bytes<EK>() : 0) + kTables;
+}
+
+template <int EK, bool OUTPUT>
+constexpr int first_parts()
+{
+    if constexpr (EK == kElemF32)
+        return 0;
+    else
+        return OUTPUT ? Operand<EK>::kPassing : Operand<EK>::kTerm;
 }
 
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
@@ -487,6 +512,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     const int ys = s.y_f32 ? 4 : ES;
     char* py = OUTPUT ? static_cast<char*>(const_cast<void*>(s.y.p)) + (begins(s.y) + col0 + wave * 16 * CT) * ys : nullptr;
     bool bad = false;
+    const bool kept = at.ends && s.ends;            // (the state is a result, not only an operand of the rows to come; y is the same, asked for or not)
     for (int64_t t = at.first; t < at.last; t += CH) {
         const int from = from_of(t);
         {
@@ -605,7 +631,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                 put_all(static_cast<T*>(nullptr));
             py += dir * CH * s.y.token * ys;
         }
-        add_products<EK, MT, CT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
+        add_products<EK, MT, CT, first_parts<EK, OUTPUT>()>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b, kept);
     }
 #pragma unroll
     for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] *= frame[i % CT];
