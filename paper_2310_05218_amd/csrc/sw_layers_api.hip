@@ -84,8 +84,6 @@ int check_dims(const sw_linear_attention_dims& d)
         return SW_ERR_SHAPE;
     if (d.T > kMaxExtent / d.B || (int64_t)d.B + 2 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.dk > kMaxHead || d.dv > kMaxHead || d.heads > 65535) return SW_ERR_UNSUPPORTED;
-    // (a place for every 128 tokens and two a sequence, every head one, three sums: workgroups of a launch)
-    if ((d.T / 128 * d.B + 2 * ((int64_t)d.B + 2)) * d.heads * 3 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.type != SW_F32 && d.type != SW_BF16 && d.type != SW_F16) return SW_ERR_UNSUPPORTED;
     return SW_OK;
 }
@@ -96,6 +94,13 @@ bool packed_too_long(const sw_linear_attention_dims& d, const int32_t* starts) {
 AttentionSegments segments_of(const sw_linear_attention_dims& d, bool packed)
 {
     return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed);
+}
+
+// The same of calls that work on `sums` at a time: a launch has fewer than 2^32 threads, 256 for every segment's place, head and sum.
+int check_sums(const sw_linear_attention_dims& d, bool packed, int sums)
+{
+    if (const int rc = check_dims(d)) return rc;
+    return segments_of(d, packed).count > ((1 << 24) - 1) / ((int64_t)d.heads * sums) ? SW_ERR_SHAPE : SW_OK;
 }
 
 // Whether the chunk kernels' 32-bit distances within a chunk reach its rows; tensors that lie further apart go token by token.
@@ -185,7 +190,7 @@ int sw_layer_norm_backward(const void* dy, const void* x, const float* weight, c
 
 int64_t sw_linear_attention_workspace_bytes(const sw_linear_attention_dims* dims, int packed)
 {
-    if (!dims || check_dims(*dims) != SW_OK) return 0;
+    if (!dims || check_sums(*dims, packed != 0, 1) != SW_OK) return 0;
     return state_bytes(*dims, packed != 0);
 }
 
@@ -196,7 +201,7 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
 {
     if (!q || !k || !v || !o || !log_decay || !dims || !q_strides || !k_strides || !v_strides || !o_strides) return SW_ERR_NULL;
     const sw_linear_attention_dims d = *dims;
-    if (const int rc = check_dims(d)) return rc;
+    if (const int rc = check_sums(d, starts != nullptr, 1)) return rc;
     const int64_t batches = starts ? 1 : d.B;
     const int share = d.heads / d.kv_heads;
     Tensor4 tq, tk, tv, to;
@@ -238,7 +243,7 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
 
 int64_t sw_linear_attention_backward_workspace_bytes(const sw_linear_attention_dims* dims, int packed)
 {
-    if (!dims || check_dims(*dims) != SW_OK) return 0;
+    if (!dims || check_sums(*dims, packed != 0, 3) != SW_OK) return 0;
     return fold_bytes(*dims, packed != 0, dims->dk) + fold_bytes(*dims, packed != 0, dims->dv) + 2 * state_bytes(*dims, packed != 0);
 }
 
@@ -253,7 +258,7 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
         !dq_strides || !dk_strides || !dv_strides)
         return SW_ERR_NULL;
     const sw_linear_attention_dims d = *dims;
-    if (const int rc = check_dims(d)) return rc;
+    if (const int rc = check_sums(d, starts != nullptr, 3)) return rc;
     const int64_t batches = starts ? 1 : d.B;
     const int share = d.heads / d.kv_heads;
     Tensor4 tdo, tq, tk, tv, tdq, tdk, tdv;
@@ -330,7 +335,7 @@ int sw_linear_attention_step(const void* q, const void* k, const void* v, void* 
     if (const int rc = check_dims(d)) return rc;
     const int share = d.heads / d.kv_heads;
     Tensor4 tq, tk, tv, to;
-    if (d.T != 1 || !tq.set(q, q_strides, d.B, 1, d.heads, d.dk, 1) || !tk.set(k, k_strides, d.B, 1, d.kv_heads, d.dk, share) ||
+    if (d.T != 1 || d.B >= 1 << 24 || !tq.set(q, q_strides, d.B, 1, d.heads, d.dk, 1) || !tk.set(k, k_strides, d.B, 1, d.kv_heads, d.dk, share) ||
         !tv.set(v, v_strides, d.B, 1, d.kv_heads, d.dv, share) || !to.set(o, o_strides, d.B, 1, d.heads, d.dv, 1, true) || d.n_states <= 0 ||
         (!slots && d.n_states < d.B))
         return SW_ERR_SHAPE;

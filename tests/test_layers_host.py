@@ -100,6 +100,22 @@ def test_attention_refusals(L):
     assert L.sw_linear_attention_workspace_bytes(dims(T=0), 0) == 0
 
 
+def test_attention_sizes_of_a_launch(L):
+    """Packed rows count once, not once a sequence; what no launch has threads for is refused, workspace and call alike."""
+    many = dims(T=1 << 23, B=1000, heads=16, kv_heads=16, dk=64, dv=64, n_states=0)
+    state = 16 * 64 * 64 * 4
+    assert 1000 * state <= L.sw_linear_attention_workspace_bytes(many, 1) <= 2000 * state
+    assert L.sw_linear_attention_backward_workspace_bytes(many, 1) == 2 * L.sw_linear_attention_workspace_bytes(many, 1)
+    most = dims(T=64, B=(1 << 24) // 96, heads=32, kv_heads=16, n_states=0)         # 2^24 / 3 heads of sequences
+    assert L.sw_linear_attention_backward_workspace_bytes(most, 0) > 0
+    more = dims(T=64, B=(1 << 24) // 96 + 1, heads=32, kv_heads=16, n_states=0)
+    assert L.sw_linear_attention_backward_workspace_bytes(more, 0) == 0
+    s = B.SwStrides(64 * 32 * 16, 32 * 16, 16), B.SwStrides(64 * 16 * 16, 16 * 16, 16), B.SwStrides(64 * 16 * 32, 16 * 32, 32), B.SwStrides(64 * 32 * 32, 32 * 32, 32)
+    T = 1 << 44
+    call = lambda d: L.sw_linear_attention_backward(T, 2 * T, 3 * T, 4 * T, X, None, None, 5 * T, 6 * T, 7 * T, None, None, None, d, s[3], *s[:3], *s[:3], None, 0, None)
+    assert call(more) == B.SW_ERR_SHAPE and call(most) == B.SW_ERR_WORKSPACE
+
+
 def test_attention_backward_refusals(L):
     sq, sk, sv, so = strides(10, 4, 16), strides(10, 2, 16), strides(10, 2, 32), strides(10, 4, 32)
     need = L.sw_linear_attention_backward_workspace_bytes(dims(), 0)
