@@ -393,3 +393,18 @@ def test_refusals(sw):
                  lambda: A(q[0], q[0], q[0], g, starts=i32(0)), lambda: A(q, q, q, g, scale=math.inf), lambda: Bk(q, q, q, q, g, out=(q, q, q))):
         with pytest.raises(sw.SwError):
             call()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("B,T,H,Hk,dk,dv", [(13, 70, 20, 20, 72, 100), (13, 33, 20, 10, 24, 128), (9, 65, 32, 8, 130, 70), (5, 20, 52, 52, 200, 130), (1, 1300, 32, 32, 16, 80),
+                                            (2, 700, 30, 30, 80, 72)])
+def test_many_heads_of_wide_values(sw, B, T, H, Hk, dk, dv, t):
+    """Launches that fill the chip, on values (and keys) of more than 64 columns."""
+    c = Case(t, B, T, H, Hk, dk, dv, seed=B + T)
+    check(sw, c)
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_many_packed_heads_of_wide_values(sw, t):
+    starts = [0, 0, 1, 130, 700, 701, 1000, 1490]
+    check(sw, Case(t, len(starts) - 1, 1500, 30, 30, 24, 96, starts=starts, seed=7))
