@@ -659,21 +659,29 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     }
 }
 
-// The sums of one size in one launch.
+// The sums of one size in one launch; all of them where that does not fill the chip.
 template <int EK, bool OUTPUT>
 hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
     auto padded = [](int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; };
     auto columns = [](int d) { return d <= 64 ? 0 : (d + 127) / 128; };
+    // At most two workgroups of 64 columns a CU: in one launch, with as many rows of the state as the most of them have (gradients of 500 tokens
+    // on 8 heads of 64 x 128 bf16, us: 36.6 in two launches, 27.4 in one).  States of 256 rows have no room for two on a CU.
+    int most_rows = 0, most_columns = 0;
+    for (int i = 0; i < all.count; ++i) {
+        most_rows = padded(all.of[i].DA) > most_rows ? padded(all.of[i].DA) : most_rows;
+        most_columns = all.of[i].DC > most_columns ? all.of[i].DC : most_columns;
+    }
+    const bool together = most_rows <= 128 && g.count * n.H * all.count * ((most_columns + 63) / 64) <= 512;
     bool done[3] = {false, false, false};
     for (int i = 0; i < all.count; ++i) {
         if (done[i]) continue;
         AttentionSums s;
         s.count = 0;
-        const int da = padded(all.of[i].DA);
+        const int da = together ? most_rows : padded(all.of[i].DA);
         int dc = all.of[i].DC;                  // the most columns of them
         for (int j = i; j < all.count; ++j)
-            if (!done[j] && padded(all.of[j].DA) == da && columns(all.of[j].DC) == columns(dc)) {
+            if (!done[j] && (together || (padded(all.of[j].DA) == da && columns(all.of[j].DC) == columns(dc)))) {
                 s.of[s.count++] = all.of[j], done[j] = true;
                 dc = all.of[j].DC > dc ? all.of[j].DC : dc;
             }
@@ -695,9 +703,9 @@ hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const
             default: return with(std::integral_constant<int, 256>(), ct);
             }
         };
-// Wavefronts of 16 columns where workgroups of 128 columns would be fewer than the CUs: twice as many, each through in less time (128
+        // Wavefronts of 16 columns where workgroups of 128 columns would be no more than the CUs: twice as many, each through in less time (128
         // tokens, us with 32 and with 16 columns: 8 heads of 128 bf16 17.9 and 13.4, 192 heads 21.4 and 18.6, 288 heads 24.8 and 30.1).
-        const bool few = g.count * n.H * s.count * ((dc + 127) / 128) < 256;
+        const bool few = g.count * n.H * s.count * ((dc + 127) / 128) <= 256;
         const hipError_t e = dc <= 64 || few ? rows(std::integral_constant<int, 1>()) : rows(std::integral_constant<int, 2>());
         if (e != hipSuccess) return e;
     }

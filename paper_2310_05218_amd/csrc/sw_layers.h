@@ -169,7 +169,7 @@ struct AttentionSegments {
     int64_t length, count;              // count: places for segments in all
 };
 constexpr int kAttentionChunk = 64;
-AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed);
+AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed, int ek);
 // a segment's own sum for all but the last of a sequence, into `states`
 hipError_t launch_attention_states(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
 // ... from which the state before each segment of a sequence that has several

@@ -93,7 +93,7 @@ bool packed_too_long(const sw_linear_attention_dims& d, const int32_t* starts) {
 
 AttentionSegments segments_of(const sw_linear_attention_dims& d, bool packed)
 {
-    return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed);
+    return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed, d.type);
 }
 
 // The same of calls that work on `sums` at a time: a launch has fewer than 2^32 threads, 256 for every segment's place, head and sum.

@@ -243,15 +243,23 @@ SW_ATTENTION_UNITS(states)
 SW_ATTENTION_UNITS(chunks)
 #undef SW_ATTENTION_UNITS
 
-AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed)
+// Sequences are cut where there are fewer heads than `want` workgroups, and where that gains more than the two launches that it takes. us:
+// - equal ones of up to four chunks stay whole (256 tokens bf16, 8 x 16 heads of 64: 18.2 whole, 28.5 cut; 200 tokens fp32, gradients, 8 heads of
+//   64: 24.5 and 22.9); so do packed ones that are short in the mean and 512 tokens together, which bounds what the longest of them takes (8 of
+//   500 tokens bf16, 8 heads of 64: 15.0 and 23.1).
+// - segments of one chunk of 64 while those of two would be fewer than 192 workgroups (1000 tokens fp32, 8 heads of 64: 25.4, with two 32.8; where
+//   they would be 256, the states cost more: 2 x 1000 tokens half on 16 heads of 128 51 and 42), but for packed ones that are that short.
+AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed, int ek)
 {
-    const int64_t rows = packed ? n.T : n.T * n.B, columns = (DC + 127) / 128;
+    const int64_t rows = packed ? n.T : n.T * n.B, columns = (DC + 127) / 128, two = 2 * kAttentionChunk;
     AttentionSegments g{(int64_t)1 << 62, 0};
     const int64_t want = 512;          // workgroups
-    if ((packed ? 1 : n.B) * n.H * columns < want) {
-        const int64_t length = (rows * n.H * columns + want - 1) / want;
-        const int64_t chunks = (length + kAttentionChunk - 1) / kAttentionChunk;
-        if (chunks * kAttentionChunk < n.T) g.length = (chunks < 2 ? 2 : chunks) * kAttentionChunk;
+    const bool brief = packed && n.T / n.B <= two;
+    const bool whole = packed ? brief && n.T <= 4 * two : n.T <= (ek == kElemF32 ? two : 2 * two);
+    if (!whole && (packed ? 1 : n.B) * n.H * columns < want) {
+        const int64_t chunks = ((rows * n.H * columns + want - 1) / want + kAttentionChunk - 1) / kAttentionChunk;
+        const int64_t least = !brief && rows * n.H * columns < 192 * two ? 1 : 2;
+        g.length = (chunks < least ? least : chunks) * kAttentionChunk;
     }
     if (g.length >= n.T) g.length = (int64_t)1 << 62;
     g.count = packed ? n.T / g.length + n.B + 2 : n.B * ((n.T + g.length - 1) / g.length);
