@@ -95,6 +95,11 @@ struct Row {
         for (int e = 0; e < VEC; ++e) f[e] = first + e < C ? f[e] : 0.f;
         return f;
     }
+    // VEC elements, all there
+    static __device__ __forceinline__ vec load(const T* p) { return reinterpret_cast<const loose*>(p)->v; }
+    static __device__ __forceinline__ void store(T* p, floats f) { reinterpret_cast<loose*>(p)->v = __builtin_convertvector(f, vec); }
+    static __device__ __forceinline__ floats load_floats(const float* p) { return reinterpret_cast<const loose_floats*>(p)->v; }
+    static __device__ __forceinline__ void store_floats(float* p, floats f) { reinterpret_cast<loose_floats*>(p)->v = f; }
     static __device__ __forceinline__ float sum(floats f)
     {
         float s = 0.f;
