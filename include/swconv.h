@@ -456,8 +456,9 @@ int64_t sw_layer_norm_backward_workspace_bytes(int64_t rows, int64_t C);     /* 
  * state, final_state: [n_states, heads, dk, dv] fp32 or NULL, contiguous; sequence b has entry slots[b] of both, or
  * entry b where slots is NULL (n_states >= B then, else SW_ERR_SHAPE).  slots: [B] int32 (device), no entry twice; a
  * sequence with an entry outside 0 ... n_states-1 starts from zero and its final state is not kept.  final_state
- * may be state.  Extents: 1 <= dk, dv <= 256 (SW_ERR_UNSUPPORTED beyond); all tensors aligned to their elements,
- * `o` overlapping no input.
+ * may be state.  Extents: 1 <= dk, dv <= 256, heads <= 65535 (SW_ERR_UNSUPPORTED beyond); B * heads below 2^24, in the
+ * backward pass a third of that (SW_ERR_SHAPE beyond: a launch's threads); all tensors aligned to their elements, `o`
+ * overlapping no input.
  */
 typedef struct {
     int64_t batch, token, head;         /* elements from one to the next */
