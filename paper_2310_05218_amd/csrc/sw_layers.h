@@ -182,8 +182,13 @@ hipError_t launch_attention_scan(const AttentionSums& s, const AttentionBatch& n
 // the outputs and last states
 hipError_t launch_attention_chunks(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, int ek, hipStream_t st);
 hipError_t launch_attention_recurrent(const AttentionSum& s, const AttentionBatch& n, int ek, hipStream_t st);
-// y[row, u] = sum over the heads of group u of part[row, head], rows of D fp32 each, rounded to the format
-hipError_t launch_attention_fold(const float* part, const AttentionOperand& y, const AttentionBatch& n, int kv_heads, int D, int ek, hipStream_t st);
+// y[row, u] = sum over the heads of group u of part[row, head], rows of D fp32 each (16-byte aligned), rounded to the format
+struct AttentionFold {
+    const float* part;
+    AttentionOperand y;
+    int D;
+};
+hipError_t launch_attention_fold(const AttentionFold& dk, const AttentionFold& dv, const AttentionBatch& n, int ek, hipStream_t st);
 
 struct AttentionStepArgs {
     AttentionOperand q, k, v, o;

@@ -321,8 +321,7 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     } else {
         for (int i = 0; i < 3 && e == hipSuccess; ++i) e = launch_attention_recurrent(gradients.of[i], n, d.type, st);
     }
-    if (e == hipSuccess && share > 1) e = launch_attention_fold(part_k, tdk.op, n, d.kv_heads, d.dk, d.type, st);
-    if (e == hipSuccess && share > 1) e = launch_attention_fold(part_v, tdv.op, n, d.kv_heads, d.dv, d.type, st);
+    if (e == hipSuccess && share > 1) e = launch_attention_fold(AttentionFold{part_k, tdk.op, d.dk}, AttentionFold{part_v, tdv.op, d.dv}, n, d.type, st);
     return launch_status(e);
 }
 
