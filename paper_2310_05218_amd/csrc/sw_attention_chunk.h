@@ -14,6 +14,9 @@
 // times that; 8192 tokens on 16 heads of 128 bf16 took 88 us for 89, gradients of 4 x 4096 tokens 305 for 316).  The state's new terms: three
 // bf16 or two scaled half values, 22 bits and more, as the state is an fp32 result; two bf16 values, 16 bits, where it is none and only later rows of
 // the segment come from it, as operand of as many.  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
+//
+// 8192 tokens on 16 heads of 128 bf16: 88 us, of which 60 without any of the products (335 MB at 5.6 TB/s: the operands, those of the segments' own sums
+// once more, and 134 MB of states); the rest are a chunk's phases, one after another in a workgroup, with two of these on a CU (74 KB of LDS each).
 #pragma once
 
 #include "sw_attention.h"

@@ -4,7 +4,7 @@
 // fewest lanes that hold it in a few vectors each: 8, 16 or 32 lanes (several rows a wavefront), a wavefront, 256 to 1024 threads.
 // Workgroups walk over rows a grid apart: a thread's columns never change, so weight and bias stay in its registers (they are 4 bytes an
 // element, twice a 16-bit row), and the next row is on its way while this one is folded.  Rows of more than 2048 vectors are read again from
-// memory instead.
+// memory instead.  16384 rows of 4096 bf16: 52 us forwards (5.2 TB/s), 80 backwards (5.0).
 //
 // Loads are 16 bytes at any element's address.  The lane at the end of a row that is no whole number of vectors has the row's last vector, whose
 // first elements are another's too: it leaves them out of its sums and stores what the other stores.  (With single elements in their place the
