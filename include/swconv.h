@@ -459,6 +459,8 @@ int64_t sw_layer_norm_backward_workspace_bytes(int64_t rows, int64_t C);     /* 
  * may be state.  Extents: 1 <= dk, dv <= 256, heads <= 65535 (SW_ERR_UNSUPPORTED beyond); B * heads below 2^24, in the
  * backward pass a third of that (SW_ERR_SHAPE beyond: a launch's threads); all tensors aligned to their elements, `o`
  * overlapping no input.
+ * What a matrix product takes of values computed on the way (products of q and k, states, their new terms) has 24 bits or
+ * more; with half tensors the states and their new terms have 22, of the largest value in their column.
  */
 typedef struct {
     int64_t batch, token, head;         /* elements from one to the next */

@@ -8,15 +8,14 @@
 // the operand of S^T a, with a's values picked in that order.  Outputs are computed transposed (rows: columns of y), so that a lane holds
 // four neighbouring columns of one token.  Pair products are shared: each 16 x 16 tile is computed by one wavefront and handed round in LDS.
 //
-// Operands derived in fp32 enter a product as sums of 16-bit values, and which sums is a choice of precision.  Pair products: two bf16
-// values (17 bits; half, whose range they may leave, meets c as two bf16 values too).  The state: two values of the format, in half scaled
-// by a power of two, so that y's error is that of its last rounding (with one value, y's own rounding twice, y's error against 64 bits was 1.25
-// times that; 8192 tokens on 16 heads of 128 bf16 took 88 us for 89, gradients of 4 x 4096 tokens 305 for 316).  The state's new terms: three
-// bf16 or two scaled half values, 22 bits and more, as the state is an fp32 result; two bf16 values, 16 bits, where it is none and only later rows of
-// the segment come from it, as operand of as many.  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
+// Operands derived in fp32 enter a product as sums of 16-bit values that hold fp32's bits: pair products, the state and its new terms are three
+// bf16 values each, 25 bits.  In half the state and its new terms are two values scaled by a power of two, 22 bits, and pair products, whose range
+// half may not have, are three bf16 values that meet c as two (which are all of it).  fp32 tensors stay fp32 throughout, on the fp32 matrix instructions.
+// So a result is what sums in 32 bits make it before its one rounding.  (With two bf16 values each, 17 bits, 8192 tokens on 16 heads of 128 bf16 took 88 us
+// for 94, gradients of 4 x 4096 tokens 318 for 359, and three times as many of their results were rounded the other way.)
 //
-// 8192 tokens on 16 heads of 128 bf16: 88 us, of which 60 without any of the products (335 MB at 5.6 TB/s: the operands, those of the segments' own sums
-// once more, and 134 MB of states); the rest are a chunk's phases, one after another in a workgroup, with two of these on a CU (74 KB of LDS each).
+// 8192 tokens on 16 heads of 128 bf16: 94 us, of which 60 without any of the products (335 MB at 5.6 TB/s: the operands, those of the segments' own sums
+// once more, and 134 MB of states); the rest are a chunk's phases, one after another in a workgroup, with two of these on a CU (76 KB of LDS each).
 #pragma once
 
 #include "sw_attention.h"
@@ -71,10 +70,9 @@ __device__ __forceinline__ f32x8 widened(V v)
     return f;
 }
 
-// v as a sum of N values of a format: v rounded, the rest rounded, ...; what is left.  (In pairs: converted one by one the compiler converts
-// each twice.)
+// v as a sum of N values of a format: v rounded, the rest rounded, ...  (In pairs: converted one by one the compiler converts each twice.)
 template <class V, int N>
-__device__ __forceinline__ f32x8 parts(f32x8 v, V (&p)[N])
+__device__ __forceinline__ void parts(f32x8 v, V (&p)[N])
 {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -86,7 +84,6 @@ __device__ __forceinline__ f32x8 parts(f32x8 v, V (&p)[N])
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] -= w[j];
     }
-    return v;
 }
 
 template <int EK>
@@ -94,12 +91,12 @@ struct Operand;
 template <>
 struct Operand<kElemBF16> {
     typedef bf16x8 vec;
-    static constexpr int kState = 2, kTerm = 3, kPassing = 2;
+    static constexpr int kState = 3, kTerm = 3;
 };
 template <>
 struct Operand<kElemF16> {
     typedef f16x8 vec;
-    static constexpr int kState = 2, kTerm = 2, kPassing = 2;
+    static constexpr int kState = 2, kTerm = 2;
 };
 // fp32: K is 4, a value a lane; a vector holds the operands of four instructions, K in the order 4 (lane / 16) + element.
 template <>
@@ -286,7 +283,7 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
     } else {
 #pragma unroll
         for (int m = 0; m < MT / 2; ++m) {
-            V x[TI], p[CT][Operand<EK>::kState];
+            V x[TI];
 #pragma unroll
             for (int i = 0; i < TI; ++i) {
                 const unsigned char* at = a + 16 * i * pitch_of<EK>(16 * MT) + 64 * m;
@@ -297,14 +294,13 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
                 f32x8 v;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = EK == kElemF16 ? S[2 * m + e / 4][c][e % 4] * in[c] : S[2 * m + e / 4][c][e % 4];
-                parts(v, p[c]);
+                V p[Operand<EK>::kState];
+                parts(v, p);
+#pragma unroll
+                for (int k = Operand<EK>::kState; k-- > 0;)
+#pragma unroll
+                    for (int i = 0; i < TI; ++i) O[i][c] = multiply(p[k], x[i], O[i][c]);
             }
-#pragma unroll
-            for (int k = Operand<EK>::kState; k-- > 0;)
-#pragma unroll
-                for (int i = 0; i < TI; ++i)
-#pragma unroll
-                    for (int c = 0; c < CT; ++c) O[i][c] = multiply(p[c][k], x[i], O[i][c]);
         }
     }
 #pragma unroll
@@ -314,10 +310,10 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
 }
 
 // S <- whole S + sum over the chunk's tokens of b times weighted c (an operand vector's tokens: weights in `tables`, those of
-// the first vector times shift).  FIRST parts of the weighted c, and the others where `all`.
-template <int EK, int MT, int CT, int FIRST>
+// the first vector times shift).
+template <int EK, int MT, int CT>
 __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[CT], float whole, const typename Operand<EK>::vec (&cv)[2][CT],
-                                             const float* tables, float shift, const unsigned char* b, bool all)
+                                             const float* tables, float shift, const unsigned char* b)
 {
     typedef typename Operand<EK>::vec V;
     const f32x4 tail[2] = {*reinterpret_cast<const f32x4*>(tables), *reinterpret_cast<const f32x4*>(tables + 256)};
@@ -367,33 +363,18 @@ __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            V p[CT][FIRST];
-            f32x8 rest[CT];
+            V p[CT][Operand<EK>::kTerm];
 #pragma unroll
             for (int c = 0; c < CT; ++c) {
                 f32x8 w = weighted(k, c);
                 if (EK == kElemF16) w *= in[c];
-                rest[c] = parts(w, p[c]);
-            }
-            constexpr int MORE = Operand<EK>::kTerm - FIRST;
-            if (MORE && all) {
-                V r[CT][MORE ? MORE : 1];
-#pragma unroll
-                for (int c = 0; c < CT; ++c) parts(rest[c], r[c]);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const V x = turned<EK, 16 * MT>(b, 16 * m, 32 * k);
-#pragma unroll
-                    for (int q = MORE; q-- > 0;)
-#pragma unroll
-                        for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, r[c][q], S[m][c]);
-                }
+                parts(w, p[c]);
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 const V x = turned<EK, 16 * MT>(b, 16 * m, 32 * k);
 #pragma unroll
-                for (int q = FIRST; q-- > 0;)
+                for (int q = Operand<EK>::kTerm; q-- > 0;)
 #pragma unroll
                     for (int c = 0; c < CT; ++c) S[m][c] = multiply(x, p[c][q], S[m][c]);
             }
@@ -403,28 +384,26 @@ __device__ __forceinline__ void add_products(f32x4 (&S)[MT][CT], float (&frame)[
 
 // ---- the kernel ---------------------------------------------------------------------------------------------------------------------
 
-// Pair products in LDS: row i, column j; two bf16 parts, or fp32.
+// Pair products in LDS: row i, column j, as three bf16 parts or as fp32.  16-bit rows are read in whole operand vectors of two tiles: those of the
+// first two tiles end where the first vector does.
+constexpr int kPairParts = 3;
 template <int EK>
-constexpr int pair_pitch() { return pitch_of<EK>(chunk_of(EK)); }
+constexpr int pair_pitch(int tile) { return EK != kElemF32 && tile < 2 ? pitch_of<EK>(chunk_of(EK) / 2) : pitch_of<EK>(chunk_of(EK)); }
 template <int EK>
-constexpr int pair_bytes() { return chunk_of(EK) * pair_pitch<EK>(); }      // of one part
+constexpr int pair_row(int tile)                                        // where the rows of a tile begin
+{
+    return EK != kElemF32 && tile >= 2 ? 32 * pair_pitch<EK>(0) + 16 * (tile - 2) * pair_pitch<EK>(2) : 16 * tile * pair_pitch<EK>(0);
+}
 template <int EK>
-constexpr int pair_parts() { return EK == kElemF32 ? 1 : 2; }
+constexpr int pair_bytes() { return pair_row<EK>(tiles_of(EK)); }           // of one part
+template <int EK>
+constexpr int pair_parts() { return EK == kElemF32 ? 1 : kPairParts; }
 constexpr int kTables = 64 * 16 * 4;                // bytes of the lanes' weights
 
 template <int EK, int DAP, int WC, bool OUTPUT>
 constexpr int chunk_lds_bytes()
 {
     return chunk_of(EK) * ((OUTPUT ? 2 : 1) * pitch_of<EK>(DAP) + pitch_of<EK>(WC)) + (OUTPUT ? pair_parts<EK>() * pair_bytes<EK>() : 0) + kTables;
-}
-
-template <int EK, bool OUTPUT>
-constexpr int first_parts()
-{
-    if constexpr (EK == kElemF32)
-        return 0;
-    else
-        return OUTPUT ? Operand<EK>::kPassing : Operand<EK>::kTerm;
 }
 
 __device__ __forceinline__ float uniform(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
@@ -437,7 +416,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
 {
     typedef typename ElemOf<EK>::type T;
     typedef typename Operand<EK>::vec V;
-    constexpr int CH = chunk_of(EK), TI = tiles_of(EK), ES = elem_size(EK), kPairPitch = pair_pitch<EK>(), kPairs = pair_bytes<EK>(), NW = 4, WC = 16 * CT * NW, MT = DAP / 16, THREADS = 64 * NW;
+    constexpr int CH = chunk_of(EK), TI = tiles_of(EK), ES = elem_size(EK), kPairs = pair_bytes<EK>(), NW = 4, WC = 16 * CT * NW, MT = DAP / 16, THREADS = 64 * NW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char *tb = smem, *tc = tb + CH * pitch_of<EK>(DAP), *ta = tc + CH * pitch_of<EK>(WC), *tp = ta + (OUTPUT ? CH * pitch_of<EK>(DAP) : 0);
 
@@ -477,16 +456,16 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
 #pragma unroll
         for (int k = 0; k < 3; ++k) further[k] = uniform(power(g2, 16 * (k + 1)));
         // (tiles above the diagonal that are read with their neighbours and never written)
-        for (int i = threadIdx.x; EK != kElemF32 && i < 2 * 2 * 16 * 2; i += THREADS) {
-            const int part = i / 64, tile = i / 32 % 2, row = i / 2 % 16, side = i % 2;
-            *reinterpret_cast<u32x4*>(tp + part * kPairs + (32 * tile + row) * kPairPitch + 64 * tile + 32 + 16 * side) = (u32x4){0, 0, 0, 0};
+        for (int i = threadIdx.x; EK != kElemF32 && i < kPairParts * 2 * 16 * 2; i += THREADS) {
+            const int part = i / 64, tile = i / 32 % 2 * 2, row = i / 2 % 16, side = i % 2;
+            *reinterpret_cast<u32x4*>(tp + part * kPairs + pair_row<EK>(tile) + row * pair_pitch<EK>(tile) + 32 * tile + 32 + 16 * side) = (u32x4){0, 0, 0, 0};
         }
     }
     // places in the tiles
     const unsigned char *along_b = tb + l16 * pitch_of<EK>(DAP) + 16 * own, *along_a = ta + l16 * pitch_of<EK>(DAP) + 16 * own;
     const unsigned char* picked_a = ta + l16 * pitch_of<EK>(DAP) + 4 * ES * own;
     const unsigned char *down_b = turned_base<EK, DAP>(tb, lane), *down_c = turned_base<EK, WC>(tc, lane) + 16 * ES * CT * wave;
-    unsigned char* pairs = tp + l16 * kPairPitch;
+    auto pairs = [&](int tile) { return tp + pair_row<EK>(tile) + l16 * pair_pitch<EK>(tile); };
 
     f32x4 S[MT][CT];
     float frame[CT];                                // half: S is in units of `frame`, a power of two a column
@@ -516,7 +495,6 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     const int ys = s.y_f32 ? 4 : ES;
     char* py = OUTPUT ? static_cast<char*>(const_cast<void*>(s.y.p)) + (begins(s.y) + col0 + wave * 16 * CT) * ys : nullptr;
     bool bad = false;
-    const bool kept = at.ends && s.ends;            // (the state is a result, not only an operand of the rows to come; y is the same, asked for or not)
     for (int64_t t = at.first; t < at.last; t += CH) {
         const int from = from_of(t);
         {
@@ -549,14 +527,17 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                     p = multiply(*reinterpret_cast<const V*>(along_b + 16 * j * pitch_of<EK>(DAP) + 64 * k),
                                  *reinterpret_cast<const V*>(along_a + 16 * i * pitch_of<EK>(DAP) + 64 * k), p);
                 p *= *reinterpret_cast<const f32x4*>(tables + (i == j ? 512 : 768)) * (i - j < 2 ? 1.f : further[i - j - 2]);
-                unsigned char* to = pairs + 16 * i * kPairPitch + 16 * ES * j + 4 * ES * own;
+                unsigned char* to = pairs(i) + 16 * ES * j + 4 * ES * own;
                 if constexpr (EK == kElemF32) {
                     *reinterpret_cast<f32x4*>(to) = p;
                 } else {
-                    const u32x2 h = {pack<bf16x8>(p[0], p[1]), pack<bf16x8>(p[2], p[3])};
-                    const f32x2 h0 = widen<bf16x8>(h[0]), h1 = widen<bf16x8>(h[1]);
-                    *reinterpret_cast<u32x2*>(to) = h;
-                    *reinterpret_cast<u32x2*>(to + kPairs) = (u32x2){pack<bf16x8>(p[0] - h0[0], p[1] - h0[1]), pack<bf16x8>(p[2] - h1[0], p[3] - h1[1])};
+#pragma unroll
+                    for (int q = 0; q < kPairParts; ++q) {
+                        const u32x2 h = {pack<bf16x8>(p[0], p[1]), pack<bf16x8>(p[2], p[3])};
+                        const f32x2 h0 = widen<bf16x8>(h[0]), h1 = widen<bf16x8>(h[1]);
+                        *reinterpret_cast<u32x2*>(to + q * kPairs) = h;
+                        p -= (f32x4){h0[0], h0[1], h1[0], h1[1]};
+                    }
                 }
             }
 
@@ -580,7 +561,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                 if constexpr (EK == kElemF32) {
 #pragma unroll
                     for (int i = k; i < TI; ++i) {
-                        const f32x4 p = *reinterpret_cast<const f32x4*>(pairs + 16 * i * kPairPitch + 64 * k + 16 * own);
+                        const f32x4 p = *reinterpret_cast<const f32x4*>(pairs(i) + 64 * k + 16 * own);
 #pragma unroll
                         for (int c = 0; c < CT; ++c) O[i][c] = multiply(cv[k][c], p, O[i][c]);
                     }
@@ -591,19 +572,19 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                         for (int c = 0; c < CT; ++c) parts(widened<V>(cv[k][c]), c2[c]);
 #pragma unroll
                     for (int i = 2 * k; i < TI; ++i) {
-                        bf16x8 p[2];
 #pragma unroll
-                        for (int q = 0; q < 2; ++q) p[q] = *reinterpret_cast<const bf16x8*>(pairs + q * kPairs + 16 * i * kPairPitch + 64 * k + 16 * own);
+                        for (int q = kPairParts; q-- > 0;) {
+                            const bf16x8 p = *reinterpret_cast<const bf16x8*>(pairs(i) + q * kPairs + 64 * k + 16 * own);
 #pragma unroll
-                        for (int c = 0; c < CT; ++c)
-                            if constexpr (EK == kElemF16) {
-                                O[i][c] = multiply(c2[c][1], p[0], O[i][c]);
-                                O[i][c] = multiply(c2[c][0], p[1], O[i][c]);
-                                O[i][c] = multiply(c2[c][0], p[0], O[i][c]);
-                            } else {
-                                O[i][c] = multiply(cv[k][c], p[1], O[i][c]);
-                                O[i][c] = multiply(cv[k][c], p[0], O[i][c]);
-                            }
+                            for (int c = 0; c < CT; ++c)
+                                if constexpr (EK == kElemF16) {
+                                    // (the last parts' product is below what the others are rounded to)
+                                    if (q < kPairParts - 1) O[i][c] = multiply(c2[c][1], p, O[i][c]);
+                                    O[i][c] = multiply(c2[c][0], p, O[i][c]);
+                                } else {
+                                    O[i][c] = multiply(cv[k][c], p, O[i][c]);
+                                }
+                        }
                     }
                 }
             }
@@ -635,7 +616,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
                 put_all(static_cast<T*>(nullptr));
             py += dir * CH * s.y.token * ys;
         }
-        add_products<EK, MT, CT, first_parts<EK, OUTPUT>()>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b, kept);
+        add_products<EK, MT, CT>(S, frame, from == 0 ? chunk_decay : power(g2, CH - from), cv, tables, shift, down_b);
     }
 #pragma unroll
     for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] *= frame[i % CT];

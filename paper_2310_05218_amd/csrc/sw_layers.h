@@ -154,7 +154,6 @@ struct AttentionSum {
     int DA, DC;
     float alpha_s, alpha_y;
     bool reverse, y_f32;
-    bool ends;                          // the state after the last token is a result (where `last` asks for it)
     float* states = nullptr;            // [segments, H, DA, DC]: the state before each segment
     bool turned = false;                // ... of the sum with a's and c's widths exchanged: [segments, H, DC, DA]
 };

@@ -229,7 +229,7 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
     const AttentionState first{const_cast<float*>(state), states, per_head, d.dv, 1}, last{final_state, states, per_head, d.dv, 1};
     AttentionSums s;
     s.count = 1;
-    s.of[0] = AttentionSum{tq.op, tk.op, tv.op, to.op, first, last, slots, d.dk, d.dv, 1.0f, d.scale, false, false, true, static_cast<float*>(workspace)};
+    s.of[0] = AttentionSum{tq.op, tk.op, tv.op, to.op, first, last, slots, d.dk, d.dv, 1.0f, d.scale, false, false, static_cast<float*>(workspace)};
     const AttentionBatch n{log_decay, starts, d.T, d.B, d.heads, d.n_states};
     const AttentionSegments g = segments_of(d, starts != nullptr);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -301,18 +301,18 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     // the states before each segment, forwards (those of the forward call) and backwards in time
     const int64_t bytes = state_bytes(d, starts != nullptr);
     float *ahead = part_v + fold_bytes(d, starts != nullptr, d.dv) / 4, *back = ahead + bytes / 4;
-    const AttentionSum of_q{tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false, false, ahead, true};
+    const AttentionSum of_q{tdo.op, tv.op, tk.op, tdq.op, turned, none, slots, d.dv, d.dk, 1.0f, d.scale, false, false, ahead, true};
     const AttentionSum of_k{tv.op, tdo.op, tq.op, share > 1 ? part(part_k, d.dk) : tdk.op, turned_final, none, nullptr, d.dv, d.dk, d.scale, 1.0f, true,
-                            share > 1, false, back, true};
+                            share > 1, back, true};
     const AttentionSum of_v{tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale, 1.0f, true,
-                            share > 1, true, back, false};
+                            share > 1, back, false};
     const AttentionSums gradients{{of_q, of_k, of_v}, 3};
     const AttentionSegments g = segments_of(d, starts != nullptr);
     hipError_t e = hipSuccess;
     if (near_rows({&tdo, &tq, &tk, &tv, &tdq, &tdk, &tdv})) {
         if (bytes) {
             const AttentionSum forward{tq.op, tk.op, tv.op, tdo.op, {const_cast<float*>(state), states, per_head, d.dv, 1}, none, slots, d.dk, d.dv, 1.0f,
-                                       d.scale, false, false, false, ahead, false};
+                                       d.scale, false, false, ahead, false};
             const AttentionSums both{{forward, of_v, of_v}, 2};
             e = launch_attention_states(both, n, g, d.type, st);
             if (e == hipSuccess) e = launch_attention_scan(both, n, g, st);
