@@ -236,8 +236,8 @@ __device__ __forceinline__ float column_largest(float v)
     return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
 }
 
-// The exponent that brings a magnitude to 2^13 ... 2^14, within what halves hold.  (Of a column, or a state, far below 2^-30 some bits are
-// lost; halves themselves end at 2^-24.)
+// The exponent that brings a magnitude to 2^13 ... 2^14, within what halves hold.  (Of a column far below 2^-30 some bits are lost; halves
+// themselves end at 2^-24.)
 __device__ __forceinline__ int half_exponent(float largest)
 {
     const int e = __builtin_amdgcn_frexp_expf(largest);
@@ -251,25 +251,22 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
 {
     typedef typename Operand<EK>::vec V;
     constexpr int TI = tiles_of(EK);
-    float in[CT], out = 1.f;
+    float in[CT];
+    f32x4 out[CT];
     if constexpr (EK == kElemF16) {
-        // one scale for the wavefront's columns: they are the rows of what is computed
-        float largest = 0.f;
+        // a scale for each column, which is a row of what is computed: those of a lane's four rows are other lanes'
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-            float of = 0.f;
+            float largest = 0.f;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) of = fmaxf(of, fabsf(S[m][c][e]));
-            largest = fmaxf(largest, of * frame[c]);
+                for (int e = 0; e < 4; ++e) largest = fmaxf(largest, fabsf(S[m][c][e]));
+            const int exponent = half_exponent(column_largest(largest * frame[c]));
+            in[c] = frame[c] * __builtin_amdgcn_ldexpf(1.f, -exponent);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) out[c][e] = __builtin_amdgcn_ldexpf(1.f, __shfl(exponent, 4 * (threadIdx.x % 64 / 16) + e, 64));
         }
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d, 64));
-        const int e = half_exponent(column_largest(largest));
-#pragma unroll
-        for (int c = 0; c < CT; ++c) in[c] = frame[c] * __builtin_amdgcn_ldexpf(1.f, -e);
-        out = __builtin_amdgcn_ldexpf(1.f, e);
     }
     if constexpr (EK == kElemF32) {
 #pragma unroll
@@ -306,7 +303,10 @@ __device__ __forceinline__ void state_times_a(const f32x4 (&S)[MT][CT], const fl
 #pragma unroll
     for (int i = 0; i < TI; ++i)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) O[i][c] *= reach[i] * out;
+        for (int c = 0; c < CT; ++c) {
+            O[i][c] *= reach[i];
+            if (EK == kElemF16) O[i][c] *= out[c];
+        }
 }
 
 // S <- whole S + sum over the chunk's tokens of b times weighted c (an operand vector's tokens: weights in `tables`, those of

@@ -73,3 +73,23 @@ def test_one_rounding(sw, B, T, H, Hk, dk, dv, t):
     for name, x, w, a in (("final_state", last, want[1], mag[1]), ("d_state", first, want[5], mag[5])):
         off = float(((x.cpu().double() - w).abs() / a).max())
         assert off <= 16 * U, f"{name}: {off:.3g} of the terms' magnitudes"
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("B,T,H,dk,dv", [(1, 1000, 4, 128, 128), (2, 200, 16, 64, 96)])
+def test_columns_of_different_magnitudes(sw, B, T, H, dk, dv, t):
+    """Neighbouring columns of values, and of what comes of them, 2^20 apart: each keeps its own bits."""
+    r = torch.Generator().manual_seed(T)
+    n = lambda *s: torch.randn(s, generator=r)
+    apart = lambda d: torch.where(torch.arange(d) % 2 == 0, 2.0 ** 8, 2.0 ** -12)
+    q, k, v, do = n(B, T, H, dk).to(TYPES[t]), n(B, T, H, dk), (n(B, T, H, dv) * apart(dv)).to(TYPES[t]), n(B, T, H, dv).to(TYPES[t])
+    s0 = n(B, H, dk, dv) * apart(dv)
+    k = k.to(TYPES[t])
+    g = torch.log1p(-torch.exp2(-torch.linspace(2, 8, H)))
+    o = sw.sw_linear_attention(*(x.cuda() for x in (q, k, v, g)), state=s0.cuda()).cpu().double()
+    w = definition(q, k, v, do, g, dk ** -0.5, s0, torch.zeros_like(s0), False)[0]
+    w = w if t == "f32" else w.to(TYPES[t]).double()
+    bound = 9 * U if t == "f32" else (8 * U * torch.finfo(TYPES[t]).eps) ** 0.5
+    for first in (0, 1):
+        off = float((o - w)[..., first::2].norm() / w[..., first::2].norm())
+        assert off <= bound, f"columns {first}, {first + 2} ...: {off:.3g} off the rounded result, {bound:.3g} allowed"
