@@ -306,7 +306,7 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
                             share > 1, back, true};
     const AttentionSum of_v{tk.op, tq.op, tdo.op, share > 1 ? part(part_v, d.dv) : tdv.op, first, last, nullptr, d.dk, d.dv, d.scale, 1.0f, true,
                             share > 1, back, false};
-    const AttentionSums gradients{{of_q, of_k, of_v}, 3};
+    const AttentionSums gradients{{of_q, of_k, of_v}, 3}, of_q_and_k{{of_q, of_k, of_k}, 2}, of_v_alone{{of_v, of_v, of_v}, 1};
     const AttentionSegments g = segments_of(d, starts != nullptr);
     hipError_t e = hipSuccess;
     if (near_rows({&tdo, &tq, &tk, &tv, &tdq, &tdk, &tdv})) {
@@ -317,8 +317,12 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
             e = launch_attention_states(both, n, g, d.type, st);
             if (e == hipSuccess) e = launch_attention_scan(both, n, g, st);
         }
-        if (e == hipSuccess) e = launch_attention_chunks(gradients, n, g, d.type, st);
+        // (where d_state replaces d_final_state, all of dk's sum has read it before dv's, which writes it, begins: workgroups of one launch have no order)
+        const bool in_place = d_state && d_state == d_final_state;
+        if (e == hipSuccess) e = launch_attention_chunks(in_place ? of_q_and_k : gradients, n, g, d.type, st);
+        if (e == hipSuccess && in_place) e = launch_attention_chunks(of_v_alone, n, g, d.type, st);
     } else {
+        // (dv's last, for the same reason)
         for (int i = 0; i < 3 && e == hipSuccess; ++i) e = launch_attention_recurrent(gradients.of[i], n, d.type, st);
     }
     if (e == hipSuccess && share > 1) e = launch_attention_fold(AttentionFold{part_k, tdk.op, d.dk}, AttentionFold{part_v, tdv.op, d.dv}, n, d.type, st);
