@@ -48,6 +48,7 @@ __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel
     const int entry = s.first_slots ? s.first_slots[seq] : seq;
     const bool kept = !s.first_slots || (entry >= 0 && entry < n.n_states);
     const float decay = expf(n.log_decay[head]);
+    const int own = s.DA - group * ROWS;            // rows of the state here (those beyond it would be zero times whatever c is)
     float state[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
@@ -68,6 +69,7 @@ __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel
         float y = 0.f;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
+            if (r >= own) break;
             const float held = s.reverse ? state[r] : state[r] * decay;
             state[r] = held + lb[buf][group * ROWS + r] * c;
             y += state[r] * la[buf][group * ROWS + r];
