@@ -102,8 +102,8 @@ __global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSums sums,
     const int i = (blockIdx.x * 256 + threadIdx.x) * VEC, head = blockIdx.y % (unsigned)n.H;
     if (i >= s.DA * s.DC) return;
     const float g2 = n.log_decay[head] * 1.44269504088896341f;
-    // (an infinity fades to none: where l is above zero, so is its power)
-    const float decay = g2 > -INFINITY ? fmaxf(__builtin_amdgcn_exp2f(g2 * (float)g.length), 1e-38f) : 0.f;
+    // (an infinity does not fade: where l is above zero, so is its power, however small)
+    const float decay = exp2f(g2 * (float)g.length), of_infinity = g2 > -INFINITY ? 1.f : 0.f;
     const int64_t step = (int64_t)n.H * s.DA * s.DC;
     for (int seq = blockIdx.z; seq < n.B; seq += gridDim.z) {
         int64_t len = n.T, slot;
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSums sums,
             for (int j = 0; j < kScanAhead; ++j) {
                 if (k + j < segments) *at(k + j) = state;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) state[e] = fmaf(state[e], decay, own[j][e]);
+                for (int e = 0; e < VEC; ++e) state[e] = fmaf(state[e], fabsf(state[e]) == INFINITY ? of_infinity : decay, own[j][e]);
             }
         }
     }
