@@ -620,7 +620,9 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
     }
 #pragma unroll
     for (int i = 0; i < MT * CT; ++i) S[i / CT][i % CT] *= frame[i % CT];
-    if (!OUTPUT) bad = any_nonfinite(S);
+    float* const last = OUTPUT && at.ends ? entry_of(s.last, s, n, at.seq, head) : nullptr;
+    // (outputs say nothing of the last chunk's new terms, nor of a half state that is too large for units of theirs)
+    if (!OUTPUT || last) bad |= any_nonfinite(S);
     if (bad) {
         __builtin_amdgcn_s_waitcnt(0);              // (what has been stored is stored before it is stored again)
         begin();
@@ -636,8 +638,7 @@ __global__ __launch_bounds__(256, DAP <= 128 ? 2 : 1) void attention_chunk_kerne
         }
     }
     if constexpr (OUTPUT) {
-        float* p = at.ends ? entry_of(s.last, s, n, at.seq, head) : nullptr;
-        if (p) store_state(S, p, s.last.row, s.last.col, s, col);
+        if (last) store_state(S, last, s.last.row, s.last.col, s, col);
     } else {
         store_state(S, s.states + (at.slot * n.H + head) * s.DA * s.DC, s.DC, 1, s, col);
     }
