@@ -452,7 +452,8 @@ int64_t sw_layer_norm_backward_workspace_bytes(int64_t rows, int64_t C);     /* 
  * log_decay: [heads] fp32, <= 0; -infinity forgets everything before a token.  It is a constant of the layer.
  * Sequences of different lengths: starts [B+1] int32 (device), not decreasing, and B = 1 in the strides: sequence b
  * is the rows starts[b] ... starts[b+1]-1 of T rows in all; rows in no sequence get zeros.  Values out of range are
- * taken as the nearest in range.  A sequence may be empty: its final state is its first.
+ * taken as the nearest in range; where they do decrease, o, the states kept and the gradients are not defined, but nothing
+ * outside of the tensors is read or written.  A sequence may be empty: its final state is its first.
  * state, final_state: [n_states, heads, dk, dv] fp32 or NULL, contiguous; sequence b has entry slots[b] of both, or
  * entry b where slots is NULL (n_states >= B then, else SW_ERR_SHAPE).  slots: [B] int32 (device), no entry twice; a
  * sequence with an entry outside 0 ... n_states-1 starts from zero and its final state is not kept.  final_state

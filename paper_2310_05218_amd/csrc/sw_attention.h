@@ -66,7 +66,7 @@ __device__ __forceinline__ Place locate(const AttentionBatch& n, const Attention
         p.rest = false;
     }
     const int64_t segments = p.len <= g.length ? 1 : (p.len + g.length - 1) / g.length;
-    p.none = segment >= segments;
+    p.none = segment < 0 || segment >= segments;    // (below zero: starts that decrease, whose places are in no order)
     if (reverse && !p.none && !p.rest) {
         p.slot += segments - 1 - 2 * segment;
         segment = segments - 1 - segment;
