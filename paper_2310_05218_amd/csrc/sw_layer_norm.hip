@@ -9,6 +9,8 @@
 // Loads are 16 bytes at any element's address.  The lane at the end of a row that is no whole number of vectors has the row's last vector, whose
 // first elements are another's too: it leaves them out of its sums and stores what the other stores.  (With single elements in their place the
 // compiler waits for a row's every load before the next one: the backward pass of 3001 rows of 1999 bf16 took 31 us for 17.)
+#include <initializer_list>
+
 #include "sw_layers.h"
 
 namespace swconv {
@@ -436,6 +438,13 @@ constexpr int kBackwardMost = 1024;
 constexpr int backward_threads(int lanes) { return lanes > 64 ? 512 : kBackwardMost; }
 constexpr int kLongParts = 64;
 
+// Rows of sums that a backward launch writes.
+unsigned backward_parts(int64_t rows, int lanes)
+{
+    if (lanes == 0) return (unsigned)(rows < kLongParts ? rows : kLongParts);
+    return row_groups(rows, lanes, backward_threads(lanes));
+}
+
 }  // namespace
 
 hipError_t launch_layer_norm(const LayerNormArgs& a, int ek, hipStream_t st)
@@ -454,10 +463,18 @@ hipError_t launch_layer_norm(const LayerNormArgs& a, int ek, hipStream_t st)
     });
 }
 
-int layer_norm_backward_parts(int64_t rows, int64_t)
+int layer_norm_backward_parts(int64_t rows, int64_t C)
 {
-    const int64_t most = kCUs * (kBackwardMost / 256);      // of any format and width
-    return (int)(rows < most ? rows : most);
+    unsigned most = 0;          // of any format
+    for (const int ek : {kElemF32, kElemBF16, kElemF16})
+        (void)with_elem(ek, [&](auto e) {
+            return with_lanes<e(), true>(C, [&](auto lanes, auto) {
+                const unsigned parts = backward_parts(rows, lanes());
+                if (parts > most) most = parts;
+                return hipSuccess;
+            });
+        });
+    return (int)most;
 }
 
 hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek, hipStream_t st)
@@ -466,9 +483,8 @@ hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek,
     if (!a.dweight && !a.dbias) a.partial = nullptr;
     return with_elem(ek, [&](auto e) {
         return with_lanes<e(), true>(a.C, [&](auto lanes, auto nv) {
-            unsigned parts;
+            const unsigned parts = backward_parts(a.rows, lanes());
             if constexpr (lanes() == 0) {
-                parts = (unsigned)(a.rows < kLongParts ? a.rows : kLongParts);
                 note_kernel("layer_norm_long_dx_kernel", ek);
                 if (a.partial) {
                     hipLaunchKernelGGL(layer_norm_long_sums_kernel<e()>, dim3((a.C + 255) / 256, parts), dim3(256), 0, st, a, (a.rows + parts - 1) / parts);
@@ -476,7 +492,6 @@ hipError_t launch_layer_norm_backward(const LayerNormBackwardArgs& args, int ek,
                 }
                 if (a.dx) hipLaunchKernelGGL(layer_norm_long_dx_kernel<e()>, dim3(row_groups(a.rows, 1024, kForwardThreads)), dim3(1024), 0, st, a);
             } else {
-                parts = row_groups(a.rows, lanes(), backward_threads(lanes()));
                 const dim3 block(threads_of(lanes()));
                 note_kernel("layer_norm_backward_kernel", ek, lanes(), nv());
                 with_tail<e(), lanes(), nv()>(
