@@ -214,7 +214,7 @@ int sw_linear_attention(const void* q, const void* k, const void* v, void* o, co
         misaligned(state, 4) || misaligned(final_state, 4) || misaligned(slots, 4) || misaligned(starts, 4))
         return SW_ERR_ALIGN;
     const int64_t per_head = (int64_t)d.dk * d.dv, states = per_head * d.heads;
-    if (states > kMaxExtent / (d.n_states + 1)) return SW_ERR_SHAPE;
+    if (states > kMaxExtent / ((int64_t)d.n_states + 1)) return SW_ERR_SHAPE;
     const int64_t need = sw_linear_attention_workspace_bytes(dims, starts != nullptr);
     if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
     const Span in[7] = {span_of(q, tq.elements, size), span_of(k, tk.elements, size), span_of(v, tv.elements, size), span_of(log_decay, d.heads, 4),
@@ -275,7 +275,7 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
         misaligned(starts, 4))
         return SW_ERR_ALIGN;
     const int64_t per_head = (int64_t)d.dk * d.dv, states = per_head * d.heads;
-    if (states > kMaxExtent / (d.n_states + 1) || states > kMaxExtent / d.B) return SW_ERR_SHAPE;
+    if (states > kMaxExtent / ((int64_t)d.n_states + 1) || states > kMaxExtent / d.B) return SW_ERR_SHAPE;
     const int64_t need = sw_linear_attention_backward_workspace_bytes(dims, starts != nullptr);
     if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
     const Span in[9] = {span_of(d_o, tdo.elements, size), span_of(q, tq.elements, size), span_of(k, tk.elements, size),
