@@ -96,10 +96,12 @@ AttentionSegments segments_of(const sw_linear_attention_dims& d, bool packed)
     return attention_segments(AttentionBatch{nullptr, nullptr, d.T, d.B, d.heads, d.n_states}, d.dk, d.dv, packed, d.type);
 }
 
-// The same of calls that work on `sums` at a time: a launch has fewer than 2^32 threads, 256 for every segment's place, head and sum.
+// The same of calls that work on `sums` at a time: a launch has fewer than 2^32 threads, 256 for every segment's place, head and sum.  (Heads' rows
+// beyond a tensor's extent are refused before bytes are counted from them.)
 int check_sums(const sw_linear_attention_dims& d, bool packed, int sums)
 {
     if (const int rc = check_dims(d)) return rc;
+    if (d.T * (packed ? 1 : d.B) > kMaxExtent / ((int64_t)d.heads * (d.dk > d.dv ? d.dk : d.dv))) return SW_ERR_SHAPE;
     return segments_of(d, packed).count > ((1 << 24) - 1) / ((int64_t)d.heads * sums) ? SW_ERR_SHAPE : SW_OK;
 }
 

@@ -30,3 +30,18 @@ def test_as_many_states_as_an_int_counts(L, n_states):
                                                     s, s, s, s, s, s, s, None, 0, None)
     inside = (1 << 30) + n_states * 2 * 64 * 64 * 4 - 0x10000
     assert call(inside) == back(inside) == B.SW_ERR_ALIAS
+
+
+@pytest.mark.parametrize("T,n,heads,packed", [(1 << 46, 1, 65535, 0), (1 << 46, 1, 65535, 1), (1 << 30, 100, 65535, 0), (1 << 44, 1, 1024, 0)])
+def test_workspaces_of_rows_beyond_any_tensor(L, T, n, heads, packed):
+    """Bytes that 64 bits do not count: 0, as for all invalid extents."""
+    d = B.SwLinearAttentionDims(T, n, heads, 1, 256, 256, 0, B.SW_BF16, 1.0)
+    assert L.sw_linear_attention_backward_workspace_bytes(d, packed) == L.sw_linear_attention_workspace_bytes(d, packed) == 0
+
+
+@pytest.mark.parametrize("T,n,heads,packed", [(1 << 24, 1 << 14, 64, 1), (8192, 32, 64, 0)])
+def test_workspaces_of_ordinary_rows(L, T, n, heads, packed):
+    """Packed rows count once, whatever the number of sequences."""
+    d = B.SwLinearAttentionDims(T, n, heads, 8, 128, 128, 0, B.SW_BF16, 1.0)
+    rows = T if packed else T * n
+    assert L.sw_linear_attention_backward_workspace_bytes(d, packed) >= 2 * rows * heads * 128 * 4
