@@ -485,7 +485,8 @@ int64_t sw_linear_attention_workspace_bytes(const sw_linear_attention_dims* dims
  *     dS_t = scale * q_t do_t^T + l * dS_{t+1},  dq_t = scale * S_t do_t,  dk_t = dS_t v_t,  dv_t = dS_t^T k_t,  d_state = l * dS_1
  * dk and dv of shared rows are sums over the heads that share them.  state as in the forward call; d_final_state and
  * d_state: [B, heads, dk, dv] (entry b, whatever slots says of state); d_state is NULL where it is not wanted and may be
- * d_final_state.  dq, dk, dv have q's, k's and v's shapes and strides of their own; rows in no sequence get zeros.
+ * d_final_state.  dq, dk, dv have q's, k's and v's shapes and strides of their own, and may lie interleaved but have no
+ * element in common (SW_ERR_ALIAS where two begin at one address); rows in no sequence get zeros.
  */
 int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, const void* v, const float* log_decay,
                                  const float* state, const float* d_final_state, void* dq, void* dk, void* dv, float* d_state,

@@ -283,14 +283,14 @@ int sw_linear_attention_backward(const void* d_o, const void* q, const void* k, 
     const Span in[9] = {span_of(d_o, tdo.elements, size), span_of(q, tq.elements, size), span_of(k, tk.elements, size),
                         span_of(v, tv.elements, size), span_of(log_decay, d.heads, 4), span_of(state, states * d.n_states, 4),
                         span_of(d_final_state, states * d.B, 4), span_of(slots, d.B, 4), span_of(starts, d.B + 1, 4)};
-    // (gradients may lie interleaved in one tensor, as q, k and v may: their spans are not held against each other)
+    // (gradients may lie interleaved in one tensor, as q, k and v may: their spans are not held against each other, but no two begin together)
     const Span out[5] = {span_of(dq, tdq.elements, size), span_of(dk, tdk.elements, size), span_of(dv, tdv.elements, size),
                          span_of(d_state, states * d.B, 4), span_of(workspace, need, 1)};
     for (int p = 0; p < 5; ++p) {
         for (int i = 0; i < 9; ++i)
             if (meet(out[p], in[i]) && !(p == 3 && i == 6 && d_state == d_final_state)) return SW_ERR_ALIAS;
-        for (int r = 0; r < p && p >= 3; ++r)
-            if (meet(out[p], out[r])) return SW_ERR_ALIAS;
+        for (int r = 0; r < p; ++r)
+            if (p >= 3 ? meet(out[p], out[r]) : out[p].at == out[r].at) return SW_ERR_ALIAS;
     }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     const AttentionBatch n{log_decay, starts, d.T, d.B, d.heads, d.n_states};

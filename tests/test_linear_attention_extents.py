@@ -1,4 +1,4 @@
-"""Linear attention's checks of extents at the ends of their types, on addresses that are never used."""
+"""Linear attention's checks of extents at the ends of their types, and of gradients in one place, on addresses that are never used."""
 import pytest
 
 from paper_2310_05218_amd import binding as B
@@ -45,3 +45,14 @@ def test_workspaces_of_ordinary_rows(L, T, n, heads, packed):
     d = B.SwLinearAttentionDims(T, n, heads, 8, 128, 128, 0, B.SW_BF16, 1.0)
     rows = T if packed else T * n
     assert L.sw_linear_attention_backward_workspace_bytes(d, packed) >= 2 * rows * heads * 128 * 4
+
+
+@pytest.mark.parametrize("same", ["qk", "qv", "kv"])
+def test_gradients_in_one_place(L, same):
+    d = B.SwLinearAttentionDims(10, 2, 4, 4, 16, 16, 0, B.SW_F32, 0.25)
+    s = strides(10, 4, 16)
+    at = {n: FAR + i * 0x100000 for i, n in enumerate("qkv")}
+    at[same[1]] = at[same[0]]
+    call = lambda g: L.sw_linear_attention_backward(1 << 40, (1 << 40) + 0x10000, (1 << 40) + 0x20000, (1 << 40) + 0x30000, 1 << 39, None, None, g["q"], g["k"], g["v"], None, None, None, d,
+                                                    s, s, s, s, s, s, s, None, 0, None)
+    assert call(at) == B.SW_ERR_ALIAS
