@@ -168,7 +168,7 @@ struct AttentionBatch {
     int B, H, n_states;
 };
 // A long sequence is cut into segments of `length` tokens (a multiple of the chunk) that are worked on side by side: their own sums first
-// (attention_states), the state before each from these (attention_scan), then the outputs (attention_chunks).  length 0: whole sequences.
+// (attention_states), the state before each from these (attention_scan), then the outputs (attention_chunks).  A length of 2^62: whole sequences.
 struct AttentionSegments {
     int64_t length, count;              // count: places for segments in all
 };

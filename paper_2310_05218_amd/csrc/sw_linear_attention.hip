@@ -7,15 +7,6 @@ namespace {
 
 constexpr int kColumns = 64, kGroups = 4;       // a workgroup has 64 columns of the state, a quarter of its rows a wavefront
 
-__device__ __forceinline__ int64_t clamped(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
-
-// Rows [lo, hi) of a packed batch's sequence j - 1, j = 1 ... B; j = 0 and B + 1: the rows before the first and after the last one.
-__device__ __forceinline__ void packed_rows(const AttentionBatch& n, int j, int64_t* lo, int64_t* hi)
-{
-    *lo = j == 0 ? 0 : clamped(n.starts[j - 1], 0, n.T);
-    *hi = j == n.B + 1 ? n.T : clamped(n.starts[j], *lo, n.T);
-}
-
 template <int EK, int ROWS>
 __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel(AttentionSum s, AttentionBatch n)
 {
@@ -28,7 +19,8 @@ __global__ __launch_bounds__(kColumns * kGroups) void attention_recurrent_kernel
     int64_t batch = seq;
     bool rest = false;
     if (n.starts) {
-        packed_rows(n, blockIdx.x, &lo, &hi);
+        lo = attention::packed_first(n, blockIdx.x);
+        hi = attention::packed_end(n, blockIdx.x, lo);
         rest = blockIdx.x == 0 || (int)blockIdx.x == n.B + 1;
         seq = (int)blockIdx.x - 1;
         batch = 0;
