@@ -14,8 +14,8 @@
 // So a result is what sums in 32 bits make it before its one rounding.  (With two bf16 values each, 17 bits, 8192 tokens on 16 heads of 128 bf16 took 88 us
 // for 94, gradients of 4 x 4096 tokens 318 for 359, and three times as many of their results were rounded the other way.)
 //
-// 8192 tokens on 16 heads of 128 bf16: 94 us, of which 60 without any of the products (335 MB at 5.6 TB/s: the operands, those of the segments' own sums
-// once more, and 134 MB of states); the rest are a chunk's phases, one after another in a workgroup, with two of these on a CU (76 KB of LDS each).
+// 8192 tokens on 16 heads of 128 bf16: 94 us; of one set of inputs 91, of which 63 without any of the computations (335 MB at 5.3 TB/s: the operands, those of
+// the segments' own sums once more, and 134 MB of states); the rest are a chunk's phases, one after another in a workgroup, with two of these on a CU (76 KB of LDS each).
 #pragma once
 
 #include "sw_attention.h"
@@ -651,7 +651,7 @@ hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const
     auto padded = [](int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 128 ? 128 : 256; };
     auto columns = [](int d) { return d <= 64 ? 0 : (d + 127) / 128; };
     // At most two workgroups of 64 columns a CU: in one launch, with as many rows of the state as the most of them have (gradients of 500 tokens
-    // on 8 heads of 64 x 128 bf16, us: 36.6 in two launches, 27.4 in one).  States of 256 rows have no room for two on a CU.
+    // on 8 heads of 64 x 128 bf16, us: 32.6 in two launches, 26.5 in one).  States of 256 rows have no room for two on a CU.
     int most_rows = 0, most_columns = 0;
     for (int i = 0; i < all.count; ++i) {
         most_rows = padded(all.of[i].DA) > most_rows ? padded(all.of[i].DA) : most_rows;
@@ -689,7 +689,7 @@ hipError_t launch_chunk(const AttentionSums& all, const AttentionBatch& n, const
             }
         };
         // Wavefronts of 16 columns where workgroups of 128 columns would be no more than the CUs: twice as many, each through in less time (128
-        // tokens, us with 32 and with 16 columns: 8 heads of 128 bf16 17.9 and 13.4, 192 heads 21.4 and 18.6, 288 heads 24.8 and 30.1).
+        // tokens, us with 32 and with 16 columns: 8 heads of 128 bf16 17.2 and 13.5, 192 heads 18.1 and 17.8, 288 heads 22.9 and 27.0).
         const bool few = g.count * n.H * s.count * ((dc + 127) / 128) <= 256;
         const hipError_t e = dc <= 64 || few ? rows(std::integral_constant<int, 1>()) : rows(std::integral_constant<int, 2>());
         if (e != hipSuccess) return e;

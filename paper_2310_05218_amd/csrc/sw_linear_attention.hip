@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void attention_scan_kernel(AttentionSums sums,
 }
 
 // VEC elements of a row and group of heads a thread, dk's and dv's workgroups side by side (gradients of 4 x 2000 tokens, 16 heads on 4 of 128 bf16:
-// 239 us with a launch for each and an element a thread, 216 so).
+// 230 us, 23 more with a launch for each and an element a thread).
 template <int EK, int VEC>
 __global__ __launch_bounds__(256) void attention_fold_kernel(AttentionFold dk, AttentionFold dv, int H, int64_t T, int64_t rows)
 {
@@ -255,11 +255,11 @@ SW_ATTENTION_UNITS(chunks)
 #undef SW_ATTENTION_UNITS
 
 // Sequences are cut where there are fewer heads than `want` workgroups, and where that gains more than the two launches that it takes. us:
-// - equal ones of up to four chunks stay whole (256 tokens bf16, 8 x 16 heads of 64: 18.2 whole, 28.5 cut; 200 tokens fp32, gradients, 8 heads of
+// - equal ones of up to four chunks stay whole (256 tokens bf16, 8 x 16 heads of 64: 17.8 whole, 24.8 cut; 200 tokens fp32, gradients, 8 heads of
 //   64: 24.5 and 22.9); so do packed ones that are short in the mean and 512 tokens together, which bounds what the longest of them takes (8 of
-//   500 tokens bf16, 8 heads of 64: 15.0 and 23.1).
+//   500 tokens bf16, 8 heads of 64: 15.1 and 24.1).
 // - segments of one chunk of 64 while those of two would be fewer than 192 workgroups (1000 tokens fp32, 8 heads of 64: 25.4, with two 32.8; where
-//   they would be 256, the states cost more: 2 x 1000 tokens half on 16 heads of 128 51 and 42), but for packed ones that are that short.
+//   they would be 256, the states cost more: 2 x 1000 tokens half on 16 heads of 128 50 and 39), but for packed ones that are that short.
 AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bool packed, int ek)
 {
     const int64_t rows = packed ? n.T : n.T * n.B, columns = (DC + 127) / 128, two = 2 * kAttentionChunk;
@@ -280,7 +280,7 @@ AttentionSegments attention_segments(const AttentionBatch& n, int DA, int DC, bo
 hipError_t launch_attention_scan(const AttentionSums& s, const AttentionBatch& n, const AttentionSegments& g, hipStream_t st)
 {
     // Four elements a thread where single ones would be more than the chip has room for (the calls' us with one and with four: 24 packed sequences on
-    // 8 heads of 64 x 64, 3072 workgroups, 37.1 and 33.5; 4096 tokens on 8 such heads, 128 workgroups, 28.2 and 29.8).
+    // 8 heads of 64 x 64, 3072 workgroups, 38.8 and 33.2; 4096 tokens on 8 such heads, 128 workgroups, 27.2 and 28.1).
     const int elements = s.of[0].DA * s.of[0].DC;
     const int64_t single = (int64_t)((elements + 255) / 256) * n.H * s.count * n.B;
     const int vec = elements % 4 == 0 && single >= 2048 ? 4 : 1;
