@@ -506,6 +506,113 @@ int sw_linear_attention_step(const void* q, const void* k, const void* v, void* 
                              const int32_t* slots, const sw_linear_attention_dims* dims, const sw_strides* q_strides,
                              const sw_strides* k_strides, const sw_strides* v_strides, const sw_strides* o_strides, void* hip_stream);
 
+/*
+ * ---- Gated linear recurrence, norms of heads with their rotation, low-rank adapters -----------------------
+ * More of a sequence model's block on the same rows; conventions as for layer norm and linear attention.  Tensors that lie
+ * interleaved (slices of the rows of a fused projection) do not overlap; those that do are SW_ERR_ALIAS.
+ */
+
+/*
+ * A linear recurrence with a decay for each channel that gates open, another sliding window without an end.  For every sequence
+ * and channel c, with s = sigmoid(decay_gate_t), a_t = exp(log_decay[c] * s) and the state h [C],
+ *     h_t = a_t * h_{t-1} + sqrt(1 - a_t^2) * sigmoid(input_gate_t) * x_t,      h before the first token: `state` or zero.
+ * x, decay_gate, input_gate, h: [B, T, C], each with strides of its own (strides[0 ... 3] in this order; head is unused).
+ * log_decay: [C] fp32, <= 0 (-infinity forgets everything unless s is 0, which it is below fp32's normal numbers).  Packed sequences, slots and states as in
+ * sw_linear_attention: starts [B+1] int32, rows in no sequence get zeros; state, final_state: [n_states, C] fp32 or NULL, contiguous;
+ * final_state may be state.  The state is kept in fp32; h is rounded once.  C <= 2^20 (SW_ERR_UNSUPPORTED beyond); rows and
+ * sequences as far as a launch has workgroups (SW_ERR_SHAPE beyond).  An infinity or a NaN reaches later tokens of its sequence and channel only.
+ */
+typedef struct {
+    int64_t T;                          /* tokens of a sequence, or of all packed ones (starts)        */
+    int64_t C;
+    int B;                              /* sequences                                                   */
+    int n_states;                       /* entries of state and final_state (0 where there is neither) */
+    int type;                           /* sw_type of the [B, T, C] tensors                            */
+} sw_gated_recurrence_dims;
+
+int sw_gated_recurrence(const void* x, const void* decay_gate, const void* input_gate, const float* log_decay, void* h,
+                        const float* state, float* final_state, const int32_t* slots, const int32_t* starts,
+                        const sw_gated_recurrence_dims* dims, const sw_strides* strides, void* workspace, int64_t workspace_bytes,
+                        void* hip_stream);
+int64_t sw_gated_recurrence_workspace_bytes(const sw_gated_recurrence_dims* dims, int packed);     /* packed: starts is given */
+
+/*
+ * Its backward pass, from dh, the forward call's inputs and its result h (as it was rounded) and, where the final state went on,
+ * d_final_state (else NULL).  With w_t = sqrt(1 - a_t^2), p_t = sigmoid(input_gate_t), s_t = sigmoid(decay_gate_t), L_t = log_decay * s_t:
+ *     u_t = dh_t + a_{t+1} u_{t+1},   dx_t = u_t w_t p_t,   d_input_gate_t = u_t w_t x_t p_t (1 - p_t),
+ *     l_t = u_t (a_t h_{t-1} - p_t x_t a_t^2 / w_t),   d_decay_gate_t = l_t L_t (1 - s_t),   d_log_decay = sum of l_t s_t,   d_state = a_1 u_1;
+ * where w_t is 0 its term of l_t is 0.  The sums over tokens and sequences are added in a fixed order: equal calls give equal bits.
+ * state as in the forward call; d_final_state, d_state: [B, C] fp32 (entry b, whatever slots says of state); d_log_decay: [C] fp32 or
+ * NULL; d_state is NULL where it is not wanted and may be d_final_state.  strides: of dh, x, decay_gate, input_gate, h, dx, d_decay_gate,
+ * d_input_gate.  Rows in no sequence get zeros.
+ */
+int sw_gated_recurrence_backward(const void* dh, const void* x, const void* decay_gate, const void* input_gate, const float* log_decay,
+                                 const void* h, const float* state, const float* d_final_state, void* dx, void* d_decay_gate,
+                                 void* d_input_gate, float* d_log_decay, float* d_state, const int32_t* slots, const int32_t* starts,
+                                 const sw_gated_recurrence_dims* dims, const sw_strides* strides, void* workspace,
+                                 int64_t workspace_bytes, void* hip_stream);
+int64_t sw_gated_recurrence_backward_workspace_bytes(const sw_gated_recurrence_dims* dims, int packed);
+
+/*
+ * Its form for one token of each of B requests (dims->T is 1), on a cache of states that is brought up to date in place.
+ * x, decay_gate, input_gate, h: [B, C], a request `batch` elements after the one before (token unused); state: [n_states, C] fp32; slots
+ * as above: a row whose entry is out of range gets zeros and touches no state.
+ */
+int sw_gated_recurrence_step(const void* x, const void* decay_gate, const void* input_gate, const float* log_decay, void* h, float* state,
+                             const int32_t* slots, const sw_gated_recurrence_dims* dims, const sw_strides* strides, void* hip_stream);
+
+/*
+ * Norms of the heads of queries and keys, and their rotation by position, in one pass.  For every token and head
+ *     n = x / sqrt(mean(x^2) + eps) * weight,      (y_i, y_j) = (n_i cos f - n_j sin f, n_i sin f + n_j cos f),  f = position * frequencies[k]
+ * for the `pairs` pairs (i, j) = (k, k + pairs) or, `interleaved`, (2k, 2k + 1); the elements from 2 * pairs on are not turned.
+ * q, q_out: [B, T, heads, d], k, k_out: [B, T, kv_heads, d] (strides: of q, k, q_out, k_out); weights: [d] fp32 or NULL (ones), one for all
+ * heads; frequencies: [pairs] fp32, radians a position, or NULL with pairs 0; positions: [B, T] int32, any value, contiguous, or NULL:
+ * a token's place in its sequence.  The angle is taken in 64 bits: far positions lose nothing.  q_out may be q and k_out may be k
+ * (same pointer and strides).  1 <= d <= 256, heads and kv_heads <= 65535 (SW_ERR_UNSUPPORTED beyond); eps >= 0 and finite;
+ * 2 * pairs <= d.
+ */
+typedef struct {
+    int64_t B, T;
+    int heads, kv_heads, d, pairs, interleaved;
+    int type;                           /* sw_type of q, k and their results and gradients */
+    float eps;
+} sw_head_norm_dims;
+
+int sw_head_norm(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* frequencies,
+                 const int32_t* positions, void* q_out, void* k_out, const sw_head_norm_dims* dims, const sw_strides* strides, void* hip_stream);
+
+/*
+ * Its backward pass, from the gradients dq, dk of the results and the forward call's inputs: q_grad, k_grad as q, k; q_weight_grad,
+ * k_weight_grad: [d] fp32, each or both NULL where they are not wanted.  The sums over tokens and heads are added in a fixed order.
+ * strides: of dq, dk, q, k, q_grad, k_grad.  q_grad may be dq or q, k_grad dk or k (same pointer and strides).
+ */
+int sw_head_norm_backward(const void* dq, const void* dk, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                          const float* frequencies, const int32_t* positions, void* q_grad, void* k_grad, float* q_weight_grad,
+                          float* k_weight_grad, const sw_head_norm_dims* dims, const sw_strides* strides, void* workspace,
+                          int64_t workspace_bytes, void* hip_stream);
+int64_t sw_head_norm_backward_workspace_bytes(const sw_head_norm_dims* dims);
+
+/*
+ * Low-rank adapters of many requests at once, beside a projection that they share (y, of sw_conv2d_nhwc say):
+ *     out[row] = y[row] + scales[s] * b[s] (a[s] x[row]),      s = slots[sequence of the row].
+ * x: rows of C_in elements, y, out: rows of C_out, x_stride, y_stride, out_stride apart; the rows are B sequences of T, or packed ones
+ * (starts [B+1] int32, T rows in all).  a: [n, rank, C_in], b: [n, C_out, rank], of the same type, contiguous; scales: [n] fp32 or NULL
+ * (ones); slots: [B] int32 (device) or NULL: sequence b has adapter b (n >= B then, else SW_ERR_SHAPE).  Several sequences may have one
+ * adapter.  Rows of a sequence whose entry is outside 0 ... n-1, and rows in no sequence, are copied.  Products are added in fp32, a[s] x is
+ * kept in fp32, and the result is rounded once.  out may be y (same pointer and stride); any other overlap is SW_ERR_ALIAS.
+ * 1 <= rank <= 256, C_in, C_out <= 2^20 (SW_ERR_UNSUPPORTED beyond); all rows below 2^31.
+ */
+typedef struct {
+    int64_t T;
+    int B, C_in, C_out, rank, n;
+    int type;                           /* sw_type of x, a, b, y and out */
+} sw_adapters_dims;
+
+int sw_adapters(const void* x, const void* a, const void* b, const void* y, const float* scales, const int32_t* slots,
+                const int32_t* starts, void* out, const sw_adapters_dims* dims, int64_t x_stride, int64_t y_stride, int64_t out_stride,
+                void* workspace, int64_t workspace_bytes, void* hip_stream);
+int64_t sw_adapters_workspace_bytes(const sw_adapters_dims* dims, int packed);
+
 /* Output extent of one axis; <= 0 means the filter does not fit (or bad arguments). */
 int64_t sw_out_dim(int64_t in, int k, int stride, int pad);
 

@@ -1,7 +1,7 @@
-"""Sliding Window Sum convolution and pooling for AMD Instinct MI355X (gfx950), and the layer norm and linear attention of
-sequence models on the same channel-last rows.
+"""Sliding Window Sum convolution and pooling for AMD Instinct MI355X (gfx950), and operators of
+sequence models on the same channel-last rows: layer norm, linear attention, a gated recurrence, norms of heads, adapters.
 
-``binding`` and ``layers`` wrap the C ABI of libswconv.so (``include/swconv.h``); ``inputs`` draws the seeded
+``binding``, ``layers`` and ``sequence`` wrap the C ABI of libswconv.so (``include/swconv.h``); ``inputs`` draws the seeded
 synthetic workloads; ``build`` compiles the library with hipcc.  Importing the package loads
 nothing: the library is opened on the first call.
 """
@@ -13,3 +13,5 @@ from .binding import (SW_POOL_AVG, SW_POOL_MAX, SwError, sw_conv1d, sw_conv2d, s
                       SW_PROBE_MFMA_F32, SW_PROBE_MFMA_I8, SW_PROBE_FMA_F32, SW_PROBE_FMA_MFMA_F32, SW_PROBE_MFMA_F32_FED, SW_PROBE_MFMA_F32_FED2, SW_PROBE_MFMA_BF16)
 from .layers import (sw_layer_norm, sw_layer_norm_backward, sw_linear_attention, sw_linear_attention_backward,  # noqa: F401
                      sw_linear_attention_step)
+from .sequence import (sw_adapters, sw_gated_recurrence, sw_gated_recurrence_backward, sw_gated_recurrence_step, sw_head_norm,  # noqa: F401
+                       sw_head_norm_backward)

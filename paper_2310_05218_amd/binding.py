@@ -27,6 +27,9 @@ EXPORTS = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2d_depthw
            "sw_layer_norm", "sw_layer_norm_backward", "sw_layer_norm_backward_workspace_bytes",
            "sw_linear_attention", "sw_linear_attention_workspace_bytes", "sw_linear_attention_backward",
            "sw_linear_attention_backward_workspace_bytes", "sw_linear_attention_step",
+           "sw_gated_recurrence", "sw_gated_recurrence_workspace_bytes", "sw_gated_recurrence_backward",
+           "sw_gated_recurrence_backward_workspace_bytes", "sw_gated_recurrence_step",
+           "sw_head_norm", "sw_head_norm_backward", "sw_head_norm_backward_workspace_bytes", "sw_adapters", "sw_adapters_workspace_bytes",
            "sw_probe", "sw_probe_ops", "sw_out_dim", "sw_out_dim_dilated", "sw_workspace_bytes", "sw_status_string", "sw_version", "sw_last_kernel")
 
 _lib = None
@@ -40,6 +43,22 @@ class SwStrides(ctypes.Structure):
 class SwLinearAttentionDims(ctypes.Structure):
     """sw_linear_attention_dims of include/swconv.h."""
     _fields_ = [("T", ctypes.c_int64), *((n, ctypes.c_int) for n in ("B", "heads", "kv_heads", "dk", "dv", "n_states", "type")), ("scale", ctypes.c_float)]
+
+
+class SwGatedRecurrenceDims(ctypes.Structure):
+    """sw_gated_recurrence_dims of include/swconv.h."""
+    _fields_ = [("T", ctypes.c_int64), ("C", ctypes.c_int64), *((n, ctypes.c_int) for n in ("B", "n_states", "type"))]
+
+
+class SwHeadNormDims(ctypes.Structure):
+    """sw_head_norm_dims of include/swconv.h."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64),
+                *((n, ctypes.c_int) for n in ("heads", "kv_heads", "d", "pairs", "interleaved", "type")), ("eps", ctypes.c_float)]
+
+
+class SwAdaptersDims(ctypes.Structure):
+    """sw_adapters_dims of include/swconv.h."""
+    _fields_ = [("T", ctypes.c_int64), *((n, ctypes.c_int) for n in ("B", "C_in", "C_out", "rank", "n", "type"))]
 
 
 class SwError(RuntimeError):
@@ -129,6 +148,28 @@ def lib() -> ctypes.CDLL:
         getattr(L, name).argtypes = [dims, i32]
     L.sw_linear_attention_step.restype = i32
     L.sw_linear_attention_step.argtypes = [vp] * 7 + [dims] + [strides] * 4 + [vp]
+    dims = ctypes.POINTER(SwGatedRecurrenceDims)
+    L.sw_gated_recurrence.restype = i32
+    L.sw_gated_recurrence.argtypes = [vp] * 9 + [dims, strides, vp, i64, vp]
+    L.sw_gated_recurrence_backward.restype = i32
+    L.sw_gated_recurrence_backward.argtypes = [vp] * 15 + [dims, strides, vp, i64, vp]
+    for name in ("sw_gated_recurrence_workspace_bytes", "sw_gated_recurrence_backward_workspace_bytes"):
+        getattr(L, name).restype = i64
+        getattr(L, name).argtypes = [dims, i32]
+    L.sw_gated_recurrence_step.restype = i32
+    L.sw_gated_recurrence_step.argtypes = [vp] * 7 + [dims, strides, vp]
+    dims = ctypes.POINTER(SwHeadNormDims)
+    L.sw_head_norm.restype = i32
+    L.sw_head_norm.argtypes = [vp] * 8 + [dims, strides, vp]
+    L.sw_head_norm_backward.restype = i32
+    L.sw_head_norm_backward.argtypes = [vp] * 12 + [dims, strides, vp, i64, vp]
+    L.sw_head_norm_backward_workspace_bytes.restype = i64
+    L.sw_head_norm_backward_workspace_bytes.argtypes = [dims]
+    dims = ctypes.POINTER(SwAdaptersDims)
+    L.sw_adapters.restype = i32
+    L.sw_adapters.argtypes = [vp] * 8 + [dims] + [i64] * 3 + [vp, i64, vp]
+    L.sw_adapters_workspace_bytes.restype = i64
+    L.sw_adapters_workspace_bytes.argtypes = [dims, i32]
     L.sw_probe.restype = i32
     L.sw_probe.argtypes = [i32, i32, vp]
     L.sw_probe_ops.restype = i64
@@ -312,7 +353,8 @@ def _bind_current_stream():
 
 # operations of the native short way (csrc/binding/sw_binding.cpp), in its order
 (_CONV1D, _POOL1D, _POOL2D, _CONV2D, _BIAS_RELU, _DILATED, _DEPTHWISE, _DEPTHWISE_BIAS_RELU, _DEPTHWISE_BF16, _S8, _S8_REQUANT, _S8_NHWC,
- _NHWC, _LAYER_NORM, _LAYER_NORM_BACKWARD, _ATTENTION, _ATTENTION_BACKWARD, _ATTENTION_STEP) = range(18)
+ _NHWC, _LAYER_NORM, _LAYER_NORM_BACKWARD, _ATTENTION, _ATTENTION_BACKWARD, _ATTENTION_STEP, _RECURRENCE,
+ _RECURRENCE_BACKWARD, _RECURRENCE_STEP, _HEAD_NORM, _HEAD_NORM_BACKWARD, _ADAPTERS) = range(24)
 _NATIVE_ENTRIES = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2d_bias_relu", "sw_conv2d_dilated", "sw_conv2d_depthwise",
                    "sw_conv2d_depthwise_bias_relu", "sw_conv2d_depthwise_bf16", "sw_conv2d_s8", "sw_conv2d_s8_requant", "sw_conv2d_s8_nhwc",
                    "sw_conv2d_s8_nhwc_requant", "sw_conv2d_nhwc", "sw_conv2d_bf16_nhwc", "sw_conv2d_f16_nhwc",

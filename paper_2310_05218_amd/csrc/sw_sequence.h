@@ -1,0 +1,80 @@
+// Declarations shared by the translation units of the gated recurrence, the norms of heads with their rotation, and the adapters:
+// launchers (validated arguments in, the HIP error of the launch out).
+#pragma once
+
+#include "sw_layers.h"
+
+namespace swconv {
+
+// ---- gated linear recurrence ---------------------------------------------------------------------------------------------------
+// rows of channels [batch, token, C]: strides in elements
+struct Channels {
+    const void* p;
+    int64_t batch, token;
+};
+struct RecurrenceBatch {
+    const float* log_decay;             // [C]
+    const int32_t *starts, *slots;      // packed sequences: [B + 1]; entries of the states: [B]; null: none, in order
+    int64_t T;
+    int C, B, n_states;
+};
+struct RecurrenceArgs {
+    Channels x, decay_gate, input_gate, h;
+    const float* state;
+    float* final_state;
+    RecurrenceBatch n;
+    void* work;
+};
+struct RecurrenceBackwardArgs {
+    Channels dh, x, decay_gate, input_gate, h, dx, d_decay_gate, d_input_gate;
+    const float *state, *d_final_state; // state: entries by slots; d_final_state, d_state: by sequence
+    float *d_log_decay, *d_state;       // null: not wanted
+    RecurrenceBatch n;
+    void* work;
+};
+struct RecurrenceStepArgs {
+    Channels x, decay_gate, input_gate, h;
+    float* state;
+    RecurrenceBatch n;
+};
+int64_t    recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek);
+int64_t    recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek);
+hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st);
+hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, hipStream_t st);
+hipError_t launch_recurrence_step(const RecurrenceStepArgs& a, int ek, hipStream_t st);
+
+// ---- norms of heads, with the rotation by positions -------------------------------------------------------------------------------
+struct HeadNormSide {                   // the queries or the keys
+    AttentionOperand x, dy, y;          // [batch, token, head, D]; dy: backward only; y: the result, backward the gradient of x
+    const float* weight;                // [D] or null: ones
+    float* dweight;                     // backward; null: not wanted
+    int heads;
+};
+struct HeadNormArgs {
+    HeadNormSide side[2];
+    const float* frequencies;           // [pairs] or null: no rotation
+    const int32_t* positions;           // [B * T] or null: places in the sequence
+    int64_t B, T;
+    int D, pairs;
+    bool interleaved;
+    float eps;
+    void* work;
+};
+int64_t    head_norm_backward_workspace(int64_t rows, int heads, int kv_heads, int D);
+hipError_t launch_head_norm(const HeadNormArgs& a, int ek, hipStream_t st);
+hipError_t launch_head_norm_backward(const HeadNormArgs& a, int ek, hipStream_t st);
+
+// ---- low-rank adapters --------------------------------------------------------------------------------------------------------------
+struct AdapterArgs {
+    const void *x, *a, *b, *y;          // x: rows of C_in; a: [n, rank, C_in]; b: [n, C_out, rank]; y, out: rows of C_out
+    void* out;
+    const float* scales;                // [n] or null: ones
+    const int32_t *slots, *starts;      // the sequences' adapters (null: in order) and, packed, first rows
+    int64_t T, x_stride, y_stride, out_stride;
+    int B, C_in, C_out, rank, n;
+    void* work;
+};
+int64_t    adapters_workspace(const AdapterArgs& a, int ek);
+hipError_t launch_adapters(const AdapterArgs& a, int ek, hipStream_t st);
+
+}  // namespace swconv

@@ -1,0 +1,312 @@
+// C entry points of the gated recurrence, the norms of heads and the adapters: host-side validation, then the launchers.  Every argument error
+// is reported before anything is enqueued; scratch memory is the caller's.
+#include "../../include/swconv.h"
+
+#include "sw_layers_check.h"
+#include "sw_sequence.h"
+
+using namespace swconv;
+
+namespace {
+
+bool known(int type) { return type == SW_F32 || type == SW_BF16 || type == SW_F16; }
+
+// Where a tensor's elements lie: `width` of every `period`, or, period 0, anywhere in its span.
+struct Places {
+    Span span;
+    int64_t width = 0, period = 0;      // elements
+};
+Places places(const Tensor4& t, int width, int64_t heads, int64_t size)
+{
+    const AttentionOperand& o = t.op;
+    Places p{span_of(o.p, t.elements, size)};
+    const int64_t period = o.token ? o.token : o.batch, reach = o.head * (heads - 1) + width;
+    if (period >= reach && (!o.token || o.batch % o.token == 0)) p.width = reach, p.period = period;
+    return p;
+}
+Places places(const void* p, int64_t elements, int64_t size) { return Places{span_of(p, elements, size)}; }
+Places places(const void* p, int64_t elements, int64_t width, int64_t stride, int64_t size) { return Places{span_of(p, elements, size), width, stride}; }
+
+// Whether two tensors have memory in common; rows of one stride that lie interleaved have none.
+bool overlap(const Places& a, const Places& b, int64_t size)
+{
+    if (!meet(a.span, b.span)) return false;
+    if (!a.period || a.period != b.period) return true;
+    const int64_t bytes = a.period * size;
+    int64_t off = (int64_t)(b.span.at - a.span.at) % bytes;     // (unsigned difference: as a two's complement one it has the sign of b - a)
+    if (off < 0) off += bytes;
+    return off < a.width * size || bytes - off < b.width * size;
+}
+bool same(const Tensor4& a, const Tensor4& b)
+{
+    return a.op.p == b.op.p && a.op.batch == b.op.batch && a.op.token == b.op.token && a.op.head == b.op.head;
+}
+
+Channels channels(const Tensor4& t) { return Channels{t.op.p, t.op.batch, t.op.token}; }
+
+int check_recurrence(const sw_gated_recurrence_dims& d, bool packed)
+{
+    const int64_t batches = packed ? 1 : d.B;
+    if (d.T <= 0 || d.B <= 0 || d.C <= 0 || d.n_states < 0 || d.T > kMaxExtent / batches || (int64_t)d.B + 2 > 0x7fffffff) return SW_ERR_SHAPE;
+    if (d.C > kMaxChannels || !known(d.type)) return SW_ERR_UNSUPPORTED;
+    if (d.C > kMaxExtent / ((int64_t)d.n_states + d.B) || d.T * batches > kMaxExtent / d.C) return SW_ERR_SHAPE;
+    return SW_OK;
+}
+RecurrenceBatch batch_of(const sw_gated_recurrence_dims& d, const float* log_decay, const int32_t* starts, const int32_t* slots)
+{
+    return RecurrenceBatch{log_decay, starts, slots, d.T, (int)d.C, d.B, d.n_states};
+}
+
+int check_heads(const sw_head_norm_dims& d)
+{
+    if (d.B <= 0 || d.T <= 0 || d.heads <= 0 || d.kv_heads <= 0 || d.d <= 0 || d.pairs < 0 || 2 * (int64_t)d.pairs > d.d || !(d.eps >= 0.f) ||
+        !std::isfinite(d.eps) || d.T > kMaxExtent / d.B)
+        return SW_ERR_SHAPE;
+    if (d.d > 256 || d.heads > 65535 || d.kv_heads > 65535 || !known(d.type)) return SW_ERR_UNSUPPORTED;
+    if (d.B * d.T > kMaxExtent / ((int64_t)(d.heads + d.kv_heads) * d.d)) return SW_ERR_SHAPE;
+    return SW_OK;
+}
+
+int check_adapters(const sw_adapters_dims& d, bool packed)
+{
+    if (d.T <= 0 || d.B <= 0 || d.C_in <= 0 || d.C_out <= 0 || d.rank <= 0 || d.n <= 0 || (int64_t)d.B + 2 > 0x7fffffff ||
+        d.T > 0x7fffffff / (packed ? 1 : d.B))
+        return SW_ERR_SHAPE;
+    if (d.rank > 256 || d.C_in > kMaxChannels || d.C_out > kMaxChannels || !known(d.type)) return SW_ERR_UNSUPPORTED;
+    if ((int64_t)d.n > kMaxExtent / ((int64_t)d.rank * (d.C_in > d.C_out ? d.C_in : d.C_out))) return SW_ERR_SHAPE;
+    return SW_OK;
+}
+AdapterArgs adapter_args(const sw_adapters_dims& d, const int32_t* starts)
+{
+    AdapterArgs a{};
+    a.starts = starts, a.T = d.T, a.B = d.B, a.C_in = d.C_in, a.C_out = d.C_out, a.rank = d.rank, a.n = d.n;
+    return a;
+}
+const int32_t* const kPacked = reinterpret_cast<const int32_t*>(16);    // an address that only says that starts is given
+
+}  // namespace
+
+extern "C" {
+
+int64_t sw_gated_recurrence_workspace_bytes(const sw_gated_recurrence_dims* dims, int packed)
+{
+    if (!dims || check_recurrence(*dims, packed != 0) != SW_OK) return 0;
+    return align16(recurrence_workspace(batch_of(*dims, nullptr, nullptr, nullptr), packed != 0, dims->type));
+}
+
+int sw_gated_recurrence(const void* x, const void* decay_gate, const void* input_gate, const float* log_decay, void* h, const float* state,
+                        float* final_state, const int32_t* slots, const int32_t* starts, const sw_gated_recurrence_dims* dims,
+                        const sw_strides* strides, void* workspace, int64_t workspace_bytes, void* hip_stream)
+{
+    if (!x || !decay_gate || !input_gate || !log_decay || !h || !dims || !strides) return SW_ERR_NULL;
+    const sw_gated_recurrence_dims d = *dims;
+    if (const int rc = check_recurrence(d, starts != nullptr)) return rc;
+    const int64_t batches = starts ? 1 : d.B;
+    const int C = (int)d.C;
+    Tensor4 tx, tr, ti, th;
+    if (!tx.set(x, strides, batches, d.T, 1, C, 1) || !tr.set(decay_gate, strides + 1, batches, d.T, 1, C, 1) ||
+        !ti.set(input_gate, strides + 2, batches, d.T, 1, C, 1) || !th.set(h, strides + 3, batches, d.T, 1, C, 1, true) ||
+        (starts && d.T > 0x7fffffff) || ((state || final_state) && (d.n_states <= 0 || (!slots && d.n_states < d.B))))
+        return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : {x, decay_gate, input_gate, static_cast<const void*>(h)})
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    for (const void* p : {static_cast<const void*>(log_decay), static_cast<const void*>(state), static_cast<const void*>(final_state),
+                          static_cast<const void*>(slots), static_cast<const void*>(starts)})
+        if (misaligned(p, 4)) return SW_ERR_ALIGN;
+    const int64_t need = sw_gated_recurrence_workspace_bytes(dims, starts != nullptr), states = (int64_t)d.n_states * C;
+    if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
+    const Places in[7] = {places(tx, C, 1, size), places(tr, C, 1, size), places(ti, C, 1, size), places(log_decay, C, 4),
+                          places(state, states, 4), places(slots, d.B, 4), places(starts, (int64_t)d.B + 1, 4)};
+    const Places out[3] = {places(th, C, 1, size), places(final_state, states, 4), places(workspace, need, 1)};
+    for (int o = 0; o < 3; ++o) {
+        for (int i = 0; i < 7; ++i)
+            if (overlap(out[o], in[i], size) && !(o == 1 && i == 4 && state == final_state)) return SW_ERR_ALIAS;
+        for (int p = 0; p < o; ++p)
+            if (overlap(out[o], out[p], size)) return SW_ERR_ALIAS;
+    }
+    const RecurrenceArgs a{channels(tx), channels(tr), channels(ti), channels(th), state, final_state, batch_of(d, log_decay, starts, slots), workspace};
+    return launch_status(launch_recurrence(a, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+int64_t sw_gated_recurrence_backward_workspace_bytes(const sw_gated_recurrence_dims* dims, int packed)
+{
+    if (!dims || check_recurrence(*dims, packed != 0) != SW_OK) return 0;
+    return align16(recurrence_backward_workspace(batch_of(*dims, nullptr, nullptr, nullptr), packed != 0, dims->type));
+}
+
+int sw_gated_recurrence_backward(const void* dh, const void* x, const void* decay_gate, const void* input_gate, const float* log_decay,
+                                 const void* h, const float* state, const float* d_final_state, void* dx, void* d_decay_gate,
+                                 void* d_input_gate, float* d_log_decay, float* d_state, const int32_t* slots, const int32_t* starts,
+                                 const sw_gated_recurrence_dims* dims, const sw_strides* strides, void* workspace, int64_t workspace_bytes,
+                                 void* hip_stream)
+{
+    if (!dh || !x || !decay_gate || !input_gate || !log_decay || !h || !dx || !d_decay_gate || !d_input_gate || !dims || !strides) return SW_ERR_NULL;
+    const sw_gated_recurrence_dims d = *dims;
+    if (const int rc = check_recurrence(d, starts != nullptr)) return rc;
+    const int64_t batches = starts ? 1 : d.B;
+    const int C = (int)d.C;
+    const void* const tensors[8] = {dh, x, decay_gate, input_gate, h, dx, d_decay_gate, d_input_gate};
+    Tensor4 t[8];
+    for (int i = 0; i < 8; ++i)
+        if (!t[i].set(tensors[i], strides + i, batches, d.T, 1, C, 1, i >= 5)) return SW_ERR_SHAPE;
+    if ((starts && d.T > 0x7fffffff) || (state && (d.n_states <= 0 || (!slots && d.n_states < d.B)))) return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : tensors)
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    for (const void* p : {static_cast<const void*>(log_decay), static_cast<const void*>(state), static_cast<const void*>(d_final_state),
+                          static_cast<const void*>(d_log_decay), static_cast<const void*>(d_state), static_cast<const void*>(slots),
+                          static_cast<const void*>(starts)})
+        if (misaligned(p, 4)) return SW_ERR_ALIGN;
+    const int64_t need = sw_gated_recurrence_backward_workspace_bytes(dims, starts != nullptr), each = (int64_t)d.B * C;
+    if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
+    Places in[10] = {Places{}, Places{}, Places{}, Places{}, Places{}, places(log_decay, C, 4), places(state, (int64_t)d.n_states * C, 4),
+                     places(d_final_state, each, 4), places(slots, d.B, 4), places(starts, (int64_t)d.B + 1, 4)};
+    Places out[6] = {Places{}, Places{}, Places{}, places(d_log_decay, C, 4), places(d_state, each, 4), places(workspace, need, 1)};
+    for (int i = 0; i < 8; ++i) (i < 5 ? in[i] : out[i - 5]) = places(t[i], C, 1, size);
+    for (int o = 0; o < 6; ++o) {
+        for (int i = 0; i < 10; ++i)
+            if (overlap(out[o], in[i], size) && !(o == 4 && i == 7 && d_state == d_final_state)) return SW_ERR_ALIAS;
+        for (int p = 0; p < o; ++p)
+            if (overlap(out[o], out[p], size)) return SW_ERR_ALIAS;
+    }
+    const RecurrenceBackwardArgs a{channels(t[0]), channels(t[1]), channels(t[2]), channels(t[3]), channels(t[4]), channels(t[5]), channels(t[6]),
+                                   channels(t[7]), state, d_final_state, d_log_decay, d_state, batch_of(d, log_decay, starts, slots), workspace};
+    return launch_status(launch_recurrence_backward(a, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+int sw_gated_recurrence_step(const void* x, const void* decay_gate, const void* input_gate, const float* log_decay, void* h, float* state,
+                             const int32_t* slots, const sw_gated_recurrence_dims* dims, const sw_strides* strides, void* hip_stream)
+{
+    if (!x || !decay_gate || !input_gate || !log_decay || !h || !state || !dims || !strides) return SW_ERR_NULL;
+    const sw_gated_recurrence_dims d = *dims;
+    if (const int rc = check_recurrence(d, false)) return rc;
+    const int C = (int)d.C;
+    Tensor4 tx, tr, ti, th;
+    if (d.T != 1 || !tx.set(x, strides, d.B, 1, 1, C, 1) || !tr.set(decay_gate, strides + 1, d.B, 1, 1, C, 1) ||
+        !ti.set(input_gate, strides + 2, d.B, 1, 1, C, 1) || !th.set(h, strides + 3, d.B, 1, 1, C, 1, true) || d.n_states <= 0 ||
+        (!slots && d.n_states < d.B))
+        return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : {x, decay_gate, input_gate, static_cast<const void*>(h)})
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    if (misaligned(log_decay, 4) || misaligned(state, 4) || misaligned(slots, 4)) return SW_ERR_ALIGN;
+    const Places in[5] = {places(tx, C, 1, size), places(tr, C, 1, size), places(ti, C, 1, size), places(log_decay, C, 4), places(slots, d.B, 4)};
+    const Places out[2] = {places(th, C, 1, size), places(state, (int64_t)d.n_states * C, 4)};
+    for (const Places& o : out)
+        for (const Places& i : in)
+            if (overlap(o, i, size)) return SW_ERR_ALIAS;
+    if (overlap(out[0], out[1], size)) return SW_ERR_ALIAS;
+    const RecurrenceStepArgs a{channels(tx), channels(tr), channels(ti), channels(th), state, batch_of(d, log_decay, nullptr, slots)};
+    return launch_status(launch_recurrence_step(a, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+int sw_head_norm(const void* q, const void* k, const float* q_weight, const float* k_weight, const float* frequencies, const int32_t* positions,
+                 void* q_out, void* k_out, const sw_head_norm_dims* dims, const sw_strides* strides, void* hip_stream)
+{
+    if (!q || !k || !q_out || !k_out || !dims || !strides || (dims->pairs > 0 && !frequencies)) return SW_ERR_NULL;
+    const sw_head_norm_dims d = *dims;
+    if (const int rc = check_heads(d)) return rc;
+    Tensor4 tq, tk, oq, ok;
+    if (!tq.set(q, strides, d.B, d.T, d.heads, d.d, 1) || !tk.set(k, strides + 1, d.B, d.T, d.kv_heads, d.d, 1) ||
+        !oq.set(q_out, strides + 2, d.B, d.T, d.heads, d.d, 1, true) || !ok.set(k_out, strides + 3, d.B, d.T, d.kv_heads, d.d, 1, true))
+        return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : {q, k, static_cast<const void*>(q_out), static_cast<const void*>(k_out)})
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    if (misaligned(q_weight, 4) || misaligned(k_weight, 4) || misaligned(frequencies, 4) || misaligned(positions, 4)) return SW_ERR_ALIGN;
+    const Places in[6] = {places(tq, d.d, d.heads, size), places(tk, d.d, d.kv_heads, size), places(q_weight, d.d, 4), places(k_weight, d.d, 4),
+                          places(frequencies, d.pairs, 4), places(positions, d.B * d.T, 4)};
+    const Places out[2] = {places(oq, d.d, d.heads, size), places(ok, d.d, d.kv_heads, size)};
+    for (int o = 0; o < 2; ++o)
+        for (int i = 0; i < 6; ++i)
+            if (overlap(out[o], in[i], size) && !(o == i && (o ? same(ok, tk) : same(oq, tq)))) return SW_ERR_ALIAS;
+    if (overlap(out[0], out[1], size)) return SW_ERR_ALIAS;
+    const AttentionOperand none{};
+    const HeadNormArgs a{{{tq.op, none, oq.op, q_weight, nullptr, d.heads}, {tk.op, none, ok.op, k_weight, nullptr, d.kv_heads}},
+                         frequencies, positions, d.B, d.T, d.d, d.pairs, d.interleaved != 0, d.eps, nullptr};
+    return launch_status(launch_head_norm(a, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+int64_t sw_head_norm_backward_workspace_bytes(const sw_head_norm_dims* dims)
+{
+    if (!dims || check_heads(*dims) != SW_OK) return 0;
+    return align16(head_norm_backward_workspace(dims->B * dims->T, dims->heads, dims->kv_heads, dims->d));
+}
+
+int sw_head_norm_backward(const void* dq, const void* dk, const void* q, const void* k, const float* q_weight, const float* k_weight,
+                          const float* frequencies, const int32_t* positions, void* q_grad, void* k_grad, float* q_weight_grad,
+                          float* k_weight_grad, const sw_head_norm_dims* dims, const sw_strides* strides, void* workspace,
+                          int64_t workspace_bytes, void* hip_stream)
+{
+    if (!dq || !dk || !q || !k || !q_grad || !k_grad || !dims || !strides || (dims->pairs > 0 && !frequencies)) return SW_ERR_NULL;
+    const sw_head_norm_dims d = *dims;
+    if (const int rc = check_heads(d)) return rc;
+    const void* const tensors[6] = {dq, dk, q, k, q_grad, k_grad};
+    Tensor4 t[6];
+    for (int i = 0; i < 6; ++i)
+        if (!t[i].set(tensors[i], strides + i, d.B, d.T, i % 2 ? d.kv_heads : d.heads, d.d, 1, i >= 4)) return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : tensors)
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    if (misaligned(q_weight, 4) || misaligned(k_weight, 4) || misaligned(frequencies, 4) || misaligned(positions, 4) || misaligned(q_weight_grad, 4) ||
+        misaligned(k_weight_grad, 4))
+        return SW_ERR_ALIGN;
+    const int64_t need = q_weight_grad || k_weight_grad ? sw_head_norm_backward_workspace_bytes(dims) : 0;
+    if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
+    Places in[8] = {Places{}, Places{}, Places{}, Places{}, places(q_weight, d.d, 4), places(k_weight, d.d, 4), places(frequencies, d.pairs, 4),
+                    places(positions, d.B * d.T, 4)};
+    Places out[5] = {Places{}, Places{}, places(q_weight_grad, d.d, 4), places(k_weight_grad, d.d, 4), places(workspace, need, 1)};
+    for (int i = 0; i < 6; ++i) (i < 4 ? in[i] : out[i - 4]) = places(t[i], d.d, i % 2 ? d.kv_heads : d.heads, size);
+    for (int o = 0; o < 5; ++o) {
+        for (int i = 0; i < 8; ++i) {
+            const bool replaces = o < 2 && i < 4 && i % 2 == o && same(t[4 + o], t[i]);
+            if (overlap(out[o], in[i], size) && !replaces) return SW_ERR_ALIAS;
+        }
+        for (int p = 0; p < o; ++p)
+            if (overlap(out[o], out[p], size)) return SW_ERR_ALIAS;
+    }
+    const HeadNormArgs a{{{t[2].op, t[0].op, t[4].op, q_weight, q_weight_grad, d.heads}, {t[3].op, t[1].op, t[5].op, k_weight, k_weight_grad, d.kv_heads}},
+                         frequencies, positions, d.B, d.T, d.d, d.pairs, d.interleaved != 0, d.eps, workspace};
+    return launch_status(launch_head_norm_backward(a, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+int64_t sw_adapters_workspace_bytes(const sw_adapters_dims* dims, int packed)
+{
+    if (!dims || check_adapters(*dims, packed != 0) != SW_OK) return 0;
+    return align16(adapters_workspace(adapter_args(*dims, packed ? kPacked : nullptr), dims->type));
+}
+
+int sw_adapters(const void* x, const void* a, const void* b, const void* y, const float* scales, const int32_t* slots, const int32_t* starts,
+                void* out, const sw_adapters_dims* dims, int64_t x_stride, int64_t y_stride, int64_t out_stride, void* workspace,
+                int64_t workspace_bytes, void* hip_stream)
+{
+    if (!x || !a || !b || !y || !out || !dims) return SW_ERR_NULL;
+    const sw_adapters_dims d = *dims;
+    if (const int rc = check_adapters(d, starts != nullptr)) return rc;
+    const int64_t rows = starts ? d.T : d.T * d.B;
+    int64_t nx, ny, no;
+    if (!row_extent(rows, d.C_in, x_stride, &nx) || !row_extent(rows, d.C_out, y_stride, &ny) || !row_extent(rows, d.C_out, out_stride, &no) ||
+        (!slots && d.n < d.B))
+        return SW_ERR_SHAPE;
+    const int size = elem_size(d.type);
+    for (const void* p : {x, a, b, y, static_cast<const void*>(out)})
+        if (misaligned(p, size)) return SW_ERR_ALIGN;
+    if (misaligned(scales, 4) || misaligned(slots, 4) || misaligned(starts, 4)) return SW_ERR_ALIGN;
+    const int64_t need = sw_adapters_workspace_bytes(dims, starts != nullptr);
+    if (!workspace_fits(workspace, workspace_bytes, need)) return SW_ERR_WORKSPACE;
+    const int64_t ranks = (int64_t)d.n * d.rank;
+    const Places in[7] = {places(x, nx, d.C_in, x_stride, size), places(a, ranks * d.C_in, size), places(b, ranks * d.C_out, size),
+                          places(y, ny, d.C_out, y_stride, size), places(scales, d.n, 4), places(slots, d.B, 4), places(starts, (int64_t)d.B + 1, 4)};
+    const Places to[2] = {places(out, no, d.C_out, out_stride, size), places(workspace, need, 1)};
+    for (int o = 0; o < 2; ++o)
+        for (int i = 0; i < 7; ++i)
+            if (overlap(to[o], in[i], size) && !(o == 0 && i == 3 && out == y && out_stride == y_stride)) return SW_ERR_ALIAS;
+    if (overlap(to[0], to[1], size)) return SW_ERR_ALIAS;
+    AdapterArgs args = adapter_args(d, starts);
+    args.x = x, args.a = a, args.b = b, args.y = y, args.out = out, args.scales = scales, args.slots = slots, args.work = workspace;
+    args.x_stride = x_stride, args.y_stride = y_stride, args.out_stride = out_stride;
+    return launch_status(launch_adapters(args, d.type, static_cast<hipStream_t>(hip_stream)));
+}
+
+}  // extern "C"
