@@ -1,7 +1,7 @@
 // The terms of the gated recurrence of one token and channel, from its two gates:
 //     s = sigmoid(r), L = log_decay s, a = e^L, w = sqrt(1 - a^2), p = sigmoid(i).
 // e^x is 2^(x log2 e): the product's rounding is an error of |x| units of the result's last place, which fp32 tensors get back from its remainder.
-// 1 - a^2 = -(e^u - 1), u = 2 L, loses its leading digits to the subtraction where a is near 1: there it is the series of e^u - 1.
+// 1 - a^2 loses its leading digits to the subtraction where a is near 1: there it is the series of 1 - e^(2L).
 #pragma once
 
 #include "sw_layers.h"
@@ -19,26 +19,33 @@ __device__ __forceinline__ float exp_of(float x)
     return fabsf(t) < 128.f ? __builtin_fmaf(e * kLn2, low, e) : e;
 }
 
-// -(e^u - 1) for u <= 0, where a2 = e^u.  The series' first term that is left out is below 2^-25 of the sum at either border, the subtraction's
-// error below 2^-18 (half a step of 16-bit formats is 2^-12 at least), EXACT below 2^-22.
+// 1 - e^(2L) for L <= 0, a = e^L: for L near 0 -L times the series of (e^(2L) - 1) / L, whose first term that is left out is below 2^-24 of the sum at the border;
+// beyond, the subtraction, whose error is below 2^-17 of it there (w has half of that; half a step of 16-bit formats is 2^-12 at least), EXACT below 2^-22.
 template <bool EXACT>
-__device__ __forceinline__ float one_minus(float u, float a2)
+__device__ __forceinline__ float one_minus_square(float L, float a)
 {
-    constexpr float kBorder = EXACT ? -0.5f : -0.03125f;
+    constexpr float kBorder = EXACT ? -0.25f : -0.015625f;
     float q;
     if constexpr (EXACT) {
-        q = 2.48015873e-5f;                             // 1/8!
-        q = __builtin_fmaf(q, u, 1.98412698e-4f);
-        q = __builtin_fmaf(q, u, 1.38888889e-3f);
-        q = __builtin_fmaf(q, u, 8.33333333e-3f);
-        q = __builtin_fmaf(q, u, 4.16666667e-2f);
+        q = 6.34920635e-3f;                             // 2^8 / 8!
+        q = __builtin_fmaf(q, L, 2.53968254e-2f);
+        q = __builtin_fmaf(q, L, 8.88888889e-2f);
+        q = __builtin_fmaf(q, L, 0.266666667f);
+        q = __builtin_fmaf(q, L, 0.666666667f);         // 2^4 / 4!
+        q = __builtin_fmaf(q, L, 1.33333333f);
     } else {
-        q = 4.16666667e-2f;                             // 1/4!
+        q = __builtin_fmaf(0.666666667f, L, 1.33333333f);
     }
-    q = __builtin_fmaf(q, u, 0.166666667f);
-    q = __builtin_fmaf(q, u, 0.5f);
-    q = __builtin_fmaf(q, u, 1.f);
-    return u > kBorder ? -u * q : 1.f - a2;
+    q = __builtin_fmaf(q, L, 2.f);
+    q = __builtin_fmaf(q, L, 2.f);
+    return L > kBorder ? -L * q : __builtin_fmaf(-a, a, 1.f);
+}
+
+template <int EK>
+__device__ __forceinline__ float decay_of(float log_decay, float r)
+{
+    constexpr bool EXACT = EK == kElemF32;
+    return exp_of<EXACT>(log_decay * __builtin_amdgcn_rcpf(1.f + exp_of<EXACT>(-r)));
 }
 
 template <int EK>
@@ -52,7 +59,7 @@ struct Gate {
         s = __builtin_amdgcn_rcpf(1.f + es), p = __builtin_amdgcn_rcpf(1.f + ep);
         L = log_decay * s;
         a = exp_of<EXACT>(L);
-        w = __builtin_amdgcn_sqrtf(one_minus<EXACT>(2.f * L, a * a));
+        w = __builtin_amdgcn_sqrtf(one_minus_square<EXACT>(L, a));
     }
     // 1 - s and 1 - p, to fp32's bits at both ends
     __device__ __forceinline__ float shut_s(float r) const { return r > 0.f ? es * s : 1.f - s; }

@@ -1,108 +1,270 @@
-// Gated linear recurrence: a thread a channel of a sequence, token after token.
-#include "sw_gates.h"
-#include "sw_sequence.h"
+// Gated linear recurrence.
+#include <initializer_list>
+
+#include "sw_scan.h"
 
 namespace swconv {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kForwardRows = 8;
 
-__device__ __forceinline__ int64_t clamped(int64_t v, int64_t most) { return v < 0 ? 0 : v > most ? most : v; }
-
-struct Rows {
-    int64_t first, last, left, right;       // of the sequence; zeros go to [left, first) and [last, right)
-    int entry;                              // of state; -1: none
-};
-__device__ __forceinline__ Rows rows_of(const RecurrenceBatch& n, int b)
+// A tile of V channels a lane: decays and terms of its rows in registers, read once, the carry, then the rows' states.
+template <int EK, int V, bool PACKED>
+__global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu(8))) void recurrence_kernel(RecurrenceArgs p, Tiles tiles)
 {
-    Rows r;
-    if (n.starts) {
-        r.first = clamped(n.starts[b], n.T), r.last = clamped(n.starts[b + 1], n.T);
-        r.left = b == 0 ? 0 : r.first, r.right = b == n.B - 1 ? n.T : r.last;
-    } else {
-        r.first = r.left = 0, r.last = r.right = n.T;
+    typedef Lane<EK, V> L;
+    typedef typename L::T T;
+    constexpr int R = kForwardRows;
+    __shared__ float2 pairs[kMostWaves][V][64], met[kMostWaves][V][64];
+    __shared__ unsigned ticket;
+    const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
+    const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = tiles.waves;
+    // (the last lanes of a width that is no whole number of groups share channels, with equal results)
+    int channel = at.group * group_width<V>() + lane * V;
+    channel = channel < p.n.C - V ? channel : p.n.C - V;
+    const int64_t first = ((int64_t)at.segment * waves + wave) * R, left = p.n.T - first;
+    const int rows = left < 0 ? 0 : left < R ? (int)left : R;
+    float log_decay[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]);
+    typename L::vec x[R], r[R], i[R];
+    L::template load<R>(p.decay_gate, at.batch, first, p.n.T, channel, r);
+    L::template load<R>(p.input_gate, at.batch, first, p.n.T, channel, i);
+    L::template load<R>(p.x, at.batch, first, p.n.T, channel, x);
+    PackedRows packed{0, 0, 0, 0, -1};
+    if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
+    float a[R][V], b[R][V];
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gate<EK> g(log_decay[v], (float)r[k][v], (float)i[k][v]);
+            a[k][v] = g.a, b[k][v] = g.w * g.p * (float)x[k][v];
+        }
+    if (rows < R)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k >= rows)
+#pragma unroll
+                for (int v = 0; v < V; ++v) a[k][v] = 1.f, b[k][v] = 0.f;
+    // states that sequences begin from are part of their first term: they are read before any last state is written
+    auto begin = [&](int k, int entry) {
+        if (p.state && entry >= 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) b[k][v] = __builtin_fmaf(a[k][v], p.state[(int64_t)entry * p.n.C + channel + v], b[k][v]);
+    };
+    if constexpr (PACKED) {
+        if (packed.begins | packed.outside)
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (packed.begins >> k & 1) begin(k, __builtin_amdgcn_readlane(packed.entry, k));
+                if (packed.outside >> k & 1)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) b[k][v] = 0.f;
+            }
+    } else if (first == 0) {
+        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        begin(0, entry < p.n.n_states ? entry : -1);
     }
-    r.entry = n.slots ? n.slots[b] : b;
-    if (r.entry < 0 || r.entry >= n.n_states) r.entry = -1;
-    return r;
+    const unsigned cut = packed.begins | packed.outside;
+    auto next = [&](int k, int v, float c) { return __builtin_fmaf(a[k][v], PACKED && (cut >> k & 1) ? 0.f : c, b[k][v]); };
+    float A[V], B[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        A[v] = 1.f, B[v] = 0.f;
+#pragma unroll
+        for (int k = 0; k < R; ++k) A[v] *= a[k][v], B[v] = next(k, v, B[v]);
+        if (PACKED && cut) A[v] = kCut;
+        pairs[wave][v][lane] = make_float2(A[v], B[v]);
+    }
+    __syncthreads();
+    float h[V];
+    carry_in<V>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, h);
+    auto keep = [&](int entry) {
+        if (p.final_state && entry >= 0)
+#pragma unroll
+            for (int v = 0; v < V; ++v) p.final_state[(int64_t)entry * p.n.C + channel + v] = h[v];
+    };
+    T* out = static_cast<T*>(const_cast<void*>(p.h.p)) + at.batch * p.h.batch + first * p.h.token;
+#pragma unroll
+    for (int k = 0; k < R; ++k, out += p.h.token) {
+        if (k >= rows) continue;
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = next(k, v, h[v]);
+        L::store(out + channel, h);
+        if (PACKED && (packed.ends >> k & 1)) keep(__builtin_amdgcn_readlane(packed.entry, k));
+    }
+    if constexpr (PACKED) {
+        // (their last states are their first; in place there is nothing to do)
+        if (p.final_state && p.final_state != p.state && wave == 0)
+            for_empty(p.n, tiles, at.segment, [&](int, int entry) {
+                if (entry < 0) return;
+#pragma unroll
+                for (int v = 0; v < V; ++v) h[v] = p.state ? p.state[(int64_t)entry * p.n.C + channel + v] : 0.f;
+                keep(entry);
+            });
+    } else if (rows > 0 && first + rows == p.n.T) {
+        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        keep(entry < p.n.n_states ? entry : -1);
+    }
 }
+
+constexpr int kBackwardRows = 8;
+
+// The same backwards in time: what a token passes on to the one before is c' = a (dh + c).  A workgroup's first wavefront has its last rows.
+template <int EK, int V, bool PACKED>
+__global__ __launch_bounds__(64 * kMostWaves) void recurrence_backward_kernel(RecurrenceBackwardArgs p, Tiles tiles, float* partial)
+{
+    typedef Lane<EK, V> L;
+    typedef typename L::T T;
+    constexpr int R = kBackwardRows;
+    __shared__ float2 pairs[kMostWaves][V][64], met[kMostWaves][V][64];
+    __shared__ unsigned ticket;
+    const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
+    const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
+    const int64_t part = at.segment * tiles.batches + at.batch, segment = tiles.segments - 1 - at.segment;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = tiles.waves;
+    int channel = at.group * group_width<V>() + lane * V;
+    channel = channel < p.n.C - V ? channel : p.n.C - V;
+    const int64_t first = (segment * waves + (waves - 1 - wave)) * R, left = p.n.T - first;
+    const int rows = left < 0 ? 0 : left < R ? (int)left : R;
+    float log_decay[V], sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]), sum[v] = 0.f;
+    typename L::vec dh[R], x[R], r[R], i[R], h[R];
+    L::template load<R>(p.decay_gate, at.batch, first, p.n.T, channel, r);
+    L::template load<R>(p.dh, at.batch, first, p.n.T, channel, dh);
+    L::template load<R>(p.input_gate, at.batch, first, p.n.T, channel, i);
+    L::template load<R>(p.x, at.batch, first, p.n.T, channel, x);
+    L::template load<R>(p.h, at.batch, first - 1, p.n.T, channel, h);        // the state before each row
+    PackedRows packed{0, 0, 0, 0, -1};
+    if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
+    float a[R][V], u[R][V];
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            a[k][v] = decay_of<EK>(log_decay[v], (float)r[k][v]);
+            u[k][v] = (float)dh[k][v];
+        }
+    if (rows < R)
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k >= rows)
+#pragma unroll
+                for (int v = 0; v < V; ++v) a[k][v] = 1.f, u[k][v] = 0.f;
+    // the gradient of a last state is part of its token's: it is read before any gradient of a first one is written
+    auto end = [&](int k, int64_t sequence) {
+        if (p.d_final_state)
+#pragma unroll
+            for (int v = 0; v < V; ++v) u[k][v] += p.d_final_state[sequence * p.n.C + channel + v];
+    };
+    if constexpr (PACKED) {
+        if (packed.ends | packed.outside)
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                if (packed.ends >> k & 1) end(k, __builtin_amdgcn_readlane(packed.sequence, k));
+                if (packed.outside >> k & 1)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) u[k][v] = 0.f;
+            }
+    } else if (rows > 0 && first + rows == p.n.T) {
+#pragma unroll
+        for (int k = 0; k < R; ++k)
+            if (k == rows - 1) end(k, at.batch);
+    }
+    const unsigned cut = packed.ends | packed.outside;
+    // dh and what the next token passes on
+    auto whole = [&](int k, int v, float c) { return u[k][v] + (PACKED && (cut >> k & 1) ? 0.f : c); };
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float A = 1.f, B = 0.f;
+#pragma unroll
+        for (int k = R - 1; k >= 0; --k) A *= a[k][v], B = a[k][v] * whole(k, v, B);
+        if (PACKED && cut) A = kCut;
+        pairs[wave][v][lane] = make_float2(A, B);
+    }
+    __syncthreads();
+    float c[V];
+    carry_in<V>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, c);
+    auto entry_of = [&]() {
+        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        return entry < p.n.n_states ? entry : -1;
+    };
+    T* const dx = static_cast<T*>(const_cast<void*>(p.dx.p)) + at.batch * p.dx.batch + first * p.dx.token + channel;
+    T* const dr = static_cast<T*>(const_cast<void*>(p.d_decay_gate.p)) + at.batch * p.d_decay_gate.batch + first * p.d_decay_gate.token + channel;
+    T* const di = static_cast<T*>(const_cast<void*>(p.d_input_gate.p)) + at.batch * p.d_input_gate.batch + first * p.d_input_gate.token + channel;
+#pragma unroll
+    for (int k = R - 1; k >= 0; --k) {
+        if (k >= rows) continue;
+        const bool begins = PACKED ? packed.begins >> k & 1 : first + k == 0;
+        float before[V], gx[V], gr[V], gi[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) before[v] = (float)h[k][v];
+        if (begins) {
+            const int entry = PACKED ? __builtin_amdgcn_readlane(packed.entry, k) : entry_of();
+#pragma unroll
+            for (int v = 0; v < V; ++v) before[v] = p.state && entry >= 0 ? p.state[(int64_t)entry * p.n.C + channel + v] : 0.f;
+        }
+        const bool outside = PACKED && (packed.outside >> k & 1);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float rk = (float)r[k][v];
+            // (what the decays came from is computed again row by row: kept for all rows it takes more registers than there are)
+            asm volatile("" : "+v"(rk));
+            const float ik = (float)i[k][v], xk = (float)x[k][v], d = whole(k, v, c[v]);
+            const Gate<EK> g(log_decay[v], rk, ik);
+            const float dw = g.w > 0.f ? g.a * g.a * __builtin_amdgcn_rcpf(g.w) : 0.f, px = g.p * xk;
+            const float l = d * (g.a * before[v] - px * dw), dw_p = d * g.w * g.p;
+            gx[v] = dw_p;
+            gi[v] = dw_p * xk * g.shut_p(ik);
+            gr[v] = l * g.L * g.shut_s(rk);
+            if (outside) gx[v] = gi[v] = gr[v] = 0.f;
+            else sum[v] = __builtin_fmaf(l, g.s, sum[v]);
+            c[v] = a[k][v] * d;
+        }
+        L::store(dx + k * p.dx.token, gx);
+        L::store(dr + k * p.d_decay_gate.token, gr);
+        L::store(di + k * p.d_input_gate.token, gi);
+        if (begins && p.d_state) {
+            const int64_t sequence = PACKED ? __builtin_amdgcn_readlane(packed.sequence, k) : at.batch;
+#pragma unroll
+            for (int v = 0; v < V; ++v) p.d_state[sequence * p.n.C + channel + v] = c[v];
+        }
+    }
+    if constexpr (PACKED)
+        if (p.d_state && p.d_state != p.d_final_state && wave == 0)
+            for_empty(p.n, tiles, at.segment, [&](int64_t sequence, int) {
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    p.d_state[sequence * p.n.C + channel + v] = p.d_final_state ? p.d_final_state[sequence * p.n.C + channel + v] : 0.f;
+            });
+    if (!p.d_log_decay) return;
+    __syncthreads();            // (all have taken their carry from the pairs)
+#pragma unroll
+    for (int v = 0; v < V; ++v) pairs[wave][v][lane].x = sum[v];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        for (int w = 1; w < waves; ++w) sum[v] += pairs[w][v][lane].x;
+        partial[part * p.n.C + channel + v] = sum[v];
+    }
+}
+
+__global__ __launch_bounds__(256) void recurrence_clear_kernel(Word* words, int64_t count)
+{
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < count; k += (int64_t)gridDim.x * 256) words[k] = 0;
+}
+
+constexpr int kThreads = 256;
 
 template <int EK>
 __device__ __forceinline__ const typename ElemOf<EK>::type* at(const Channels& c, int64_t batch, int channel)
 {
     return static_cast<const typename ElemOf<EK>::type*>(c.p) + batch * c.batch + channel;
-}
-template <int EK>
-__device__ __forceinline__ typename ElemOf<EK>::type* to(const Channels& c, int64_t batch, int channel)
-{
-    return static_cast<typename ElemOf<EK>::type*>(const_cast<void*>(c.p)) + batch * c.batch + channel;
-}
-
-template <int EK>
-__global__ __launch_bounds__(kThreads) void recurrence_kernel(RecurrenceArgs p, int groups)
-{
-    typedef typename ElemOf<EK>::type T;
-    const int b = blockIdx.x / groups, c = blockIdx.x % groups * kThreads + threadIdx.x;
-    if (c >= p.n.C) return;
-    const Rows rows = rows_of(p.n, b);
-    const int64_t batch = p.n.starts ? 0 : b;
-    const T *x = at<EK>(p.x, batch, c), *r = at<EK>(p.decay_gate, batch, c), *i = at<EK>(p.input_gate, batch, c);
-    T* h = to<EK>(p.h, batch, c);
-    const float log_decay = finite_decay(p.n.log_decay[c]);
-    float now = p.state && rows.entry >= 0 ? p.state[(int64_t)rows.entry * p.n.C + c] : 0.f;
-    for (int64_t t = rows.left; t < rows.first; ++t) h[t * p.h.token] = (T)0.f;
-    for (int64_t t = rows.first; t < rows.last; ++t) {
-        const Gate<EK> g(log_decay, (float)r[t * p.decay_gate.token], (float)i[t * p.input_gate.token]);
-        now = __builtin_fmaf(g.a, now, g.w * g.p * (float)x[t * p.x.token]);
-        h[t * p.h.token] = (T)now;
-    }
-    for (int64_t t = rows.last; t < rows.right; ++t) h[t * p.h.token] = (T)0.f;
-    if (p.final_state && rows.entry >= 0) p.final_state[(int64_t)rows.entry * p.n.C + c] = now;
-}
-
-template <int EK>
-__global__ __launch_bounds__(kThreads) void recurrence_backward_kernel(RecurrenceBackwardArgs p, int groups)
-{
-    typedef typename ElemOf<EK>::type T;
-    const int b = blockIdx.x / groups, c = blockIdx.x % groups * kThreads + threadIdx.x;
-    if (c >= p.n.C) return;
-    const Rows rows = rows_of(p.n, b);
-    const int64_t batch = p.n.starts ? 0 : b;
-    const T *dh = at<EK>(p.dh, batch, c), *x = at<EK>(p.x, batch, c), *r = at<EK>(p.decay_gate, batch, c), *i = at<EK>(p.input_gate, batch, c),
-            *h = at<EK>(p.h, batch, c);
-    T *dx = to<EK>(p.dx, batch, c), *dr = to<EK>(p.d_decay_gate, batch, c), *di = to<EK>(p.d_input_gate, batch, c);
-    auto zeros = [&](int64_t first, int64_t last) {
-        for (int64_t t = first; t < last; ++t) dx[t * p.dx.token] = dr[t * p.d_decay_gate.token] = di[t * p.d_input_gate.token] = (T)0.f;
-    };
-    zeros(rows.left, rows.first);
-    zeros(rows.last, rows.right);
-    const float log_decay = finite_decay(p.n.log_decay[c]);
-    const float first = p.state && rows.entry >= 0 ? p.state[(int64_t)rows.entry * p.n.C + c] : 0.f;
-    float later = p.d_final_state ? p.d_final_state[(int64_t)b * p.n.C + c] : 0.f, sum = 0.f;
-    for (int64_t t = rows.last - 1; t >= rows.first; --t) {
-        const float gr = (float)r[t * p.decay_gate.token], gi = (float)i[t * p.input_gate.token], xt = (float)x[t * p.x.token];
-        const Gate<EK> g(log_decay, gr, gi);
-        const float u = (float)dh[t * p.dh.token] + later, before = t > rows.first ? (float)h[(t - 1) * p.h.token] : first;
-        const float dw = g.w > 0.f ? g.a * g.a * __builtin_amdgcn_rcpf(g.w) : 0.f;
-        const float l = u * (g.a * before - g.p * xt * dw);
-        dx[t * p.dx.token] = (T)(u * g.w * g.p);
-        di[t * p.d_input_gate.token] = (T)(u * g.w * xt * g.p * g.shut_p(gi));
-        dr[t * p.d_decay_gate.token] = (T)(l * g.L * g.shut_s(gr));
-        sum = __builtin_fmaf(l, g.s, sum);
-        later = g.a * u;
-    }
-    if (p.d_state) p.d_state[(int64_t)b * p.n.C + c] = later;
-    if (p.d_log_decay) static_cast<float*>(p.work)[(int64_t)b * p.n.C + c] = sum;
-}
-
-__global__ __launch_bounds__(kThreads) void recurrence_fold_kernel(const float* partial, int parts, int C, float* sums)
-{
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= C) return;
-    float s = 0.f;
-    for (int k = 0; k < parts; ++k) s += partial[(int64_t)k * C + c];
-    sums[c] = s;
 }
 
 template <int EK>
@@ -111,7 +273,7 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(RecurrenceSte
     typedef typename ElemOf<EK>::type T;
     const int b = blockIdx.x / groups, c = blockIdx.x % groups * kThreads + threadIdx.x;
     if (c >= p.n.C) return;
-    T* h = to<EK>(p.h, b, c);
+    T* h = const_cast<T*>(at<EK>(p.h, b, c));
     const int entry = p.n.slots ? p.n.slots[b] : b;
     if (entry < 0 || entry >= p.n.n_states) {
         *h = (T)0.f;
@@ -126,27 +288,97 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(RecurrenceSte
 
 }  // namespace
 
-int64_t recurrence_workspace(const RecurrenceBatch&, bool, int) { return 0; }
-int64_t recurrence_backward_workspace(const RecurrenceBatch& n, bool, int) { return (int64_t)n.B * n.C * 4; }
+namespace {
+
+constexpr int kResident = 512;          // workgroups of kMostWaves wavefronts that the chip has at a time
+
+Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows)
+{
+    const int64_t most = (n.T + rows - 1) / rows;
+    Tiles t;
+    t.groups = (n.C + 64 * V - 1) / (64 * V);
+    t.waves = most < kMostWaves ? (int)most : kMostWaves;
+    t.segments = (most + t.waves - 1) / t.waves;
+    t.batches = packed ? 1 : n.B;
+    // Of a launch that fills the chip neighbours run at the same time and carries go quickly from one to the next, but what is read of pairs is taken from the
+    // rows' bandwidth; others wait for their chain alone (bf16, 8192 tokens: 4096 channels 67.5 us with blocks of 4 and 71 with 16, 512 channels 30 and 22).
+    t.block = t.count() > kResident ? 4 : kMostWaves;
+    return t;
+}
+
+// channels a lane has
+int lane_channels(const RecurrenceBatch& n, int ek) { return ek == kElemF32 || n.C < 2 ? 1 : 2; }
+
+hipError_t clear_chain(void* work, int64_t words, hipStream_t st)
+{
+    if (!words) return hipSuccess;
+    const int64_t groups = (words + 1023) / 1024;
+    hipLaunchKernelGGL(recurrence_clear_kernel, dim3((unsigned)(groups < 2048 ? groups : 2048)), dim3(256), 0, st, static_cast<Word*>(work), words);
+    return hipGetLastError();
+}
+
+// f(channels a lane, packed): integral constants
+template <int EK, class F>
+void with_lanes(int V, bool packed, F&& f)
+{
+    auto pack = [&](auto v) { packed ? f(v, std::true_type()) : f(v, std::false_type()); };
+    if constexpr (EK != kElemF32)
+        if (V == 2) return pack(std::integral_constant<int, 2>());
+    pack(std::integral_constant<int, 1>());
+}
+
+int64_t chain_bytes(const Tiles& t, int C) { return (8 * chain_words(t, C) + 15) / 16 * 16; }
+
+}  // namespace
+
+bool recurrence_fits(const RecurrenceBatch& n, bool packed, int ek)
+{
+    const int V = lane_channels(n, ek);
+    for (const int rows : {kForwardRows, kBackwardRows}) {
+        const Tiles t = tiles_of(n, packed, V, rows);
+        if (t.segments >= 1 << 22 || t.batches > ((int64_t)1 << 31) / t.segments || t.count() >= ((int64_t)1 << 26) / t.waves) return false;    // 2^32 threads
+    }
+    return true;
+}
+
+int64_t recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek)
+{
+    return chain_bytes(tiles_of(n, packed, lane_channels(n, ek), kForwardRows), n.C);
+}
+int64_t recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek)
+{
+    const Tiles t = tiles_of(n, packed, lane_channels(n, ek), kBackwardRows);
+    return chain_bytes(t, n.C) + t.segments * t.batches * n.C * 4;
+}
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 {
-    const int groups = (a.n.C + kThreads - 1) / kThreads;
+    const int V = lane_channels(a.n, ek);
+    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kForwardRows);
+    if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
     return with_elem(ek, [&](auto e) {
-        SW_NOTED_LAUNCH(note_kernel("recurrence_kernel", ek), recurrence_kernel<e()>, dim3(groups * a.n.B), dim3(kThreads), 0, st, a, groups);
+        note_kernel("recurrence_kernel", ek, V, a.n.starts != nullptr);
+        with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
+            hipLaunchKernelGGL((recurrence_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves), 0, st, a, tiles);
+        });
         return hipGetLastError();
     });
 }
 
 hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, hipStream_t st)
 {
-    const int groups = (a.n.C + kThreads - 1) / kThreads;
+    const int V = lane_channels(a.n, ek);
+    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kBackwardRows);
+    if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
+    float* const partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + chain_bytes(tiles, a.n.C));
     return with_elem(ek, [&](auto e) {
-        SW_NOTED_LAUNCH(note_kernel("recurrence_backward_kernel", ek), recurrence_backward_kernel<e()>, dim3(groups * a.n.B), dim3(kThreads), 0, st, a, groups);
+        note_kernel("recurrence_backward_kernel", ek, V, a.n.starts != nullptr);
+        with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
+            hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves), 0, st, a, tiles, partial);
+        });
         if (const hipError_t err = hipGetLastError()) return err;
-        if (a.d_log_decay)
-            hipLaunchKernelGGL(recurrence_fold_kernel, dim3(groups), dim3(kThreads), 0, st, static_cast<const float*>(a.work), a.n.B, a.n.C, a.d_log_decay);
-        return hipGetLastError();
+        if (!a.d_log_decay) return hipSuccess;
+        return launch_fold(FoldArgs{partial, (int)(tiles.segments * tiles.batches), a.n.C, {a.d_log_decay, nullptr}, a.n.C}, st);
     });
 }
 

@@ -1,0 +1,269 @@
+// What the two passes of the gated recurrence share: tiles of rows and channels, packed sequences within a wavefront's rows, and the carry
+// from tile to tile.
+//
+// A recurrence c' = a c + b over a run of rows is one pair (A, B): c' = A c + B.  A wavefront has kRows rows of 64 lanes' channels in registers, a workgroup up
+// to 16 wavefronts one after the other in time, and their pairs meet in LDS.  Workgroups of one channel group are a chain: each adds its pair to what
+// comes from the one before.  They take their places from a counter, so that whoever waits, waits for workgroups that have begun; each word of
+// a pair is stored with a flag in one 64-bit store, so that no fence is needed.  Every block-th workgroup passes on the carry itself, those
+// between their pairs, which a successor reads all at once, a wavefront each, and folds in their order: a chain of a link (1 us) for each
+// block, and the same sums in every run.
+#pragma once
+
+#include "sw_gates.h"
+#include "sw_sequence.h"
+
+namespace swconv {
+
+typedef unsigned long long Word;
+
+constexpr int kMostWaves = 16;
+constexpr float kCut = -1.f;            // A of rows among which a sequence begins: nothing from before reaches their end (decays are >= 0)
+
+struct Tiles {
+    int groups, waves;                  // channel groups; wavefronts of a workgroup
+    int block;                          // workgroups from one carry that is passed on to the next, at most kMostWaves
+    int64_t segments, batches;          // workgroups along a sequence; sequences (1: packed)
+    int64_t count() const { return groups * segments * batches; }
+};
+
+// V channels of 64 lanes
+template <int V>
+constexpr int group_width() { return 64 * V; }
+
+template <int EK, int V>
+struct Lane {
+    typedef typename ElemOf<EK>::type T;
+    typedef T vec __attribute__((ext_vector_type(V)));
+    struct __attribute__((packed, aligned(sizeof(T)))) loose {
+        vec v;
+    };
+    static __device__ __forceinline__ vec load(const T* p) { return reinterpret_cast<const loose*>(p)->v; }
+    // R rows from row `first` on, the first and the last one again beyond the ends: one multiplication for all their addresses
+    template <int R>
+    static __device__ __forceinline__ void load(const Channels& c, int64_t batch, int64_t first, int64_t rows, int channel, vec (&v)[R])
+    {
+        const int64_t begin = first < 0 ? 0 : first < rows ? first : rows - 1;
+        const T* p = static_cast<const T*>(c.p) + batch * c.batch + begin * c.token;
+        if (first >= 0 && first + R <= rows) {
+#pragma unroll
+            for (int k = 0; k < R; ++k, p += c.token) v[k] = load(p + channel);
+        } else {
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                v[k] = load(p + channel);
+                p += first + k >= 0 && first + k + 1 < rows ? c.token : 0;
+            }
+        }
+    }
+    static __device__ __forceinline__ void store(T* p, const float (&f)[V])
+    {
+        vec v;
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = (T)f[k];
+        reinterpret_cast<loose*>(p)->v = v;
+    }
+};
+
+// ---- the carry from workgroup to workgroup ---------------------------------------------------------------------------------------
+
+// { counter, carries [segments / block][batches][C], pairs [segments][batches][C] }, all zero before the launch
+struct Chain {
+    Word* base;
+    int64_t stride;                     // batches * C
+    int64_t segments;
+    int block;
+    __device__ __forceinline__ unsigned* counter() const { return reinterpret_cast<unsigned*>(base); }
+    __device__ __forceinline__ Word* carry(int segment, int64_t at) const { return base + 2 + (int64_t)(segment / block) * stride + at; }
+    __device__ __forceinline__ Word* pair(int segment, int64_t at) const
+    {
+        return base + 2 + ((segments + block - 1) / block + segment) * stride + at;
+    }
+};
+inline int64_t chain_words(const Tiles& t, int C)
+{
+    return t.segments == 1 ? 0 : 2 + ((t.segments + t.block - 1) / t.block + t.segments) * t.batches * C;
+}
+
+__device__ __forceinline__ void publish(Word* to, Word v) { __hip_atomic_store(to, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ Word look(const Word* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// A carry with a flag above it; a pair with its A, negated, above its B: A is kCut, or not negative, or NaN, so that no pair is a word of zeros above.
+__device__ __forceinline__ Word carry_word(float c) { return (Word)1 << 32 | __float_as_uint(c); }
+__device__ __forceinline__ Word pair_word(float A, float B) { return (Word)(__float_as_uint(A) ^ 0x80000000u) << 32 | __float_as_uint(B); }
+__device__ __forceinline__ bool ready(Word w) { return w >> 32 != 0; }
+__device__ __forceinline__ float low_of(Word w) { return __uint_as_float((unsigned)w); }
+__device__ __forceinline__ float A_of(Word w) { return __uint_as_float((unsigned)(w >> 32) ^ 0x80000000u); }
+
+// c after a run of rows.  Where A is 0 because decays have faded beyond fp32, a carry that is not finite still spoils what follows.
+__device__ __forceinline__ float after(float A, float B, float c) { return __builtin_fmaf(A, A < 0.f ? 0.f : c, B); }
+// the pair of a run followed by the run (A, B)
+__device__ __forceinline__ void append(float A, float B, float& all_A, float& all_B)
+{
+    all_B = after(A, B, all_B);
+    const float both = A * all_A;
+    all_A = fminf(A, all_A) < 0.f ? kCut : both;
+}
+
+// N neighbouring words as soon as all of them are there.  The wait is for workgroups that run already; it is bounded all the same, and one
+// that is given up reads as NaN.
+template <int N>
+__device__ __forceinline__ void wait_for(const Word* at, Word (&w)[N])
+{
+    for (int turns = 0;; ++turns) {
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            w[k] = look(at + k);
+            all = all && ready(w[k]);
+        }
+        if (__all(all)) return;
+        if (turns == 1 << 22) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) w[k] = ~(Word)0;
+            return;
+        }
+        __builtin_amdgcn_s_sleep(1);
+    }
+}
+
+// What comes into segment `segment` of the chain for the V channels at `at`, by all of a workgroup of kMostWaves wavefronts: each waits for one
+// of the pairs since the last carry that was passed on, the last one for that carry; they meet in LDS and are folded in their order.  One
+// trip to memory, whatever their number.
+template <int V>
+__device__ __forceinline__ void incoming(const Chain& chain, int segment, int64_t at, int wave, float2 (*met)[V][64], float (&c)[V])
+{
+    const int lane = threadIdx.x % 64, since = segment % chain.block, first = segment - since;
+    Word w[V];
+    if (wave < since) {
+        wait_for<V>(chain.pair(first + wave, at), w);
+#pragma unroll
+        for (int v = 0; v < V; ++v) met[wave][v][lane] = make_float2(A_of(w[v]), low_of(w[v]));
+    }
+    if (wave == kMostWaves - 1) {
+        if (first > 0) wait_for<V>(chain.carry(first - 1, at), w);
+#pragma unroll
+        for (int v = 0; v < V; ++v) met[kMostWaves - 1][v][lane].x = first > 0 ? low_of(w[v]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        c[v] = met[kMostWaves - 1][v][lane].x;
+        for (int k = 0; k < since; ++k) c[v] = after(met[k][v][lane].x, met[k][v][lane].y, c[v]);
+    }
+}
+
+// A workgroup's place.
+struct Place {
+    int segment, group;
+    int64_t batch;
+};
+__device__ __forceinline__ Place place_of(const Tiles& tiles, int64_t ticket)
+{
+    const int64_t rest = ticket / tiles.groups;
+    return Place{(int)(rest / tiles.batches), (int)(ticket % tiles.groups), rest % tiles.batches};
+}
+__device__ __forceinline__ int64_t take_ticket(const Tiles& tiles, const Chain& chain, unsigned* shared)
+{
+    if (tiles.segments == 1) return blockIdx.x;
+    if (threadIdx.x == 0) *shared = __hip_atomic_fetch_add(chain.counter(), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*shared);
+}
+
+// What comes into a wavefront's rows, from its workgroup's pairs and, of several along a sequence, from the chain; passes on what goes to the next workgroup.
+template <int V>
+__device__ __forceinline__ void carry_in(const Chain& chain, const Tiles& tiles, const Place& place, int64_t at, int wave, const float2 (*pairs)[V][64],
+                                         float2 (*met)[V][64], float (&c)[V])
+{
+    const int lane = threadIdx.x % 64;
+#pragma unroll
+    for (int v = 0; v < V; ++v) c[v] = 0.f;
+    if (tiles.segments > 1) {
+        const bool passes_on = place.segment % tiles.block == tiles.block - 1, mine = wave == kMostWaves - 1 && place.segment < tiles.segments - 1;
+        float A[V], B[V];
+        if (mine) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
+            for (int w = 0; w < kMostWaves; ++w)
+#pragma unroll
+                for (int v = 0; v < V; ++v) append(pairs[w][v][lane].x, pairs[w][v][lane].y, A[v], B[v]);
+            if (!passes_on)
+#pragma unroll
+                for (int v = 0; v < V; ++v) publish(chain.pair(place.segment, at + v), pair_word(A[v], B[v]));
+        }
+        incoming<V>(chain, place.segment, at, wave, met, c);
+        if (mine && passes_on)
+#pragma unroll
+            for (int v = 0; v < V; ++v) publish(chain.carry(place.segment, at + v), carry_word(after(A[v], B[v], c[v])));
+    }
+    for (int w = 0; w < wave; ++w)
+#pragma unroll
+        for (int v = 0; v < V; ++v) c[v] = after(pairs[w][v][lane].x, pairs[w][v][lane].y, c[v]);
+}
+
+// ---- packed sequences ----------------------------------------------------------------------------------------------------------------
+
+// Of the rows first ... first + R - 1 (R <= 32), a bit each; lane k < R has what concerns row first + k.
+struct PackedRows {
+    unsigned begins, ends, outside;     // the first and last rows of sequences; rows in no sequence
+    int sequence, entry;                // of the lane's row; entry -1: none
+};
+// (Addresses are the wavefront's: scalar loads, which wait for none of the rows on their way.)
+__device__ __forceinline__ int uniform_load(const int32_t* p)
+{
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
+}
+template <int R>
+__device__ __forceinline__ PackedRows packed_rows(const RecurrenceBatch& n, int64_t first)
+{
+    const int lane = threadIdx.x % 64;
+    const int64_t past = first + R < n.T ? first + R : n.T;
+    PackedRows p{0, 0, 0, 0, -1};
+    int lo = 0, hi = n.B + 1;           // how many of the B + 1 starts are at or before the first row
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (uniform_load(n.starts + mid) <= first) lo = mid + 1;
+        else hi = mid;
+    }
+    unsigned inside = 0;
+    for (int b = lo > 0 ? lo - 1 : 0; b < n.B; ++b) {
+        int64_t begin = uniform_load(n.starts + b), end = uniform_load(n.starts + b + 1);
+        begin = begin < 0 ? 0 : begin, end = end > n.T ? n.T : end;
+        if (begin >= past) break;
+        const int from = (int)((begin > first ? begin : first) - first), to = (int)((end < past ? end : past) - first);
+        if (to <= from) continue;
+        if (begin >= first) p.begins |= 1u << from;
+        if (end <= past) p.ends |= 1u << (to - 1);
+        inside |= (unsigned)(((1ull << to) - 1) & ~((1ull << from) - 1));
+        const int entry = n.slots ? uniform_load(n.slots + b) : b;
+        if (lane >= from && lane < to) p.sequence = b, p.entry = entry >= 0 && entry < n.n_states ? entry : -1;
+    }
+    const int rows = past > first ? (int)(past - first) : 0;
+    p.outside = (unsigned)((1ull << rows) - 1) & ~inside;
+    return p;
+}
+
+// f(sequence, entry) for the empty sequences among this segment's share of them (their last state is their first), by a whole wavefront
+template <class F>
+__device__ __forceinline__ void for_empty(const RecurrenceBatch& n, const Tiles& tiles, int64_t segment, F&& f)
+{
+    const int lane = threadIdx.x % 64;
+    const int from = (int)(n.B * segment / tiles.segments), to = (int)(n.B * (segment + 1) / tiles.segments);
+    for (int b0 = from; b0 < to; b0 += 64) {
+        const int b = b0 + lane;
+        bool empty = false;
+        int entry = -1;
+        if (b < to) {
+            int64_t begin = n.starts[b], end = n.starts[b + 1];
+            begin = begin < 0 ? 0 : begin > n.T ? n.T : begin, end = end < 0 ? 0 : end > n.T ? n.T : end;
+            empty = begin >= end;
+            entry = n.slots ? n.slots[b] : b;
+            if (entry < 0 || entry >= n.n_states) entry = -1;
+        }
+        for (unsigned long long left = __ballot(empty); left; left &= left - 1) {
+            const int k = __builtin_ctzll(left);
+            f(b0 + k, __builtin_amdgcn_readlane(entry, k));
+        }
+    }
+}
+
+}  // namespace swconv

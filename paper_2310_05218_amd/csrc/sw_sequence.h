@@ -6,6 +6,15 @@
 
 namespace swconv {
 
+// ---- sums of rows of fp32 values, in a fixed order ---------------------------------------------------------------------------------
+struct FoldArgs {
+    const float* partial;               // [parts, width]
+    int parts, width;
+    float* out[2];                      // the sums of the first `split` columns and of the others; null: not wanted
+    int split;
+};
+hipError_t launch_fold(const FoldArgs& a, hipStream_t st);
+
 // ---- gated linear recurrence ---------------------------------------------------------------------------------------------------
 // rows of channels [batch, token, C]: strides in elements
 struct Channels {
@@ -37,6 +46,7 @@ struct RecurrenceStepArgs {
     float* state;
     RecurrenceBatch n;
 };
+bool       recurrence_fits(const RecurrenceBatch& n, bool packed, int ek);      // a launch has workgroups for it
 int64_t    recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek);
 int64_t    recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek);
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st);

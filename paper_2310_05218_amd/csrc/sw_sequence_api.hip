@@ -44,17 +44,18 @@ bool same(const Tensor4& a, const Tensor4& b)
 
 Channels channels(const Tensor4& t) { return Channels{t.op.p, t.op.batch, t.op.token}; }
 
+RecurrenceBatch batch_of(const sw_gated_recurrence_dims& d, const float* log_decay, const int32_t* starts, const int32_t* slots)
+{
+    return RecurrenceBatch{log_decay, starts, slots, d.T, (int)d.C, d.B, d.n_states};
+}
+
 int check_recurrence(const sw_gated_recurrence_dims& d, bool packed)
 {
     const int64_t batches = packed ? 1 : d.B;
     if (d.T <= 0 || d.B <= 0 || d.C <= 0 || d.n_states < 0 || d.T > kMaxExtent / batches || (int64_t)d.B + 2 > 0x7fffffff) return SW_ERR_SHAPE;
     if (d.C > kMaxChannels || !known(d.type)) return SW_ERR_UNSUPPORTED;
     if (d.C > kMaxExtent / ((int64_t)d.n_states + d.B) || d.T * batches > kMaxExtent / d.C) return SW_ERR_SHAPE;
-    return SW_OK;
-}
-RecurrenceBatch batch_of(const sw_gated_recurrence_dims& d, const float* log_decay, const int32_t* starts, const int32_t* slots)
-{
-    return RecurrenceBatch{log_decay, starts, slots, d.T, (int)d.C, d.B, d.n_states};
+    return recurrence_fits(batch_of(d, nullptr, nullptr, nullptr), packed, d.type) ? SW_OK : SW_ERR_SHAPE;
 }
 
 int check_heads(const sw_head_norm_dims& d)
