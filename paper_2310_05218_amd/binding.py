@@ -360,7 +360,9 @@ _NATIVE_ENTRIES = ("sw_conv1d", "sw_pool1d", "sw_pool2d", "sw_conv2d", "sw_conv2
                    "sw_conv2d_s8_nhwc_requant", "sw_conv2d_nhwc", "sw_conv2d_bf16_nhwc", "sw_conv2d_f16_nhwc",
                    "sw_layer_norm", "sw_layer_norm_backward", "sw_layer_norm_backward_workspace_bytes", "sw_linear_attention",
                    "sw_linear_attention_workspace_bytes", "sw_linear_attention_backward", "sw_linear_attention_backward_workspace_bytes",
-                   "sw_linear_attention_step")
+                   "sw_linear_attention_step", "sw_gated_recurrence", "sw_gated_recurrence_workspace_bytes", "sw_gated_recurrence_backward",
+                   "sw_gated_recurrence_backward_workspace_bytes", "sw_gated_recurrence_step", "sw_head_norm", "sw_head_norm_backward",
+                   "sw_head_norm_backward_workspace_bytes", "sw_adapters", "sw_adapters_workspace_bytes")
 
 
 def _bind_native(*args):

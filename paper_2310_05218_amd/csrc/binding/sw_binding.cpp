@@ -1,6 +1,6 @@
 // The short way from a Python call to the C ABI: checks, output extents, the output tensor and the call in one native function.
 //
-// run(op, x, w, bias, scale, integers and flags ...; layer norm and attention: their own arguments) returns the output tensor or a tuple of
+// run(op, x, w, bias, scale, integers and flags ...; the sequence operators: their own arguments) returns the output tensor or a tuple of
 // them, a status code other than SW_OK, or None for whatever
 // it does not take (other types, layouts, devices, arguments out of range): the caller then goes the long way, which takes it or says
 // why not.  Nothing is kept between calls but the entry points' addresses.
@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <cmath>
 
@@ -20,7 +21,7 @@
 namespace {
 
 enum Op { kConv1d, kPool1d, kPool2d, kConv2d, kBiasRelu, kDilated, kDepthwise, kDepthwiseBiasRelu, kDepthwiseBf16, kS8, kS8Requant, kS8Nhwc, kNhwc, kLayerNorm, kLayerNormBackward,
-          kAttention, kAttentionBackward, kAttentionStep };
+          kAttention, kAttentionBackward, kAttentionStep, kRecurrence, kRecurrenceBackward, kRecurrenceStep, kHeadNorm, kHeadNormBackward, kAdapters };
 
 struct Entries {
     decltype(&sw_conv1d) conv1d;
@@ -47,6 +48,16 @@ struct Entries {
     decltype(&sw_linear_attention_backward) attention_backward;
     decltype(&sw_linear_attention_backward_workspace_bytes) attention_backward_workspace;
     decltype(&sw_linear_attention_step) attention_step;
+    decltype(&sw_gated_recurrence) recurrence;
+    decltype(&sw_gated_recurrence_workspace_bytes) recurrence_workspace;
+    decltype(&sw_gated_recurrence_backward) recurrence_backward;
+    decltype(&sw_gated_recurrence_backward_workspace_bytes) recurrence_backward_workspace;
+    decltype(&sw_gated_recurrence_step) recurrence_step;
+    decltype(&sw_head_norm) head_norm;
+    decltype(&sw_head_norm_backward) head_norm_backward;
+    decltype(&sw_head_norm_backward_workspace_bytes) head_norm_backward_workspace;
+    decltype(&sw_adapters) adapters;
+    decltype(&sw_adapters_workspace_bytes) adapters_workspace;
 };
 Entries g_entry;
 constexpr int kEntries = sizeof(Entries) / sizeof(void*);
@@ -485,6 +496,180 @@ PyObject* run_attention(int op, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- gated recurrence, norms of heads, adapters: tensors that are all on the current device --------------------------------------------
+
+bool here(const at::Tensor& t) { return g_host || t.get_device() == (int)c10::hip::current_device(); }
+template <class... T>
+bool all_here(const T*... t)
+{
+    return ((!t || here(*t)) && ...);
+}
+
+// a tensor of x's type and that shape, channels contiguous
+bool channels_of(PyObject* o, const at::Tensor& x, const at::Tensor** t, sw_strides* s)
+{
+    *t = any_tensor(o);
+    if (!*t || (*t)->is_cuda() != x.is_cuda() || (*t)->scalar_type() != x.scalar_type() || (*t)->sizes() != x.sizes() || !here(**t)) return false;
+    const auto st = (*t)->strides();
+    const size_t d = st.size();
+    if (st[d - 1] != 1 && x.size(d - 1) > 1) return false;
+    *s = sw_strides{d == 3 ? st[0] : 0, st[d - 2], 0};
+    return true;
+}
+
+at::Tensor scratch(int64_t need, const at::Tensor& like) { return need ? at::empty({need}, like.options().dtype(at::kByte)) : at::Tensor(); }
+void* address(at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; }
+
+// (x, decay_gate, input_gate, log_decay, starts, state, slots, final_state), (dh, x, decay_gate, input_gate, log_decay, h, starts, state, slots,
+// d_final_state, d_state, params) and (x, decay_gate, input_gate, log_decay, state, slots)
+PyObject* run_recurrence(int op, PyObject* const* a, Py_ssize_t n)
+{
+    const bool step = op == kRecurrenceStep, backward = op == kRecurrenceBackward;
+    if (n != (step ? 6 : backward ? 12 : 8)) return nullptr;
+    PyObject* const pdh = backward ? *a++ : nullptr;
+    PyObject* const ph = backward ? a[4] : nullptr;
+    PyObject* const* const b = backward ? a + 5 : a + 4;     // starts, state, slots, final_state, d_state, params; step: state, slots
+    PyObject *const pstarts = step ? Py_None : b[0], *const pstate = b[step ? 0 : 1], *const pslots = b[step ? 1 : 2];
+    const at::Tensor *x = any_tensor(a[0]), *r, *i, *dh = nullptr, *h = nullptr, *starts = nullptr, *slots, *decay, *state, *last = nullptr, *d_state = nullptr;
+    const bool packed = pstarts != Py_None;
+    const int64_t dim = step || packed ? 2 : 3;
+    sw_gated_recurrence_dims d{};
+    if (!x || !type_of(*x, &d.type) || x->dim() != dim || x->numel() == 0 || !fits(*x)) return nullptr;
+    if (packed && (!(starts = tensor(pstarts, at::kInt, 1)) || starts->size(0) < 2 || starts->size(0) > INT32_MAX)) return nullptr;
+    d.C = x->size(dim - 1), d.T = step ? 1 : x->size(dim - 2), d.B = packed ? (int)starts->size(0) - 1 : (int)x->size(0);
+    sw_strides s[8];
+    const int64_t channels[1] = {d.C}, sequences[1] = {d.B}, each[2] = {d.B, d.C};
+    sw_strides* const in = backward ? s + 1 : s;
+    if (!channels_of(a[0], *x, &x, in) || !channels_of(a[1], *x, &r, in + 1) || !channels_of(a[2], *x, &i, in + 2) ||
+        (backward && (!channels_of(pdh, *x, &dh, s) || !channels_of(ph, *x, &h, s + 4))) || !plain(a[3], at::kFloat, channels, false, &decay) ||
+        !plain(pslots, at::kInt, sequences, true, &slots))
+        return nullptr;
+    const at::Tensor* held = any_tensor(pstate != Py_None || backward || step ? pstate : b[3]);
+    if (held && (held->dim() != 2 || held->size(0) > INT32_MAX)) return nullptr;
+    d.n_states = held ? (int)held->size(0) : 0;
+    const int64_t entries[2] = {d.n_states, d.C};
+    if (!plain(pstate, at::kFloat, entries, !step, &state) || (!step && !plain(b[3], at::kFloat, backward ? each : entries, true, &last))) return nullptr;
+    const auto options = x->options();
+    const int64_t row[3] = {dim == 3 ? d.T * d.C : 0, d.C, 0};
+    const sw_strides dense{row[0], row[1], 0};
+    const Address xa(x), ra(r), ia(i), ga(decay), sa(slots), ca(starts);
+    if (!all_here(decay, starts, slots, state, last)) return nullptr;
+    if (step) {
+        at::Tensor y = at::empty(x->sizes(), options);
+        void* const yp = y.mutable_data_ptr();
+        float* const sp = floats(state);
+        s[3] = dense;
+        for (int k = 0; k < 4; ++k) s[k] = sw_strides{s[k].token, 0, 0};
+        at::Tensor* const out[1] = {&y};
+        return call_into(out, 1, [&](void* st) { return g_entry.recurrence_step(xa.p, ra.p, ia.p, ga, yp, sp, sa, &d, s, st); });
+    }
+    const Address first(state);
+    if (!backward) {
+        const int64_t need = g_entry.recurrence_workspace(&d, packed);
+        at::Tensor y = at::empty(x->sizes(), options), work = scratch(need, *x);
+        void *const yp = y.mutable_data_ptr(), *const wp = address(work);
+        float* const lp = floats(last);
+        s[3] = dense;
+        at::Tensor* const out[1] = {&y};
+        return call_into(out, 1, [&](void* st) { return g_entry.recurrence(xa.p, ra.p, ia.p, ga, yp, first, lp, sa, ca, &d, s, wp, need, st); });
+    }
+    int params;
+    if (!plain(b[4], at::kFloat, each, true, &d_state) || !all_here(d_state) || !flag(b[5], &params)) return nullptr;
+    const Address da(dh), ha(h), fa(last);
+    const int64_t need = g_entry.recurrence_backward_workspace(&d, packed);
+    at::Tensor dx = at::empty(x->sizes(), options), dr = at::empty(x->sizes(), options), di = at::empty(x->sizes(), options), dl, work = scratch(need, *x);
+    if (params) dl = at::empty(channels, options.dtype(at::kFloat));
+    void *const xp = dx.mutable_data_ptr(), *const rp = dr.mutable_data_ptr(), *const ip = di.mutable_data_ptr(), *const wp = address(work);
+    float *const lp = static_cast<float*>(address(dl)), *const sp = floats(d_state);
+    s[5] = s[6] = s[7] = dense;
+    at::Tensor* const out[4] = {&dx, &dr, &di, params ? &dl : nullptr};
+    return call_into(out, 4, [&](void* st) {
+        return g_entry.recurrence_backward(da.p, xa.p, ra.p, ia.p, ga, ha.p, first, fa, xp, rp, ip, lp, sp, sa, ca, &d, s, wp, need, st);
+    });
+}
+
+// (q, k, q_weight, k_weight, frequencies, positions, eps, interleaved) and (dq, dk, q, k, the same, params)
+PyObject* run_head_norm(bool backward, PyObject* const* a, Py_ssize_t n)
+{
+    if (n != (backward ? 11 : 8)) return nullptr;
+    PyObject *const pdq = a[0], *const pdk = a[1];
+    if (backward) a += 2;
+    const at::Tensor *q = any_tensor(a[0]), *k = any_tensor(a[1]), *dq = nullptr, *dk = nullptr, *wq, *wk, *f = nullptr, *at_ = nullptr;
+    sw_head_norm_dims d{};
+    if (!q || !k || !type_of(*q, &d.type) || (q->dim() != 3 && q->dim() != 4) || k->dim() != q->dim() || q->numel() == 0 || k->numel() == 0 || !fits(*q) ||
+        !fits(*k))
+        return nullptr;
+    const int64_t dim = q->dim();
+    d.B = dim == 4 ? q->size(0) : 1, d.T = q->size(dim - 3), d.heads = (int)q->size(dim - 2), d.kv_heads = (int)k->size(dim - 2), d.d = (int)q->size(dim - 1);
+    int64_t nq[4], nk[4];
+    for (int i = 0; i < dim; ++i) nq[i] = nk[i] = q->size(i);
+    nk[dim - 2] = d.kv_heads;
+    const at::IntArrayRef sq(nq, dim), sk(nk, dim), front(nq, dim - 2);
+    const int64_t width[1] = {d.d};
+    sw_strides s[6];
+    sw_strides* const in = backward ? s + 2 : s;
+    int params = 0;
+    if (!heads_of(a[0], *q, sq, &q, in) || !heads_of(a[1], *q, sk, &k, in + 1) ||
+        (backward && (!heads_of(pdq, *q, sq, &dq, s) || !heads_of(pdk, *q, sk, &dk, s + 1) || !flag(a[8], &params))) ||
+        !plain(a[2], at::kFloat, width, true, &wq) || !plain(a[3], at::kFloat, width, true, &wk) || !plain(a[5], at::kInt, front, true, &at_) ||
+        a[6] == Py_None || !number(a[6], 0, &d.eps) || !flag(a[7], &d.interleaved))
+        return nullptr;
+    if (a[4] != Py_None && (!(f = tensor(a[4], at::kFloat, 1)) || f->size(0) > INT32_MAX)) return nullptr;
+    d.pairs = f ? (int)f->size(0) : 0;
+    if (!all_here(q, k, dq, dk, wq, wk, f, at_)) return nullptr;
+    const Address qa(q), ka(k), wqa(wq), wka(wk), fa(f), pa(at_);
+    const auto options = q->options();
+    at::Tensor oq = at::empty(sq, options), ok = at::empty(sk, options);
+    void *const oqp = oq.mutable_data_ptr(), *const okp = ok.mutable_data_ptr();
+    in[2] = strides_of(sq), in[3] = strides_of(sk);
+    if (!backward) {
+        at::Tensor* const out[2] = {&oq, &ok};
+        return call_into(out, 2, [&](void* st) { return g_entry.head_norm(qa.p, ka.p, wqa, wka, fa, pa, oqp, okp, &d, s, st); });
+    }
+    const Address dqa(dq), dka(dk);
+    const int64_t need = params ? g_entry.head_norm_backward_workspace(&d) : 0;
+    at::Tensor gq, gk, work = scratch(need, *q);
+    if (params) gq = at::empty(width, options.dtype(at::kFloat)), gk = at::empty(width, options.dtype(at::kFloat));
+    void* const wp = address(work);
+    float *const gqp = static_cast<float*>(address(gq)), *const gkp = static_cast<float*>(address(gk));
+    at::Tensor* const out[4] = {&oq, &ok, params ? &gq : nullptr, params ? &gk : nullptr};
+    return call_into(out, 4, [&](void* st) {
+        return g_entry.head_norm_backward(dqa.p, dka.p, qa.p, ka.p, wqa, wka, fa, pa, oqp, okp, gqp, gkp, &d, s, wp, need, st);
+    });
+}
+
+// (x, a, b, y, scales, slots, starts)
+PyObject* run_adapters(PyObject* const* a, Py_ssize_t n)
+{
+    if (n != 7) return nullptr;
+    const at::Tensor *x = any_tensor(a[0]), *fa = any_tensor(a[1]), *fb, *y = any_tensor(a[3]), *scales, *slots, *starts = nullptr;
+    const bool packed = a[6] != Py_None;
+    sw_adapters_dims d{};
+    int type;
+    if (!x || !fa || !y || !type_of(*x, &d.type) || !type_of(*y, &type) || type != d.type || fa->dim() != 3 || (x->dim() != 2 && (packed || x->dim() != 3)) ||
+        y->dim() != x->dim() || x->numel() == 0 || y->numel() == 0 || fa->numel() == 0 || !fits(*x) || !fits(*y) || !fits(*fa))
+        return nullptr;
+    if (packed && (!(starts = tensor(a[6], at::kInt, 1)) || starts->size(0) < 2 || starts->size(0) > INT32_MAX)) return nullptr;
+    const int64_t dim = x->dim();
+    d.n = (int)fa->size(0), d.rank = (int)fa->size(1), d.C_in = (int)fa->size(2), d.C_out = (int)y->size(dim - 1);
+    d.B = packed ? (int)starts->size(0) - 1 : (int)x->size(0);
+    d.T = packed ? x->size(0) : dim == 3 ? x->size(1) : 1;
+    const int64_t na[3] = {d.n, d.rank, d.C_in}, nb[3] = {d.n, d.C_out, d.rank}, adapters[1] = {d.n}, sequences[1] = {d.B};
+    Rows rx, ry;
+    if (x->size(dim - 1) != d.C_in || x->sizes().slice(0, dim - 1) != y->sizes().slice(0, dim - 1) || !rx.set(*x) || !ry.set(*y) ||
+        !plain(a[1], x->scalar_type(), na, false, &fa) || !plain(a[2], x->scalar_type(), nb, false, &fb) || !plain(a[4], at::kFloat, adapters, true, &scales) ||
+        !plain(a[5], at::kInt, sequences, true, &slots) || !all_here(x, fa, fb, y, scales, slots, starts))
+        return nullptr;
+    const Address xa(x), aa(fa), ba(fb), ya(y), sa(scales), ta(slots), ca(starts);
+    const int64_t need = g_entry.adapters_workspace(&d, packed);
+    at::Tensor o = at::empty(y->sizes(), y->options()), work = scratch(need, *x);
+    void *const op = o.mutable_data_ptr(), *const wp = address(work);
+    at::Tensor* const out[1] = {&o};
+    return call_into(out, 1, [&](void* st) {
+        return g_entry.adapters(xa.p, aa.p, ba.p, ya.p, sa, ta, ca, op, &d, rx.stride, ry.stride, d.C_out, wp, need, st);
+    });
+}
+
 PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     int op;
@@ -495,6 +680,12 @@ PyObject* run(PyObject*, PyObject* const* a, Py_ssize_t n)
                 y = run_norm(op == kLayerNormBackward, a + 1, n - 1);
             else if (op >= kAttention && op <= kAttentionStep)
                 y = run_attention(op, a + 1, n - 1);
+            else if (op >= kRecurrence && op <= kRecurrenceStep)
+                y = run_recurrence(op, a + 1, n - 1);
+            else if (op == kHeadNorm || op == kHeadNormBackward)
+                y = run_head_norm(op == kHeadNormBackward, a + 1, n - 1);
+            else if (op == kAdapters)
+                y = run_adapters(a + 1, n - 1);
             else
                 y = run_op(op, a + 1, n - 1);
             if (y) return y;

@@ -7,16 +7,16 @@ namespace swconv {
 
 namespace {
 
-constexpr int kForwardRows = 8;
+constexpr int kForwardRows = 8, kForwardWaves = 16;
 
 // A tile of V channels a lane: decays and terms of its rows in registers, read once, the carry, then the rows' states.
 template <int EK, int V, bool PACKED>
-__global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu(8))) void recurrence_kernel(RecurrenceArgs p, Tiles tiles)
+__global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per_eu(8))) void recurrence_kernel(RecurrenceArgs p, Tiles tiles)
 {
     typedef Lane<EK, V> L;
     typedef typename L::T T;
     constexpr int R = kForwardRows;
-    __shared__ float2 pairs[kMostWaves][V][64], met[kMostWaves][V][64];
+    __shared__ float2 pairs[kForwardWaves][V][64], met[kForwardWaves][V][64];
     __shared__ unsigned ticket;
     const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
     const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     }
     __syncthreads();
     float h[V];
-    carry_in<V>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, h);
+    carry_in<V, kForwardWaves>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, h);
     auto keep = [&](int entry) {
         if (p.final_state && entry >= 0)
 #pragma unroll
@@ -111,16 +111,16 @@ __global__ __launch_bounds__(64 * kMostWaves) __attribute__((amdgpu_waves_per_eu
     }
 }
 
-constexpr int kBackwardRows = 8;
+constexpr int kBackwardRows = 8, kBackwardWaves = 8;
 
 // The same backwards in time: what a token passes on to the one before is c' = a (dh + c).  A workgroup's first wavefront has its last rows.
 template <int EK, int V, bool PACKED>
-__global__ __launch_bounds__(64 * kMostWaves) void recurrence_backward_kernel(RecurrenceBackwardArgs p, Tiles tiles, float* partial)
+__global__ __launch_bounds__(64 * kBackwardWaves) void recurrence_backward_kernel(RecurrenceBackwardArgs p, Tiles tiles, float* partial)
 {
     typedef Lane<EK, V> L;
     typedef typename L::T T;
     constexpr int R = kBackwardRows;
-    __shared__ float2 pairs[kMostWaves][V][64], met[kMostWaves][V][64];
+    __shared__ float2 pairs[kBackwardWaves][V][64], met[kBackwardWaves][V][64];
     __shared__ unsigned ticket;
     const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
     const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void recurrence_backward_kernel(Re
     }
     __syncthreads();
     float c[V];
-    carry_in<V>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, c);
+    carry_in<V, kBackwardWaves>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, c);
     auto entry_of = [&]() {
         const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
         return entry < p.n.n_states ? entry : -1;
@@ -290,19 +290,19 @@ __global__ __launch_bounds__(kThreads) void recurrence_step_kernel(RecurrenceSte
 
 namespace {
 
-constexpr int kResident = 512;          // workgroups of kMostWaves wavefronts that the chip has at a time
+constexpr int kResident = 512;          // workgroups along a sequence that the chip has at a time, forwards and backwards
 
-Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows)
+Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves)
 {
     const int64_t most = (n.T + rows - 1) / rows;
     Tiles t;
     t.groups = (n.C + 64 * V - 1) / (64 * V);
-    t.waves = most < kMostWaves ? (int)most : kMostWaves;
+    t.waves = most < waves ? (int)most : waves;
     t.segments = (most + t.waves - 1) / t.waves;
     t.batches = packed ? 1 : n.B;
     // Of a launch that fills the chip neighbours run at the same time and carries go quickly from one to the next, but what is read of pairs is taken from the
     // rows' bandwidth; others wait for their chain alone (bf16, 8192 tokens: 4096 channels 67.5 us with blocks of 4 and 71 with 16, 512 channels 30 and 22).
-    t.block = t.count() > kResident ? 4 : kMostWaves;
+    t.block = t.count() > kResident ? 4 : waves;
     return t;
 }
 
@@ -334,27 +334,25 @@ int64_t chain_bytes(const Tiles& t, int C) { return (8 * chain_words(t, C) + 15)
 bool recurrence_fits(const RecurrenceBatch& n, bool packed, int ek)
 {
     const int V = lane_channels(n, ek);
-    for (const int rows : {kForwardRows, kBackwardRows}) {
-        const Tiles t = tiles_of(n, packed, V, rows);
+    for (const Tiles& t : {tiles_of(n, packed, V, kForwardRows, kForwardWaves), tiles_of(n, packed, V, kBackwardRows, kBackwardWaves)})
         if (t.segments >= 1 << 22 || t.batches > ((int64_t)1 << 31) / t.segments || t.count() >= ((int64_t)1 << 26) / t.waves) return false;    // 2^32 threads
-    }
     return true;
 }
 
 int64_t recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek)
 {
-    return chain_bytes(tiles_of(n, packed, lane_channels(n, ek), kForwardRows), n.C);
+    return chain_bytes(tiles_of(n, packed, lane_channels(n, ek), kForwardRows, kForwardWaves), n.C);
 }
 int64_t recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek)
 {
-    const Tiles t = tiles_of(n, packed, lane_channels(n, ek), kBackwardRows);
+    const Tiles t = tiles_of(n, packed, lane_channels(n, ek), kBackwardRows, kBackwardWaves);
     return chain_bytes(t, n.C) + t.segments * t.batches * n.C * 4;
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 {
     const int V = lane_channels(a.n, ek);
-    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kForwardRows);
+    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kForwardRows, kForwardWaves);
     if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
     return with_elem(ek, [&](auto e) {
         note_kernel("recurrence_kernel", ek, V, a.n.starts != nullptr);
@@ -368,7 +366,7 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, hipStream_t st)
 {
     const int V = lane_channels(a.n, ek);
-    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kBackwardRows);
+    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kBackwardRows, kBackwardWaves);
     if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
     float* const partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + chain_bytes(tiles, a.n.C));
     return with_elem(ek, [&](auto e) {

@@ -2,7 +2,7 @@
 // from tile to tile.
 //
 // A recurrence c' = a c + b over a run of rows is one pair (A, B): c' = A c + B.  A wavefront has kRows rows of 64 lanes' channels in registers, a workgroup up
-// to 16 wavefronts one after the other in time, and their pairs meet in LDS.  Workgroups of one channel group are a chain: each adds its pair to what
+// to W wavefronts one after the other in time, and their pairs meet in LDS.  Workgroups of one channel group are a chain: each adds its pair to what
 // comes from the one before.  They take their places from a counter, so that whoever waits, waits for workgroups that have begun; each word of
 // a pair is stored with a flag in one 64-bit store, so that no fence is needed.  Every block-th workgroup passes on the carry itself, those
 // between their pairs, which a successor reads all at once, a wavefront each, and folds in their order: a chain of a link (1 us) for each
@@ -16,12 +16,11 @@ namespace swconv {
 
 typedef unsigned long long Word;
 
-constexpr int kMostWaves = 16;
 constexpr float kCut = -1.f;            // A of rows among which a sequence begins: nothing from before reaches their end (decays are >= 0)
 
 struct Tiles {
     int groups, waves;                  // channel groups; wavefronts of a workgroup
-    int block;                          // workgroups from one carry that is passed on to the next, at most kMostWaves
+    int block;                          // workgroups from one carry that is passed on to the next, at most W
     int64_t segments, batches;          // workgroups along a sequence; sequences (1: packed)
     int64_t count() const { return groups * segments * batches; }
 };
@@ -125,10 +124,10 @@ __device__ __forceinline__ void wait_for(const Word* at, Word (&w)[N])
     }
 }
 
-// What comes into segment `segment` of the chain for the V channels at `at`, by all of a workgroup of kMostWaves wavefronts: each waits for one
+// What comes into segment `segment` of the chain for the V channels at `at`, by all of a workgroup of W wavefronts: each waits for one
 // of the pairs since the last carry that was passed on, the last one for that carry; they meet in LDS and are folded in their order.  One
 // trip to memory, whatever their number.
-template <int V>
+template <int V, int W>
 __device__ __forceinline__ void incoming(const Chain& chain, int segment, int64_t at, int wave, float2 (*met)[V][64], float (&c)[V])
 {
     const int lane = threadIdx.x % 64, since = segment % chain.block, first = segment - since;
@@ -138,15 +137,15 @@ __device__ __forceinline__ void incoming(const Chain& chain, int segment, int64_
 #pragma unroll
         for (int v = 0; v < V; ++v) met[wave][v][lane] = make_float2(A_of(w[v]), low_of(w[v]));
     }
-    if (wave == kMostWaves - 1) {
+    if (wave == W - 1) {
         if (first > 0) wait_for<V>(chain.carry(first - 1, at), w);
 #pragma unroll
-        for (int v = 0; v < V; ++v) met[kMostWaves - 1][v][lane].x = first > 0 ? low_of(w[v]) : 0.f;
+        for (int v = 0; v < V; ++v) met[W - 1][v][lane].x = first > 0 ? low_of(w[v]) : 0.f;
     }
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        c[v] = met[kMostWaves - 1][v][lane].x;
+        c[v] = met[W - 1][v][lane].x;
         for (int k = 0; k < since; ++k) c[v] = after(met[k][v][lane].x, met[k][v][lane].y, c[v]);
     }
 }
@@ -170,7 +169,7 @@ __device__ __forceinline__ int64_t take_ticket(const Tiles& tiles, const Chain& 
 }
 
 // What comes into a wavefront's rows, from its workgroup's pairs and, of several along a sequence, from the chain; passes on what goes to the next workgroup.
-template <int V>
+template <int V, int W>
 __device__ __forceinline__ void carry_in(const Chain& chain, const Tiles& tiles, const Place& place, int64_t at, int wave, const float2 (*pairs)[V][64],
                                          float2 (*met)[V][64], float (&c)[V])
 {
@@ -178,19 +177,19 @@ __device__ __forceinline__ void carry_in(const Chain& chain, const Tiles& tiles,
 #pragma unroll
     for (int v = 0; v < V; ++v) c[v] = 0.f;
     if (tiles.segments > 1) {
-        const bool passes_on = place.segment % tiles.block == tiles.block - 1, mine = wave == kMostWaves - 1 && place.segment < tiles.segments - 1;
+        const bool passes_on = place.segment % tiles.block == tiles.block - 1, mine = wave == W - 1 && place.segment < tiles.segments - 1;
         float A[V], B[V];
         if (mine) {
 #pragma unroll
             for (int v = 0; v < V; ++v) A[v] = 1.f, B[v] = 0.f;
-            for (int w = 0; w < kMostWaves; ++w)
+            for (int w = 0; w < W; ++w)
 #pragma unroll
                 for (int v = 0; v < V; ++v) append(pairs[w][v][lane].x, pairs[w][v][lane].y, A[v], B[v]);
             if (!passes_on)
 #pragma unroll
                 for (int v = 0; v < V; ++v) publish(chain.pair(place.segment, at + v), pair_word(A[v], B[v]));
         }
-        incoming<V>(chain, place.segment, at, wave, met, c);
+        incoming<V, W>(chain, place.segment, at, wave, met, c);
         if (mine && passes_on)
 #pragma unroll
             for (int v = 0; v < V; ++v) publish(chain.carry(place.segment, at + v), carry_word(after(A[v], B[v], c[v])));

@@ -8,6 +8,17 @@ from .binding import SW_ERR_SHAPE, SwAdaptersDims, SwError, SwGatedRecurrenceDim
 from .layers import _heads, _on, _plain, _rows, _type, _workspace
 
 
+def _elsewhere(*tensors):
+    """The GPU of a call's tensors where it is not the current one (None: it is, or there is none: tensors off the GPU are refused by name)."""
+    import torch
+
+    there = [t.device for t in tensors if t is not None and t.is_cuda]
+    for device in there:
+        if device != there[0]:
+            raise ValueError(f"tensors on {there[0]} and {device} in one call")
+    return there[0] if there and there[0].index != torch.cuda.current_device() else None
+
+
 def _channels(t, shape, dtype, name):
     """(address, strides) of a tensor of that shape, [..., C] with one or two dimensions in front, channels contiguous."""
     if not t.is_cuda:
@@ -63,6 +74,10 @@ def sw_gated_recurrence(x, decay_gate, input_gate, log_decay, starts=None, state
             return _done(y, "sw_gated_recurrence")
     import torch
 
+    other = _elsewhere(x, decay_gate, input_gate, log_decay, starts, state, slots, final_state, out)
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_gated_recurrence(x, decay_gate, input_gate, log_decay, starts, state, slots, final_state, out, stream)
     dims, g, s, at = _recurrence(x, log_decay, starts, slots, "sw_gated_recurrence")
     held = state if state is not None else final_state
     if held is not None:
@@ -91,6 +106,10 @@ def sw_gated_recurrence_backward(dh, x, decay_gate, input_gate, log_decay, h, st
             return _done(y, "sw_gated_recurrence_backward")
     import torch
 
+    other = _elsewhere(dh, x, decay_gate, input_gate, log_decay, h, starts, state, slots, d_final_state, d_state, *(out or ()))
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_gated_recurrence_backward(dh, x, decay_gate, input_gate, log_decay, h, starts, state, slots, d_final_state, d_state, params, out, stream)
     dims, g, s, at = _recurrence(x, log_decay, starts, slots, "sw_gated_recurrence_backward")
     if state is not None:
         dims.n_states = state.shape[0] if state.dim() else 0
@@ -120,6 +139,10 @@ def sw_gated_recurrence_step(x, decay_gate, input_gate, log_decay, state, slots=
             return _done(y, "sw_gated_recurrence_step")
     import torch
 
+    other = _elsewhere(x, decay_gate, input_gate, log_decay, state, slots, out)
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_gated_recurrence_step(x, decay_gate, input_gate, log_decay, state, slots, out, stream)
     if x.dim() != 2:
         raise ValueError(f"sw_gated_recurrence_step: x has 2 dimensions, got {tuple(x.shape)}")
     if 0 in x.shape:
@@ -166,6 +189,10 @@ def sw_head_norm(q, k, q_weight=None, k_weight=None, frequencies=None, positions
             return _done(y, "sw_head_norm")
     import torch
 
+    other = _elsewhere(q, k, q_weight, k_weight, frequencies, positions, *(out or ()))
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_head_norm(q, k, q_weight, k_weight, frequencies, positions, eps, interleaved, out, stream)
     dims, shape, kv_shape, wq, wk, f, at = _head_norm(q, k, q_weight, k_weight, frequencies, positions, eps, interleaved, "sw_head_norm")
     with _on(stream):
         if out is None:
@@ -186,6 +213,10 @@ def sw_head_norm_backward(dq, dk, q, k, q_weight=None, k_weight=None, frequencie
             return _done(y, "sw_head_norm_backward")
     import torch
 
+    other = _elsewhere(dq, dk, q, k, q_weight, k_weight, frequencies, positions, *(out or ()))
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_head_norm_backward(dq, dk, q, k, q_weight, k_weight, frequencies, positions, eps, interleaved, params, out, stream)
     dims, shape, kv_shape, wq, wk, f, at = _head_norm(q, k, q_weight, k_weight, frequencies, positions, eps, interleaved, "sw_head_norm_backward")
     L = lib()
     sums, work, need = (None, None), None, 0
@@ -218,6 +249,10 @@ def sw_adapters(x, a, b, y, scales=None, slots=None, starts=None, out=None, stre
             return _done(z, "sw_adapters")
     import torch
 
+    other = _elsewhere(x, a, b, y, scales, slots, starts, out)
+    if other is not None:
+        with torch.cuda.device(other):
+            return sw_adapters(x, a, b, y, scales, slots, starts, out, stream)
     what = "sw_adapters"
     if x.dim() not in ((2,) if starts is not None else (2, 3)) or y.dim() != x.dim() or a.dim() != 3:
         raise ValueError(f"{what}: x and y have 2 or 3 dimensions (2 with starts), a 3, got {tuple(x.shape)}, {tuple(y.shape)}, {tuple(a.shape)}")
