@@ -14,12 +14,14 @@ __global__ __launch_bounds__(kThreads) void fold_kernel(FoldArgs p)
     const int lane = threadIdx.x % 8, first = threadIdx.x / 8;
     const int i = blockIdx.x * 32 + lane * 4;
     R::floats s = 0.f;
-    for (int k = first; k < p.parts; k += 8 * kRows) {
+    const auto of = blockIdx.y ? p.of[1] : p.of[0];
+    if (!of.out) return;
+    for (int k = first; k < of.parts; k += 8 * kRows) {
         R::floats v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             v[j] = 0.f;
-            if (k + j * kRows < p.parts && i < p.width) v[j] = R::load(p.partial + (int64_t)(k + j * kRows) * p.width, i, p.width);
+            if (k + j * kRows < of.parts && i < p.width) v[j] = R::load(of.partial + (int64_t)(k + j * kRows) * p.width, i, p.width);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += v[j];
@@ -33,19 +35,15 @@ __global__ __launch_bounds__(kThreads) void fold_kernel(FoldArgs p)
     if (threadIdx.x >= 8) return;
     for (int k = 1; k < kThreads / 64; ++k) s += lds[k][lane];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int c = i + e;
-        if (c >= p.width) continue;
-        float* out = c < p.split ? p.out[0] : p.out[1];
-        if (out) out[c < p.split ? c : c - p.split] = s[e];
-    }
+    for (int e = 0; e < 4; ++e)
+        if (i + e < p.width) of.out[i + e] = s[e];
 }
 
 }  // namespace
 
 hipError_t launch_fold(const FoldArgs& a, hipStream_t st)
 {
-    hipLaunchKernelGGL(fold_kernel, dim3((a.width + 31) / 32), dim3(kThreads), 0, st, a);
+    hipLaunchKernelGGL(fold_kernel, dim3((a.width + 31) / 32, a.of[1].out ? 2 : 1), dim3(kThreads), 0, st, a);
     return hipGetLastError();
 }
 

@@ -1,138 +1,408 @@
-// Norms of the heads of queries and keys with their rotation: a wavefront a head.
+// Norms of the heads of queries and keys with their rotation by position, and the backward pass.
+//
+// Both are bound by memory: a head is read once into the registers of a few lanes, folded there, turned and written once.  A lane has the two vectors
+// of 16 bytes whose elements turn with each other: no element changes its lane.  A turn is the same for all heads of a token: a group of lanes
+// has several heads of one, and takes sine and cosine once for them (100 cycles an angle, of which a lane has 4 or 8, beside 700 for the rest of
+// a head).  Queries and keys are workgroups of their own, so that the weights, and the sums of their gradients, stay in registers.
+#include <initializer_list>
+
 #include "sw_sequence.h"
 
 namespace swconv {
 
 namespace {
 
-__device__ __forceinline__ float wave_sum(float v)
+// ---- sine and cosine ----------------------------------------------------------------------------------------------------------------
+
+// Of position * frequency, taken in 64 bits, at any 32-bit position: quarter turns are the product with 2 / pi in two 64-bit parts, so that what is left of whole
+// ones has fp32's bits however many there are.
+// The rest, y quarters in [-1/2, 1/2], by the Taylor series in x = pi/2 y, |x| <= pi/4: x - x^3/6 ... x^9/9! (the next term is 2e-9), 1 - x^2/2 ... - x^10/10! (5e-10).
+__device__ __forceinline__ void turn(int position, double frequency, float* c, float* s)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d, 64);
-    return v;
+    constexpr double kQuarters = 0.6366197723675814, kQuartersLow = -3.935735335036497e-17;
+    const double f = (double)position * frequency, whole = __builtin_rint(f * kQuarters);
+    const float y = (float)__builtin_fma(f, kQuartersLow, __builtin_fma(f, kQuarters, -whole)), z = y * y;
+    const int q = (int)(unsigned)(long long)whole;
+    float sn = 1.60441185e-4f;                                      // (pi/2)^9 / 9!
+    sn = __builtin_fmaf(sn, z, -4.68175414e-3f);
+    sn = __builtin_fmaf(sn, z, 7.96926262e-2f);
+    sn = __builtin_fmaf(sn, z, -0.645964098f);
+    sn = __builtin_fmaf(sn, z, 1.57079633f) * y;
+    float cs = -2.52020424e-5f;                                     // (pi/2)^10 / 10!
+    cs = __builtin_fmaf(cs, z, 9.19260275e-4f);
+    cs = __builtin_fmaf(cs, z, -2.08634807e-2f);
+    cs = __builtin_fmaf(cs, z, 0.253669508f);
+    cs = __builtin_fmaf(cs, z, -1.23370055f);
+    cs = __builtin_fmaf(cs, z, 1.f);
+    const float a = q & 1 ? sn : cs, b = q & 1 ? cs : sn;
+    *c = (q + 1) & 2 ? -a : a;
+    *s = q & 2 ? -b : b;
 }
 
-// cos and sin of position * frequency
-__device__ __forceinline__ void angle(int position, float frequency, float* c, float* s)
+// ---- which workgroups ------------------------------------------------------------------------------------------------------------------
+
+constexpr int kThreads = 256;
+
+// Workgroups of the queries, then of the keys.  A group of lanes has heads chunk, chunk + chunks ... of a row.
+struct HeadGroups {
+    int groups[2], chunks[2];
+    __host__ __device__ int all() const { return groups[0] + groups[1]; }
+};
+
+// A group's row and chunk, on from one to the next a launch apart.
+struct Task {
+    int64_t row;
+    int chunk;
+    int64_t step_rows;
+    int step_chunks, chunks;
+    __device__ __forceinline__ Task(int64_t first, int64_t step, int chunks_) : chunks(chunks_)
+    {
+        row = first / chunks, chunk = (int)(first % chunks);
+        step_rows = step / chunks, step_chunks = (int)(step % chunks);
+    }
+    __device__ __forceinline__ void next()
+    {
+        row += step_rows, chunk += step_chunks;
+        if (chunk >= chunks) chunk -= chunks, ++row;
+    }
+};
+
+template <class T>
+__device__ __forceinline__ const T* row_of(const AttentionOperand& o, int64_t batch, int64_t token)
 {
-    const double f = (double)position * (double)frequency;
-    *c = (float)cos(f), *s = (float)sin(f);
+    return static_cast<const T*>(o.p) + batch * o.batch + token * o.token;
 }
 
-constexpr int kMost = 4;        // elements of a lane: heads of up to 256
+// ---- two vectors a lane ------------------------------------------------------------------------------------------------------------------
 
-template <int EK, bool BACKWARD>
-__global__ __launch_bounds__(256) void head_norm_kernel(HeadNormArgs p)
-{
-    typedef typename ElemOf<EK>::type T;
-    __shared__ float lds[4][256];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, heads = p.side[0].heads + p.side[1].heads;
-    const int64_t tasks = p.B * p.T * heads;
-    float sums[2][kMost] = {};
-    for (int64_t task = blockIdx.x * 4 + wave; task < tasks; task += gridDim.x * 4) {
-        const int64_t row = task / heads, batch = row / p.T, token = row % p.T;
-        const int all = (int)(task % heads), which = all >= p.side[0].heads, head = all - (which ? p.side[0].heads : 0);
-        const HeadNormSide side = which ? p.side[1] : p.side[0];
-        auto place = [&](const AttentionOperand& o) { return static_cast<const T*>(o.p) + batch * o.batch + token * o.token + (int64_t)head * o.head; };
-        const T* x = place(side.x);
-        const int position = p.positions ? p.positions[row] : (int)token;
-        float v[kMost], w[kMost], other[kMost] = {}, c[kMost] = {}, s[kMost] = {}, sum = 0.f;
+// A head is its pairs, and pairs that do not turn: its other elements, halved the same way.  A lane has VEC pairs (U, W): two vectors, half of their part of the
+// head apart or, INTERLEAVED, next to each other.  Where a part is no whole number of VEC pairs, its last lane shares some with its neighbour: it
+// leaves the first `skip` out of sums, and stores what the other stores.
+template <int EK, bool INTERLEAVED>
+struct HeadLane {
+    typedef Row<EK> R;
+    typedef typename R::T T;
+    typedef typename R::floats floats;
+    static constexpr int VEC = R::VEC;
+    int first, second, skip, pair;      // where the vectors begin; VEC: no lane of the head; the first pair, -1: they do not turn
+    __device__ __forceinline__ HeadLane(int lane, int D, int pairs)
+    {
+        const int turning = (pairs + VEC - 1) / VEC, still = D / 2 - pairs, lanes = turning + (still + VEC - 1) / VEC;
+        const bool mine = lane < lanes;
+        if (!mine) lane = 0;
+        const bool turns = lane < turning;
+        const int base = turns ? 0 : 2 * pairs, count = turns ? pairs : still, nominal = (turns ? lane : lane - turning) * VEC;
+        const int start = nominal < count - VEC ? nominal : count - VEC;
+        first = base + (INTERLEAVED ? 2 * start : start);
+        second = INTERLEAVED ? first + VEC : first + count;
+        skip = mine ? nominal - start : VEC;
+        pair = turns ? start : -1;
+    }
+    struct Raw {
+        typename R::vec a, b;
+    };
+    __device__ __forceinline__ Raw load(const T* head) const { return Raw{R::load(head + first), R::load(head + second)}; }
+    static __device__ __forceinline__ void split(const Raw& r, floats& u, floats& w)
+    {
+        const floats a = __builtin_convertvector(r.a, floats), b = __builtin_convertvector(r.b, floats);
+        if constexpr (INTERLEAVED) {
 #pragma unroll
-        for (int k = 0; k < kMost; ++k) {
-            const int e = lane + 64 * k;
-            v[k] = e < p.D ? (float)x[e] : 0.f;
-            w[k] = e < p.D && side.weight ? side.weight[e] : 1.f;
-            sum += v[k] * v[k];
-        }
-        const float r = 1.f / sqrtf(wave_sum(sum) / (float)p.D + p.eps);
-        // what turns with element e: its partner, and the angle (the sign is that of the partner's term)
-        int with[kMost];
-#pragma unroll
-        for (int k = 0; k < kMost; ++k) {
-            const int e = lane + 64 * k;
-            with[k] = e;
-            if (e >= 2 * p.pairs) continue;
-            const bool second = p.interleaved ? e % 2 : e >= p.pairs;
-            const int pair = p.interleaved ? e / 2 : second ? e - p.pairs : e;
-            with[k] = p.interleaved ? e ^ 1 : second ? e - p.pairs : e + p.pairs;
-            angle(position, p.frequencies[pair], &c[k], &s[k]);
-            if (!second) s[k] = -s[k];
-            if (BACKWARD) s[k] = -s[k];
-        }
-        if constexpr (!BACKWARD) {
-            T* y = const_cast<T*>(place(side.y));
-#pragma unroll
-            for (int k = 0; k < kMost; ++k)
-                if (lane + 64 * k < p.D && with[k] != lane + 64 * k)
-                    other[k] = (float)x[with[k]] * r * (side.weight ? side.weight[with[k]] : 1.f);
-            // (y may be x: no lane stores before all have read)
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int k = 0; k < kMost; ++k) {
-                const int e = lane + 64 * k;
-                const float n = v[k] * r * w[k];
-                if (e < p.D) y[e] = (T)(with[k] == e ? n : n * c[k] + other[k] * s[k]);
-            }
+            for (int m = 0; m < VEC; ++m) u[m] = m < VEC / 2 ? a[2 * m] : b[2 * m - VEC], w[m] = m < VEC / 2 ? a[2 * m + 1] : b[2 * m + 1 - VEC];
         } else {
-            const T* dy = place(side.dy);
-            T* dx = const_cast<T*>(place(side.y));
-            float g[kMost], dot = 0.f;
+            u = a, w = b;
+        }
+    }
+    static __device__ __forceinline__ void join(const floats& u, const floats& w, floats& a, floats& b)
+    {
+        if constexpr (INTERLEAVED) {
 #pragma unroll
-            for (int k = 0; k < kMost; ++k) {
-                const int e = lane + 64 * k;
-                g[k] = e < p.D ? (float)dy[e] : 0.f;
-                if (e < p.D && with[k] != e) g[k] = g[k] * c[k] + (float)dy[with[k]] * s[k];
-                v[k] *= r;
-                if (e < p.D) sums[which][k] += g[k] * v[k];
-                g[k] *= w[k];
-                dot += g[k] * v[k];
+            for (int m = 0; m < VEC; ++m) a[m] = m % 2 ? w[m / 2] : u[m / 2], b[m] = m % 2 ? w[(VEC + m) / 2] : u[(VEC + m) / 2];
+        } else {
+            a = u, b = w;
+        }
+    }
+    __device__ __forceinline__ void store(T* head, const floats& u, const floats& w) const
+    {
+        floats a, b;
+        join(u, w, a, b);
+        if (skip < VEC) {
+            R::store(head + first, a);
+            R::store(head + second, b);
+        }
+    }
+    __device__ __forceinline__ void weights(const float* p, floats& u, floats& w) const
+    {
+        u = 1.f, w = 1.f;
+        if (!p) return;
+        const floats a = R::load_floats(p + first), b = R::load_floats(p + second);
+        if constexpr (INTERLEAVED) {
+#pragma unroll
+            for (int m = 0; m < VEC; ++m) u[m] = m < VEC / 2 ? a[2 * m] : b[2 * m - VEC], w[m] = m < VEC / 2 ? a[2 * m + 1] : b[2 * m + 1 - VEC];
+        } else {
+            u = a, w = b;
+        }
+    }
+    // the sum of x y over the pairs that are this lane's alone
+    __device__ __forceinline__ float dot(const floats& xu, const floats& xw, const floats& yu, const floats& yw) const
+    {
+        float s = 0.f;
+#pragma unroll
+        for (int m = 0; m < VEC; ++m) s = __builtin_fmaf(xu[m], yu[m], __builtin_fmaf(xw[m], yw[m], s));
+        if (skip) {
+            s = 0.f;
+#pragma unroll
+            for (int m = 0; m < VEC; ++m)
+                if (m >= skip) s = __builtin_fmaf(xu[m], yu[m], __builtin_fmaf(xw[m], yw[m], s));
+        }
+        return s;
+    }
+};
+
+template <int EK, int G, bool INTERLEAVED, bool BACKWARD>
+__global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs p, HeadGroups groups)
+{
+    typedef HeadLane<EK, INTERLEAVED> H;
+    typedef typename H::T T;
+    typedef typename H::floats floats;
+    constexpr int VEC = H::VEC, kGroups = kThreads / G;
+    const int lane = threadIdx.x % G;
+    const bool which = (int)blockIdx.x >= groups.groups[0];
+    const int block = which ? blockIdx.x - groups.groups[0] : blockIdx.x;
+    const HeadNormSide side = which ? p.side[1] : p.side[0];
+    const H at(lane, p.D, p.pairs);
+    floats wu, ww, su = 0.f, sw = 0.f;
+    at.weights(side.weight, wu, ww);
+    double frequency[VEC];
+#pragma unroll
+    for (int m = 0; m < VEC; ++m) frequency[m] = at.pair < 0 ? 0. : (double)p.frequencies[at.pair + m];
+    const float inv = 1.f / (float)p.D;
+    const int64_t rows = p.B * p.T;
+    Task task((int64_t)block * kGroups + threadIdx.x / G, (int64_t)(which ? groups.groups[1] : groups.groups[0]) * kGroups, which ? groups.chunks[1] : groups.chunks[0]);
+    // (lanes of a group go on together; those of a wavefront's other groups may have ended)
+    for (; task.row < rows; task.next()) {
+        const int64_t batch = p.B == 1 ? 0 : task.row / p.T, token = task.row - batch * p.T;
+        const T *x = row_of<T>(side.x, batch, token), *dy = BACKWARD ? row_of<T>(side.dy, batch, token) : nullptr;
+        T* y = const_cast<T*>(row_of<T>(side.y, batch, token));
+        typename H::Raw raw = at.load(x + task.chunk * side.x.head), raw_dy;
+        if constexpr (BACKWARD) raw_dy = at.load(dy + task.chunk * side.dy.head);
+        const int position = p.positions ? p.positions[task.row] : (int)token;
+        floats c, s;
+#pragma unroll
+        for (int m = 0; m < VEC; ++m) {
+            float cm, sm;
+            turn(position, frequency[m], &cm, &sm);
+            c[m] = cm, s[m] = sm;
+        }
+        for (int head = task.chunk; head < side.heads; head += task.chunks) {
+            floats u, w;
+            H::split(raw, u, w);
+            const int64_t next = head + task.chunks < side.heads ? head + task.chunks : head;
+            raw = at.load(x + next * side.x.head);
+            const float r = 1.f / sqrtf(lanes_sum<G>(at.dot(u, w, u, w)) * inv + p.eps);
+            u *= r, w *= r;
+            if constexpr (BACKWARD) {
+                floats du, dw;
+                H::split(raw_dy, du, dw);
+                raw_dy = at.load(dy + next * side.dy.head);
+                floats gu = du * c + dw * s, gw = dw * c - du * s;
+                su += gu * u, sw += gw * w;
+                gu *= wu, gw *= ww;
+                const float mean = lanes_sum<G>(at.dot(gu, gw, u, w)) * inv;
+                at.store(y + head * side.y.head, (gu - u * mean) * r, (gw - w * mean) * r);
+            } else {
+                u *= wu, w *= ww;
+                at.store(y + head * side.y.head, u * c - w * s, u * s + w * c);
             }
-            dot = wave_sum(dot) / (float)p.D;
-#pragma unroll
-            for (int k = 0; k < kMost; ++k)
-                if (lane + 64 * k < p.D) dx[lane + 64 * k] = (T)(r * (g[k] - v[k] * dot));
         }
     }
     if constexpr (BACKWARD) {
         if (!p.work) return;
-        for (int which = 0; which < 2; ++which) {
-            __syncthreads();
+        // the sums of a workgroup's groups of lanes, an element a thread
+        __shared__ float lds[kGroups][G][2 * VEC + 1];
+        floats a, b;
+        H::join(su, sw, a, b);
 #pragma unroll
-            for (int k = 0; k < kMost; ++k) lds[wave][lane + 64 * k] = sums[which][k];
-            __syncthreads();
-            if ((int)threadIdx.x < p.D)
-                static_cast<float*>(p.work)[((int64_t)blockIdx.x * 2 + which) * p.D + threadIdx.x] =
-                    lds[0][threadIdx.x] + lds[1][threadIdx.x] + lds[2][threadIdx.x] + lds[3][threadIdx.x];
-        }
+        for (int m = 0; m < VEC; ++m) lds[threadIdx.x / G][lane][m] = a[m], lds[threadIdx.x / G][lane][VEC + m] = b[m];
+        __syncthreads();
+        const int e = threadIdx.x;
+        if (e >= G * 2 * VEC) return;
+        const H of(e / (2 * VEC), p.D, p.pairs);
+        const int m = e % (2 * VEC);
+        float sum = 0.f;
+        for (int g = 0; g < kGroups; ++g) sum += lds[g][e / (2 * VEC)][m];
+        // (lanes that share an element have the same sum of it)
+        if (of.skip < VEC) static_cast<float*>(p.work)[(int64_t)blockIdx.x * p.D + (m < VEC ? of.first + m : of.second + m - VEC)] = sum;
     }
 }
 
-__global__ __launch_bounds__(256) void head_norm_fold_kernel(const float* partial, int parts, int D, float* dq, float* dk)
+// ---- any other width: a wavefront a head, single elements ----------------------------------------------------------------------------------
+
+constexpr int kMost = 4;        // elements of a lane: heads of up to 256
+
+template <int EK, bool BACKWARD>
+__global__ __launch_bounds__(kThreads) void head_norm_any_kernel(HeadNormArgs p, HeadGroups groups)
 {
-    const int e = threadIdx.x;
-    float* out = blockIdx.x ? dk : dq;
-    if (e >= D || !out) return;
-    float s = 0.f;
-    for (int k = 0; k < parts; ++k) s += partial[((int64_t)k * 2 + blockIdx.x) * D + e];
-    out[e] = s;
+    typedef typename ElemOf<EK>::type T;
+    __shared__ float lds[kThreads / 64][64 * kMost];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const bool which = (int)blockIdx.x >= groups.groups[0];
+    const int block = which ? blockIdx.x - groups.groups[0] : blockIdx.x;
+    const HeadNormSide side = which ? p.side[1] : p.side[0];
+    float weight[kMost], sums[kMost] = {}, sign[kMost];
+    double frequency[kMost];
+    int with[kMost];                // what turns with the lane's elements: themselves, where they do not turn
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+        const int e = lane + 64 * k, pair = p.interleaved ? e / 2 : e % (p.pairs ? p.pairs : 1);
+        const bool turns = e < 2 * p.pairs, second = p.interleaved ? e % 2 : e >= p.pairs;
+        with[k] = !turns ? e : p.interleaved ? e ^ 1 : second ? e - p.pairs : e + p.pairs;
+        frequency[k] = turns ? (double)p.frequencies[pair] : 0.;
+        sign[k] = second != BACKWARD ? 1.f : -1.f;
+        weight[k] = e < p.D && side.weight ? side.weight[e] : 1.f;
+    }
+    const int64_t rows = p.B * p.T;
+    Task task((int64_t)block * (kThreads / 64) + wave, (int64_t)(which ? groups.groups[1] : groups.groups[0]) * (kThreads / 64), which ? groups.chunks[1] : groups.chunks[0]);
+    for (; task.row < rows; task.next()) {
+        const int64_t batch = p.B == 1 ? 0 : task.row / p.T, token = task.row - batch * p.T;
+        const int position = p.positions ? p.positions[task.row] : (int)token;
+        float c[kMost], s[kMost];
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) {
+            turn(position, frequency[k], &c[k], &s[k]);
+            s[k] *= sign[k];
+        }
+        for (int head = task.chunk; head < side.heads; head += task.chunks) {
+            const T* x = row_of<T>(side.x, batch, token) + head * side.x.head;
+            T* y = const_cast<T*>(row_of<T>(side.y, batch, token)) + head * side.y.head;
+            float v[kMost], sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < kMost; ++k) {
+                v[k] = lane + 64 * k < p.D ? (float)x[lane + 64 * k] : 0.f;
+                sum = __builtin_fmaf(v[k], v[k], sum);
+            }
+            const float r = 1.f / sqrtf(lanes_sum<64>(sum) / (float)p.D + p.eps);
+            // the elements, forwards normed, and their partners in a wavefront's row of LDS (no other wavefront has it)
+            auto turned = [&](const float(&f)[kMost], float(&out)[kMost]) {
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) lds[wave][lane + 64 * k] = f[k];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) out[k] = f[k] * c[k] + (with[k] != lane + 64 * k ? lds[wave][with[k]] * s[k] : 0.f);
+                __builtin_amdgcn_wave_barrier();
+            };
+            if constexpr (!BACKWARD) {
+                float n[kMost], t[kMost];
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) n[k] = v[k] * r * weight[k];
+                turned(n, t);
+#pragma unroll
+                for (int k = 0; k < kMost; ++k)
+                    if (lane + 64 * k < p.D) y[lane + 64 * k] = (T)t[k];
+            } else {
+                const T* dy = row_of<T>(side.dy, batch, token) + head * side.dy.head;
+                float d[kMost], g[kMost], dot = 0.f;
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) d[k] = lane + 64 * k < p.D ? (float)dy[lane + 64 * k] : 0.f;
+                turned(d, g);
+#pragma unroll
+                for (int k = 0; k < kMost; ++k) {
+                    v[k] *= r;
+                    sums[k] = __builtin_fmaf(g[k], v[k], sums[k]);
+                    g[k] *= weight[k];
+                    dot = __builtin_fmaf(g[k], v[k], dot);
+                }
+                dot = lanes_sum<64>(dot) / (float)p.D;
+#pragma unroll
+                for (int k = 0; k < kMost; ++k)
+                    if (lane + 64 * k < p.D) y[lane + 64 * k] = (T)(r * (g[k] - v[k] * dot));
+            }
+        }
+    }
+    if constexpr (BACKWARD) {
+        if (!p.work) return;
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) lds[wave][lane + 64 * k] = sums[k];
+        __syncthreads();
+        const int e = threadIdx.x;
+        if (e < p.D) static_cast<float*>(p.work)[(int64_t)blockIdx.x * p.D + e] = lds[0][e] + lds[1][e] + lds[2][e] + lds[3][e];
+    }
 }
 
-unsigned groups_of(int64_t tasks)
+// ---- launches ------------------------------------------------------------------------------------------------------------------------------
+
+// f(lanes a head): an integral constant, 0 where single elements have to do
+template <int EK, class F>
+hipError_t with_group(const HeadNormArgs& a, F&& f)
 {
-    const int64_t want = (tasks + 3) / 4;
-    return (unsigned)(want < 2048 ? want : 2048);
+    constexpr int VEC = Row<EK>::VEC;
+    const int still = a.D / 2 - a.pairs, lanes = (a.pairs + VEC - 1) / VEC + (still + VEC - 1) / VEC;
+    if (a.D % 2 || (a.pairs && a.pairs < VEC) || (still && still < VEC)) return f(std::integral_constant<int, 0>());
+    if (lanes <= 4) return f(std::integral_constant<int, 4>());
+    if (lanes <= 8) return f(std::integral_constant<int, 8>());
+    if (lanes <= 16) return f(std::integral_constant<int, 16>());
+    if constexpr (EK == kElemF32)
+        if (lanes <= 32) return f(std::integral_constant<int, 32>());
+    return f(std::integral_constant<int, 0>());         // (256 elements in two ragged parts)
+}
+
+constexpr int kForwardWaves = 8192, kBackwardGroups = 1024;
+
+// Heads of a row go to several groups of lanes as far as wavefronts are few, to one at most kHeads at a time otherwise; workgroups are what the chip holds.
+HeadGroups head_groups(const HeadNormArgs& a, int lanes, int most_groups)
+{
+    constexpr int kHeads = 8;
+    const int per = kThreads / lanes;
+    const int64_t rows = a.B * a.T;
+    HeadGroups g;
+    int64_t want[2];
+    for (int i = 0; i < 2; ++i) {
+        const int heads = a.side[i].heads;
+        int64_t each = rows * heads * lanes / 64 / (kForwardWaves / 2);     // heads a group of lanes
+        each = each < 1 ? 1 : each > kHeads ? kHeads : each;
+        g.chunks[i] = (int)((heads + each - 1) / each);
+        want[i] = (rows * g.chunks[i] + per - 1) / per;
+    }
+    // (in proportion to the heads there are)
+    for (int i = 0; i < 2; ++i) {
+        const int64_t share = 1 + (int64_t)most_groups * a.side[i].heads / (a.side[0].heads + a.side[1].heads);
+        g.groups[i] = (int)(want[i] < share ? want[i] : share);
+    }
+    return g;
 }
 
 }  // namespace
 
-int64_t head_norm_backward_workspace(int64_t rows, int heads, int kv_heads, int D) { return (int64_t)groups_of(rows * (heads + kv_heads)) * 2 * D * 4; }
+int64_t head_norm_backward_workspace(const HeadNormArgs& a)
+{
+    int most = 0;
+    for (const int ek : {kElemF32, kElemBF16, kElemF16})
+        (void)with_elem(ek, [&](auto e) {
+            return with_group<e()>(a, [&](auto lanes) {
+                const int all = head_groups(a, lanes() ? lanes() : 64, kBackwardGroups).all();
+                if (all > most) most = all;
+                return hipSuccess;
+            });
+        });
+    return (int64_t)most * a.D * 4;
+}
 
 hipError_t launch_head_norm(const HeadNormArgs& a, int ek, hipStream_t st)
 {
     return with_elem(ek, [&](auto e) {
-        note_kernel("head_norm_kernel", ek);
-        hipLaunchKernelGGL((head_norm_kernel<e(), false>), dim3(groups_of(a.B * a.T * (a.side[0].heads + a.side[1].heads))), dim3(256), 0, st, a);
-        return hipGetLastError();
+        return with_group<e()>(a, [&](auto lanes) {
+            const HeadGroups g = head_groups(a, lanes() ? lanes() : 64, kForwardWaves / (kThreads / 64));
+            const dim3 grid(g.all()), block(kThreads);
+            if constexpr (lanes() == 0) {
+                SW_NOTED_LAUNCH(note_kernel("head_norm_any_kernel", ek), (head_norm_any_kernel<e(), false>), grid, block, 0, st, a, g);
+            } else {
+                note_kernel("head_norm_kernel", ek, lanes(), a.interleaved);
+                if (a.interleaved)
+                    hipLaunchKernelGGL((head_norm_kernel<e(), lanes(), true, false>), grid, block, 0, st, a, g);
+                else
+                    hipLaunchKernelGGL((head_norm_kernel<e(), lanes(), false, false>), grid, block, 0, st, a, g);
+            }
+            return hipGetLastError();
+        });
     });
 }
 
@@ -141,13 +411,23 @@ hipError_t launch_head_norm_backward(const HeadNormArgs& args, int ek, hipStream
     HeadNormArgs a = args;
     if (!a.side[0].dweight && !a.side[1].dweight) a.work = nullptr;
     return with_elem(ek, [&](auto e) {
-        const unsigned groups = groups_of(a.B * a.T * (a.side[0].heads + a.side[1].heads));
-        note_kernel("head_norm_backward_kernel", ek);
-        hipLaunchKernelGGL((head_norm_kernel<e(), true>), dim3(groups), dim3(256), 0, st, a);
-        if (const hipError_t err = hipGetLastError()) return err;
-        if (a.work)
-            hipLaunchKernelGGL(head_norm_fold_kernel, dim3(2), dim3(256), 0, st, static_cast<const float*>(a.work), (int)groups, a.D, a.side[0].dweight, a.side[1].dweight);
-        return hipGetLastError();
+        return with_group<e()>(a, [&](auto lanes) {
+            const HeadGroups g = head_groups(a, lanes() ? lanes() : 64, kBackwardGroups);
+            const dim3 grid(g.all()), block(kThreads);
+            if constexpr (lanes() == 0) {
+                SW_NOTED_LAUNCH(note_kernel("head_norm_any_backward_kernel", ek), (head_norm_any_kernel<e(), true>), grid, block, 0, st, a, g);
+            } else {
+                note_kernel("head_norm_backward_kernel", ek, lanes(), a.interleaved);
+                if (a.interleaved)
+                    hipLaunchKernelGGL((head_norm_kernel<e(), lanes(), true, true>), grid, block, 0, st, a, g);
+                else
+                    hipLaunchKernelGGL((head_norm_kernel<e(), lanes(), false, true>), grid, block, 0, st, a, g);
+            }
+            if (const hipError_t err = hipGetLastError()) return err;
+            if (!a.work) return hipSuccess;
+            const float* partial = static_cast<const float*>(a.work);
+            return launch_fold(FoldArgs{{{partial, g.groups[0], a.side[0].dweight}, {partial + (int64_t)g.groups[0] * a.D, g.groups[1], a.side[1].dweight}}, a.D}, st);
+        });
     });
 }
 

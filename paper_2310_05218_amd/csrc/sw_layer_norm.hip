@@ -19,31 +19,6 @@ namespace {
 
 // ---- sums over lanes ----------------------------------------------------------------------------------------------------------
 
-template <int CTRL>
-__device__ __forceinline__ float dpp_move(float v)
-{
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-
-// The sum over groups of LANES neighbouring lanes (8 to 64), in every lane.
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v)
-{
-    v += dpp_move<0xB1>(v);                          // the neighbour
-    v += dpp_move<0x4E>(v);                          // the other pair of four
-    v += dpp_move<0x141>(v);                         // the other four of eight
-    if constexpr (LANES >= 16) v += dpp_move<0x140>(v);
-    if constexpr (LANES >= 32) {
-        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-    if constexpr (LANES >= 64) {
-        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
-    }
-    return v;
-}
-
 // The sums over all LANES threads of a row, in every one of them.  `lds` holds a value for each wavefront and sum, and is written again
 // two calls later: one barrier a call, as a thread that is a call ahead of another has passed the barrier that the other's reads precede.
 template <int LANES, int N>

@@ -109,6 +109,33 @@ struct Row {
     }
 };
 
+// ---- sums over lanes ----------------------------------------------------------------------------------------------------------
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_move(float v)
+{
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+
+// The sum over groups of LANES neighbouring lanes (4 to 64), in every lane.
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v)
+{
+    v += dpp_move<0xB1>(v);                          // the neighbour
+    v += dpp_move<0x4E>(v);                          // the other pair of four
+    if constexpr (LANES >= 8) v += dpp_move<0x141>(v);       // the other four of eight
+    if constexpr (LANES >= 16) v += dpp_move<0x140>(v);
+    if constexpr (LANES >= 32) {
+        const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    if constexpr (LANES >= 64) {
+        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+
 // ---- layer norm ------------------------------------------------------------------------------------------------------------
 struct LayerNormArgs {
     const void* x;

@@ -376,7 +376,7 @@ hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, h
         });
         if (const hipError_t err = hipGetLastError()) return err;
         if (!a.d_log_decay) return hipSuccess;
-        return launch_fold(FoldArgs{partial, (int)(tiles.segments * tiles.batches), a.n.C, {a.d_log_decay, nullptr}, a.n.C}, st);
+        return launch_fold(FoldArgs{{{partial, (int)(tiles.segments * tiles.batches), a.d_log_decay}, {nullptr, 0, nullptr}}, a.n.C}, st);
     });
 }
 

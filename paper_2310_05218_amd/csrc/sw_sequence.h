@@ -8,10 +8,12 @@ namespace swconv {
 
 // ---- sums of rows of fp32 values, in a fixed order ---------------------------------------------------------------------------------
 struct FoldArgs {
-    const float* partial;               // [parts, width]
-    int parts, width;
-    float* out[2];                      // the sums of the first `split` columns and of the others; null: not wanted
-    int split;
+    struct {
+        const float* partial;           // [parts, width]
+        int parts;
+        float* out;                     // [width]; null: not wanted
+    } of[2];
+    int width;
 };
 hipError_t launch_fold(const FoldArgs& a, hipStream_t st);
 
@@ -70,7 +72,7 @@ struct HeadNormArgs {
     float eps;
     void* work;
 };
-int64_t    head_norm_backward_workspace(int64_t rows, int heads, int kv_heads, int D);
+int64_t    head_norm_backward_workspace(const HeadNormArgs& a);     // of any format
 hipError_t launch_head_norm(const HeadNormArgs& a, int ek, hipStream_t st);
 hipError_t launch_head_norm_backward(const HeadNormArgs& a, int ek, hipStream_t st);
 

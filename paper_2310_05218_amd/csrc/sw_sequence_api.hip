@@ -232,7 +232,9 @@ int sw_head_norm(const void* q, const void* k, const float* q_weight, const floa
 int64_t sw_head_norm_backward_workspace_bytes(const sw_head_norm_dims* dims)
 {
     if (!dims || check_heads(*dims) != SW_OK) return 0;
-    return align16(head_norm_backward_workspace(dims->B * dims->T, dims->heads, dims->kv_heads, dims->d));
+    HeadNormArgs a{};
+    a.B = dims->B, a.T = dims->T, a.D = dims->d, a.pairs = dims->pairs, a.side[0].heads = dims->heads, a.side[1].heads = dims->kv_heads;
+    return align16(head_norm_backward_workspace(a));
 }
 
 int sw_head_norm_backward(const void* dq, const void* dk, const void* q, const void* k, const float* q_weight, const float* k_weight,

@@ -72,7 +72,7 @@ def run(sw, made, eps=1e-6, interleaved=False):
 # d, pairs
 WIDTHS = [(1, 0), (2, 1), (3, 1), (4, 2), (6, 3), (8, 4), (8, 2), (10, 5), (16, 8), (20, 10), (24, 12), (31, 15), (32, 16), (32, 8), (34, 17), (48, 24), (64, 32),
           (64, 16), (64, 0), (66, 33), (72, 36), (80, 20), (80, 40), (96, 48), (96, 24), (100, 50), (112, 56), (126, 63), (127, 63), (128, 64), (128, 32),
-          (128, 1), (130, 65), (144, 72), (160, 80), (192, 96), (200, 50), (222, 111), (240, 120), (250, 62), (255, 127), (256, 128), (256, 64), (256, 7)]
+          (128, 1), (130, 65), (144, 72), (160, 80), (192, 96), (200, 50), (222, 111), (240, 120), (250, 62), (255, 127), (256, 128), (256, 64), (256, 7), (256, 12), (254, 11)]
 
 
 @pytest.mark.parametrize("t", TYPES)
