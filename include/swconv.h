@@ -600,7 +600,7 @@ int64_t sw_head_norm_backward_workspace_bytes(const sw_head_norm_dims* dims);
  * (ones); slots: [B] int32 (device) or NULL: sequence b has adapter b (n >= B then, else SW_ERR_SHAPE).  Several sequences may have one
  * adapter.  Rows of a sequence whose entry is outside 0 ... n-1, and rows in no sequence, are copied.  Products are added in fp32, a[s] x is
  * kept in fp32, and the result is rounded once.  out may be y (same pointer and stride); any other overlap is SW_ERR_ALIAS.
- * 1 <= rank <= 256, C_in, C_out <= 2^20 (SW_ERR_UNSUPPORTED beyond); all rows below 2^31.
+ * 1 <= rank <= 256, C_in, C_out <= 2^20 (SW_ERR_UNSUPPORTED beyond); rows as far as a launch has threads (2^20 at any size, SW_ERR_SHAPE beyond that).
  */
 typedef struct {
     int64_t T;

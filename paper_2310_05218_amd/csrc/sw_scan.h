@@ -206,11 +206,6 @@ struct PackedRows {
     unsigned begins, ends, outside;     // the first and last rows of sequences; rows in no sequence
     int sequence, entry;                // of the lane's row; entry -1: none
 };
-// (Addresses are the wavefront's: scalar loads, which wait for none of the rows on their way.)
-__device__ __forceinline__ int uniform_load(const int32_t* p)
-{
-    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
-}
 template <int R>
 __device__ __forceinline__ PackedRows packed_rows(const RecurrenceBatch& n, int64_t first)
 {

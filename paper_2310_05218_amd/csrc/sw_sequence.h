@@ -6,6 +6,13 @@
 
 namespace swconv {
 
+// A value at an address that is the same for a whole wavefront, of memory that the kernel does not write: a scalar load, which waits for none of the vector
+// loads on their way.
+__device__ __forceinline__ int uniform_load(const int32_t* p)
+{
+    return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p));
+}
+
 // ---- sums of rows of fp32 values, in a fixed order ---------------------------------------------------------------------------------
 struct FoldArgs {
     struct {
@@ -86,6 +93,7 @@ struct AdapterArgs {
     int B, C_in, C_out, rank, n;
     void* work;
 };
+bool       adapters_fit(const AdapterArgs& a);         // launches have threads for all rows
 int64_t    adapters_workspace(const AdapterArgs& a, int ek);
 hipError_t launch_adapters(const AdapterArgs& a, int ek, hipStream_t st);
 

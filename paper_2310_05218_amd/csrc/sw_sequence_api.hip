@@ -68,6 +68,13 @@ int check_heads(const sw_head_norm_dims& d)
     return SW_OK;
 }
 
+const int32_t* const kPacked = reinterpret_cast<const int32_t*>(16);    // an address that only says that starts is given
+AdapterArgs adapter_args(const sw_adapters_dims& d, const int32_t* starts)
+{
+    AdapterArgs a{};
+    a.starts = starts, a.T = d.T, a.B = d.B, a.C_in = d.C_in, a.C_out = d.C_out, a.rank = d.rank, a.n = d.n;
+    return a;
+}
 int check_adapters(const sw_adapters_dims& d, bool packed)
 {
     if (d.T <= 0 || d.B <= 0 || d.C_in <= 0 || d.C_out <= 0 || d.rank <= 0 || d.n <= 0 || (int64_t)d.B + 2 > 0x7fffffff ||
@@ -75,15 +82,8 @@ int check_adapters(const sw_adapters_dims& d, bool packed)
         return SW_ERR_SHAPE;
     if (d.rank > 256 || d.C_in > kMaxChannels || d.C_out > kMaxChannels || !known(d.type)) return SW_ERR_UNSUPPORTED;
     if ((int64_t)d.n > kMaxExtent / ((int64_t)d.rank * (d.C_in > d.C_out ? d.C_in : d.C_out))) return SW_ERR_SHAPE;
-    return SW_OK;
+    return adapters_fit(adapter_args(d, packed ? kPacked : nullptr)) ? SW_OK : SW_ERR_SHAPE;
 }
-AdapterArgs adapter_args(const sw_adapters_dims& d, const int32_t* starts)
-{
-    AdapterArgs a{};
-    a.starts = starts, a.T = d.T, a.B = d.B, a.C_in = d.C_in, a.C_out = d.C_out, a.rank = d.rank, a.n = d.n;
-    return a;
-}
-const int32_t* const kPacked = reinterpret_cast<const int32_t*>(16);    // an address that only says that starts is given
 
 }  // namespace
 
