@@ -1,8 +1,8 @@
 // Low-rank adapters beside a shared projection: low = a x for every row, then out = y + scale b low.
 //
 // Long sequences go in tiles of 32 rows on the matrix cores, single tokens a row at a time.  Both factors and x are matrix operands as they lie: 16
-// consecutive bytes of a row are a lane's.  A tile that several sequences meet in does the product for each of their adapters and keeps
-// the rows that are its own, so that tiles need no list of sequences.
+// consecutive bytes of a row are a lane's.  A tile's rows are one sequence's: packed sequences have places for their tiles that a workgroup finds without a list,
+// sequence j's from start / 32 + j on, which leaves each at least as many as it needs.
 //
 // `low` is a sum of fp32 products and enters a product itself.  Of 16-bit tensors it goes on as three 16-bit parts, v = v1 + v2 + v3, each the rest of the ones
 // before rounded: 24 bits in bf16, and in half, of the row's largest value scaled to 2^13 ... 2^14, all bits above 2^-24 of that.  Three instructions in place of
@@ -17,35 +17,63 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // ---- the rows' adapters ------------------------------------------------------------------------------------------------------------------------
 
-// From `row` to `end` (at most `limit`) rows have adapter `s`; -1: none.  (Uniform: by whole wavefronts.)
-struct Part {
-    int64_t end;
-    int s;
-};
-__device__ __forceinline__ Part part_from(const AdapterArgs& p, int64_t row, int64_t limit)
+// How many of count (>= 0) ascending values are at or before v: 64 of them looked at together, by a whole wavefront.
+template <class F>
+__device__ __forceinline__ int at_or_before(int count, int64_t v, F&& value)
 {
-    int64_t b, end;
-    if (p.starts) {
-        int lo = 0, hi = p.B + 1;       // how many of the B + 1 starts are at or before the row; the next one, where there is one, is past it
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            if (uniform_load(p.starts + mid) <= row) lo = mid + 1;
-            else hi = mid;
-        }
-        b = lo - 1;
-        end = lo <= p.B ? uniform_load(p.starts + lo) : limit;
-        if (b < 0 || b >= p.B) return Part{end < limit ? end : limit, -1};
-    } else {
-        b = row / p.T;
-        end = (b + 1) * p.T;
+    const int lane = threadIdx.x % 64;
+    int base = 0;
+    while (count > 64) {
+        const int step = (count + 63) / 64, at = lane * step;
+        const int found = __popcll(__ballot(at < count && value(base + (at < count ? at : 0)) <= v));
+        const int skip = found > 0 ? (found - 1) * step : 0;
+        base += skip;
+        count = count - skip < step ? count - skip : step;
     }
-    const int s = p.slots ? uniform_load(p.slots + b) : (int)b;
-    return Part{end < limit ? end : limit, s >= 0 && s < p.n ? s : -1};
+    return base + __popcll(__ballot(lane < count && value(base + (lane < count ? lane : 0)) <= v));
 }
 
-// ---- tiles of rows ----------------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ int adapter_of(const AdapterArgs& p, int64_t sequence)
+{
+    const int s = p.slots ? uniform_load(p.slots + sequence) : (int)sequence;
+    return s >= 0 && s < p.n ? s : -1;
+}
+
+// The adapter of a row; -1: none.
+__device__ __forceinline__ int adapter_of_row(const AdapterArgs& p, int64_t row)
+{
+    if (!p.starts) return adapter_of(p, row / p.T);
+    const int b = at_or_before(p.B + 1, row, [&](int k) { return (int64_t)p.starts[k]; }) - 1;
+    return b < 0 || b >= p.B ? -1 : adapter_of(p, b);
+}
 
 constexpr int kTileRows = 32;
+
+// A tile's rows (none: 0) and their adapter (-1: none).
+struct Tile {
+    int64_t first;
+    int rows, s;
+};
+__device__ __forceinline__ Tile tile_at(const AdapterArgs& p, int64_t place)
+{
+    if (!p.starts) {
+        const int64_t each = (p.T + kTileRows - 1) / kTileRows, b = place / each, at = place % each * kTileRows;
+        return Tile{b * p.T + at, p.T - at < kTileRows ? (int)(p.T - at) : kTileRows, adapter_of(p, b)};
+    }
+    // (j = 0 and B + 1: the rows before the first and after the last sequence)
+    auto first = [&](int j) {
+        const int64_t v = j == 0 ? 0 : p.starts[j - 1];
+        return v < 0 ? 0 : v > p.T ? p.T : v;
+    };
+    const int found = at_or_before(p.B + 2, place, [&](int j) { return first(j) / kTileRows + j; }), j = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
+    const int64_t begin = first(j), end = j == p.B + 1 ? p.T : first(j + 1), at = begin + (place - (begin / kTileRows + j)) * kTileRows, left = end - at;
+    Tile t{at, left <= 0 || at < 0 ? 0 : left < kTileRows ? (int)left : kTileRows, -1};
+    if (t.rows && j > 0 && j <= p.B) t.s = adapter_of(p, j - 1);
+    return t;
+}
+int64_t tile_places(const AdapterArgs& a) { return a.starts ? a.T / kTileRows + a.B + 3 : a.B * ((a.T + kTileRows - 1) / kTileRows); }
+
+// ---- tiles of rows ----------------------------------------------------------------------------------------------------------------------------
 
 template <int EK>
 struct Matrix {
@@ -70,201 +98,229 @@ struct Matrix {
 // The rank as the second product has it.
 constexpr int padded_rank(int rank, int ek) { return ek == kElemF32 ? (rank + 15) / 16 * 16 : (rank + 31) / 32 * 32; }
 
-// low of a tile's rows for up to 16 NT ranks, the input channels shared out to W wavefronts.  work: [rows][PARTS][padded rank], then a factor for each row.
+// { low [rows][PARTS][K], a factor for each row }
+template <int EK>
+struct Low {
+    typename Matrix<EK>::T* low;
+    float* factor;
+    __host__ __device__ Low(void* work, int64_t rows, int K)
+        : low(static_cast<typename Matrix<EK>::T*>(work)), factor(reinterpret_cast<float*>(low + rows * Matrix<EK>::PARTS * K))
+    {
+    }
+};
+
+// low of a tile's rows for up to 16 NT ranks, the input channels shared out to W wavefronts, U steps of them on their way together.
 template <int EK, int NT, int W>
 __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int64_t rows, int K)
 {
     typedef Matrix<EK> M;
     typedef typename M::R R;
     typedef typename M::T T;
-    constexpr int PITCH = 16 * NT + 1;
+    constexpr int PITCH = 16 * NT + 1, U = NT <= 4 ? 4 : NT == 8 ? 2 : 1;
     extern __shared__ float sums[];                     // [W][32][PITCH]
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
-    const int64_t first = (int64_t)blockIdx.x * kTileRows, last = first + kTileRows < rows ? first + kTileRows : rows;
-    float* const factor = reinterpret_cast<float*>(static_cast<T*>(p.work) + rows * M::PARTS * K);
-    const T* x[2];
+    const Tile tile = tile_at(p, blockIdx.x);
+    if (tile.rows == 0 || tile.s < 0) return;
+    const T *x[2], *rank_row[NT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t row = first + 16 * t + m;
-        x[t] = static_cast<const T*>(p.x) + (row < rows ? row : rows - 1) * p.x_stride;
+    for (int t = 0; t < 2; ++t) x[t] = static_cast<const T*>(p.x) + (tile.first + (16 * t + m < tile.rows ? 16 * t + m : 0)) * p.x_stride + q * R::VEC;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        rank_row[n] = static_cast<const T*>(p.a) + ((int64_t)tile.s * p.rank + (16 * n + m < p.rank ? 16 * n + m : p.rank - 1)) * p.C_in + q * R::VEC;
+    f32x4 acc[2][NT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[t][n] = 0.f;
+    auto add = [&](const typename R::vec(&xv)[2], const typename R::vec(&av)[NT]) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) acc[t][n] = M::multiply(xv[t], av[n], acc[t][n]);
+    };
+    // A wavefront's run of whole steps, from a place on that differs between tiles: rows are often a power of two apart, and what is read of 16 rows at
+    // once is in one memory channel.
+    const int whole = p.C_in / M::STEP, begin = (int)((int64_t)whole * wave / W), steps = (int)((int64_t)whole * (wave + 1) / W) - begin;
+    int step = steps ? (int)(blockIdx.x % steps) : 0, done = 0;
+    for (; done + U <= steps; done += U) {
+        typename R::vec xv[U][2], av[U][NT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int at = (begin + step) * M::STEP;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) xv[u][t] = R::load(x[t] + at);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) av[u][n] = R::load(rank_row[n] + at);
+            step = step + 1 < steps ? step + 1 : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(xv[u], av[u]);
     }
-    for (int64_t row = first; row < last;) {
-        const Part part = part_from(p, row, last);
-        if (part.s >= 0) {
-            const T* const a = static_cast<const T*>(p.a) + (int64_t)part.s * p.rank * p.C_in;
-            const T* rank_row[NT];
+    for (; done < steps; ++done) {
+        typename R::vec xv[2], av[NT];
+        const int at = (begin + step) * M::STEP;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) rank_row[n] = a + (int64_t)(16 * n + m < p.rank ? 16 * n + m : p.rank - 1) * p.C_in;
-            f32x4 acc[2][NT];
+        for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t] + at);
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n] + at);
+        step = step + 1 < steps ? step + 1 : 0;
+        add(xv, av);
+    }
+    if (wave == W - 1 && whole * M::STEP < p.C_in) {
+        typename R::vec xv[2], av[NT];
+        const int at = whole * M::STEP, left = p.C_in - q * R::VEC;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[t][n] = 0.f;
-            for (int c = wave * M::STEP; c < p.C_in; c += W * M::STEP) {
-                const int at = c + q * R::VEC;
-                typename R::vec xv[2], av[NT];
-                if (c + M::STEP <= p.C_in) {
+        for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t], at, left);
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t] + at);
+        for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n], at, left);
+        add(xv, av);
+    }
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n] + at);
-                } else {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t], at, p.C_in);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n], at, p.C_in);
-                }
+            for (int i = 0; i < 4; ++i) sums[(wave * kTileRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
+    __syncthreads();
+    // 16 lanes a row
+    const Low<EK> to(p.work, rows, K);
+    const float factor = p.scales ? p.scales[tile.s] : 1.f;
+    for (int r = threadIdx.x / 16; r < tile.rows; r += 4 * W) {
+        float v[NT], scale = 1.f;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            v[n] = 0.f;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t) acc[t][n] = M::multiply(xv[t], av[n], acc[t][n]);
-            }
-            __syncthreads();            // (the sums of the part before have been read)
+            for (int w = 0; w < W; ++w) v[n] += sums[(w * kTileRows + r) * PITCH + 16 * n + m];
+            if (16 * n + m >= p.rank) v[n] = 0.f;
+        }
+        if constexpr (EK == kElemF16) {
+            float most = 0.f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int n = 0; n < NT; ++n) most = fmaxf(most, fabsf(v[n]));
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+            for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 16));
+            // 2^e with 2^13 <= most 2^-e < 2^14; rows of zeros, and of what is not finite, as they are
+            int e = most > 0.f && most < 3.4e38f ? __builtin_amdgcn_frexp_expf(most) - 14 : 0;
+            e = e < -100 ? -100 : e;
+            scale = __builtin_amdgcn_ldexpf(1.f, e);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sums[(wave * kTileRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
-            __syncthreads();
-            // 16 lanes a row
-            for (int r = threadIdx.x / 16; r < kTileRows; r += 4 * W) {
-                const int64_t to = first + r;
-                if (to < row || to >= part.end) continue;
-                float v[NT], scale = 1.f;
+            for (int n = 0; n < NT; ++n) v[n] *= __builtin_amdgcn_ldexpf(1.f, -e);
+        }
+        T* const low = to.low + (tile.first + r) * M::PARTS * K;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    v[n] = 0.f;
+        for (int n = 0; n < NT; ++n) {
+            if (16 * n + m >= K) continue;
+            float rest = v[n];
 #pragma unroll
-                    for (int w = 0; w < W; ++w) v[n] += sums[(w * kTileRows + r) * PITCH + 16 * n + m];
-                    if (16 * n + m >= p.rank) v[n] = 0.f;
-                }
-                if constexpr (EK == kElemF16) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) most = fmaxf(most, fabsf(v[n]));
-#pragma unroll
-                    for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 16));
-                    // 2^e with 2^13 <= most 2^-e < 2^14; rows of zeros, and of what is not finite, as they are
-                    const int e = most > 0.f && most < 3.4e38f ? __builtin_amdgcn_frexp_expf(most) - 14 : 0;
-                    scale = __builtin_amdgcn_ldexpf(1.f, e < -100 ? -100 : e);
-                    const float back = __builtin_amdgcn_ldexpf(1.f, e < -100 ? 100 : -e);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) v[n] *= back;
-                }
-                T* const low = static_cast<T*>(p.work) + to * M::PARTS * K;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if (16 * n + m >= K) continue;
-                    float rest = v[n];
-#pragma unroll
-                    for (int k = 0; k < M::PARTS; ++k) {
-                        const T one = (T)rest;
-                        low[k * K + 16 * n + m] = one;
-                        rest -= (float)one;
-                    }
-                }
-                for (int n = 16 * NT + m; n < K; n += 16)
-#pragma unroll
-                    for (int k = 0; k < M::PARTS; ++k) low[k * K + n] = (T)0.f;
-                if (m == 0) factor[to] = scale * (p.scales ? p.scales[part.s] : 1.f);
+            for (int k = 0; k < M::PARTS; ++k) {
+                const T one = (T)rest;
+                low[k * K + 16 * n + m] = one;
+                rest -= (float)one;
             }
         }
-        row = part.end;
+        for (int n = 16 * NT + m; n < K; n += 16)
+#pragma unroll
+            for (int k = 0; k < M::PARTS; ++k) low[k * K + n] = (T)0.f;
+        if (m == 0) to.factor[tile.first + r] = scale * factor;
     }
 }
 
-// out of a tile's rows and a run of output channels, 64 of them a wavefront at a time.  Output channels are the matrix's rows, in an order that gives a lane 16
-// consecutive ones of a row of y.
-constexpr int kOutWaves = 4;
-template <int EK>
+// out of a tile's rows and a run of output channels, 64 of them a wavefront at a time; S steps of the rank are on their way together.  Output channels are the
+// matrix's rows; what comes of the product goes through LDS, so that y is read and out written in whole 128-byte lines.
+constexpr int kOutWaves = 4, kOutPitch = 68;
+template <int EK, int S>
 __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int chunks, int chunk)
 {
     typedef Matrix<EK> M;
     typedef typename M::R R;
     typedef typename M::T T;
-    constexpr int VEC = R::VEC, PARTS = M::PARTS;
+    typedef typename R::vec vec;
+    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES;      // lanes a row of 64 channels, rows at a time
+    __shared__ float turned[kOutWaves][kTileRows][kOutPitch];
     extern __shared__ float shared[];
     T* const low = reinterpret_cast<T*>(shared);        // [PARTS][32][K + VEC]
     const int pitch = K + VEC;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
-    // (workgroups that follow each other have different chunks: with eight of them the workgroups of a die have one, and its caches that part of b)
-    const int64_t first = blockIdx.x / chunks * (int64_t)kTileRows, last = first + kTileRows < rows ? first + kTileRows : rows;
+    // (workgroups that follow each other have different chunks: where there are as many as dies, or half, a die's workgroups have one, and its caches that part of b)
+    const Tile tile = tile_at(p, blockIdx.x / chunks);
+    if (tile.rows == 0 || (tile.s < 0 && p.out == p.y)) return;
     const int from = (int)(blockIdx.x % chunks) * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
-    const float* const factor = reinterpret_cast<const float*>(static_cast<const T*>(p.work) + rows * PARTS * K);
-    for (int k = threadIdx.x; k < kTileRows * PARTS * (K / VEC); k += 64 * kOutWaves) {
-        const int r = k / (PARTS * (K / VEC)), rest = k % (PARTS * (K / VEC)), part = rest / (K / VEC), c = rest % (K / VEC) * VEC;
-        const int64_t row = first + r < rows ? first + r : rows - 1;
-        *reinterpret_cast<typename R::vec*>(low + (part * kTileRows + r) * pitch + c) =
-            *reinterpret_cast<const typename R::vec*>(static_cast<const T*>(p.work) + (row * PARTS + part) * K + c);
+    const T* const y = static_cast<const T*>(p.y) + tile.first * p.y_stride;
+    T* const out = static_cast<T*>(p.out) + tile.first * p.out_stride;
+    const int row = lane / LANES, column = lane % LANES * VEC;          // of a run of rows
+    if (tile.s < 0) {
+        for (int r = wave * RUN + row; r < tile.rows; r += kOutWaves * RUN)
+            for (int c = from + column; c < to; c += 64)
+                R::store(out + r * p.out_stride, c, to, __builtin_convertvector(R::load(y + r * p.y_stride, c, to), typename R::floats));
+        return;
+    }
+    const Low<EK> source(p.work, rows, K);
+    float f[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) f[t] = source.factor[tile.first + (16 * t + m < tile.rows ? 16 * t + m : 0)];
+    {
+        const int run = K / VEC, all = kTileRows * PARTS * run;
+        for (int k = threadIdx.x; k < all; k += 64 * kOutWaves) {
+            const int r = k / (PARTS * run), part = k / run % PARTS, c = k % run * VEC;
+            *reinterpret_cast<vec*>(low + (part * kTileRows + r) * pitch + c) =
+                *reinterpret_cast<const vec*>(source.low + ((tile.first + (r < tile.rows ? r : 0)) * PARTS + part) * K + c);
+        }
     }
     __syncthreads();
-    for (int64_t row = first; row < last;) {
-        const Part part = part_from(p, row, last);
-        if (part.s >= 0) {
-            const T* const b = static_cast<const T*>(p.b) + (int64_t)part.s * p.C_out * p.rank;
-            bool mine[2];
-            float f[2];
-            const T* y[2];
-            T* out[2];
+    const T* const b = static_cast<const T*>(p.b) + (int64_t)tile.s * p.C_out * p.rank;
+    const int blocks = (to - from + 63) / 64, turn = (int)(blockIdx.x / chunks % blocks);
+    for (int k = wave; k < blocks; k += kOutWaves) {
+        const int c0 = from + 64 * (k + turn < blocks ? k + turn : k + turn - blocks);
+        vec yv[kTileRows / RUN];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const int64_t at = first + 16 * t + m;
-                mine[t] = at >= row && at < part.end;
-                const int64_t safe = mine[t] ? at : row;
-                f[t] = factor[safe];
-                y[t] = static_cast<const T*>(p.y) + safe * p.y_stride;
-                out[t] = static_cast<T*>(p.out) + safe * p.out_stride;
-            }
-            for (int c0 = from + 64 * wave; c0 < to; c0 += 64 * kOutWaves) {
-                const int at = c0 + 16 * q;             // the lane's 16 channels of y
-                typename R::vec yv[2][16 / VEC];
+        for (int i = 0; i < kTileRows / RUN; ++i) yv[i] = R::load(y + (i * RUN + row < tile.rows ? i * RUN + row : 0) * p.y_stride, c0 + column, to);
+        const T* rows_of_b[4];
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+        for (int j = 0; j < 4; ++j) rows_of_b[j] = b + (int64_t)(c0 + 16 * j + m < to ? c0 + 16 * j + m : to - 1) * p.rank;
+        f32x4 acc[4][2];
 #pragma unroll
-                    for (int k = 0; k < 16 / VEC; ++k) yv[t][k] = R::load(y[t], at + k * VEC, to);
-                const T* rows_of_b[4];
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) acc[j][t] = 0.f;
+        for (int k0 = 0; k0 < K; k0 += S * M::STEP) {
+            vec bv[S][4];
+#pragma unroll
+            for (int u = 0; u < S; ++u)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int c = c0 + (m / 4) * 16 + j * 4 + m % 4;
-                    rows_of_b[j] = b + (int64_t)(c < to ? c : to - 1) * p.rank;
+                    const int at = k0 + u * M::STEP;
+                    bv[u][j] = at + M::STEP <= p.rank ? R::load(rows_of_b[j] + at + q * VEC) : R::load(rows_of_b[j], at + q * VEC, p.rank);
                 }
-                f32x4 acc[4][2];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) acc[j][t] = 0.f;
-                for (int k = 0; k < K; k += M::STEP) {
-                    typename R::vec bv[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) bv[j] = k + M::STEP <= p.rank ? R::load(rows_of_b[j] + k + q * VEC) : R::load(rows_of_b[j], k + q * VEC, p.rank);
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int n = 0; n < PARTS; ++n) {
-                            const typename R::vec v = *reinterpret_cast<const typename R::vec*>(low + (n * kTileRows + 16 * t + m) * pitch + k + q * VEC);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) acc[j][t] = M::multiply(bv[j], v, acc[j][t]);
-                        }
-                }
+            for (int u = 0; u < S; ++u)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
-                    if (mine[t])
 #pragma unroll
-                        for (int k = 0; k < 16 / VEC; ++k) {
-                            typename R::floats v = __builtin_convertvector(yv[t][k], typename R::floats);
+                    for (int n = 0; n < PARTS; ++n) {
+                        const vec v = *reinterpret_cast<const vec*>(low + (n * kTileRows + 16 * t + m) * pitch + k0 + u * M::STEP + q * VEC);
 #pragma unroll
-                            for (int e = 0; e < VEC; ++e) v[e] = __builtin_fmaf(f[t], acc[(k * VEC + e) / 4][t][e % 4], v[e]);
-                            R::store(out[t], at + k * VEC, to, v);
-                        }
-            }
-        } else if (p.out != p.y) {
-            for (int64_t r = row + wave; r < part.end; r += kOutWaves)
-                for (int c = from + lane * VEC; c < to; c += 64 * VEC)
-                    R::store(static_cast<T*>(p.out) + r * p.out_stride, c, to,
-                             __builtin_convertvector(R::load(static_cast<const T*>(p.y) + r * p.y_stride, c, to), typename R::floats));
+                        for (int j = 0; j < 4; ++j) acc[j][t] = M::multiply(bv[u][j], v, acc[j][t]);
+                    }
         }
-        row = part.end;
+        // (a wavefront's own part of LDS: its instructions go there in their order)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4*>(&turned[wave][16 * t + m][16 * j + 4 * q]) = acc[j][t] * f[t];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < kTileRows / RUN; ++i) {
+            typename R::floats v = __builtin_convertvector(yv[i], typename R::floats);
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+                const f32x4 more = *reinterpret_cast<const f32x4*>(&turned[wave][i * RUN + row][column + e]);
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4) v[e + k4] += more[k4];
+            }
+            if (i * RUN + row < tile.rows) R::store(out + (i * RUN + row) * p.out_stride, c0 + column, to, v);
+        }
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -304,7 +360,7 @@ __global__ __launch_bounds__(kRowThreads) void adapters_row_low_kernel(AdapterAr
     const int64_t task = (int64_t)blockIdx.x * (kRowThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = task / each;
     const int k = (int)(task % each) * kRowRanks;
     if (row >= rows) return;
-    const int s = part_from(p, row, row + 1).s;
+    const int s = adapter_of_row(p, row);
     if (s < 0) return;
     float sum[kRowRanks];
     dots<EK, kRowRanks>(p, row, s, k, sum);
@@ -323,7 +379,7 @@ __global__ __launch_bounds__(kRowThreads) void adapters_row_out_kernel(AdapterAr
     __shared__ float low[256];
     const int64_t row = blockIdx.x / chunks;
     const int from = (int)(blockIdx.x % chunks) * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
-    const int s = part_from(p, row, row + 1).s;
+    const int s = adapter_of_row(p, row);
     const T* const y = static_cast<const T*>(p.y) + row * p.y_stride;
     T* const out = static_cast<T*>(p.out) + row * p.out_stride;
     if (s < 0) {
@@ -362,12 +418,14 @@ __global__ __launch_bounds__(kRowThreads) void adapters_row_out_kernel(AdapterAr
 
 int64_t rows_of(const AdapterArgs& a) { return a.starts ? a.T : a.T * a.B; }
 
-// Tiles where a sequence has eight rows on average: a tile that many short ones meet in does its product once for each.
+// Tiles where a sequence has eight rows on average: a tile of few rows costs what a full one does.
 bool in_tiles(const AdapterArgs& a) { return rows_of(a) >= 8 * (int64_t)a.B; }
 
 // Single rows in one launch where a factor `a` is small enough for every workgroup of a row to read it.
 constexpr int64_t kWholeBytes = 128 << 10;
 bool whole_rows(const AdapterArgs& a, int ek) { return (int64_t)a.rank * a.C_in * elem_size(ek) <= kWholeBytes; }
+
+constexpr int kChunks = 4;              // workgroups for a tile's output channels
 
 template <int EK, int NT, int W>
 hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, hipStream_t st)
@@ -375,7 +433,7 @@ hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, hipStream_t st)
     const size_t lds = sizeof(float) * W * kTileRows * (16 * NT + 1);
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_low_kernel<EK, NT, W>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (allowed != hipSuccess) return allowed;
-    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3((unsigned)((rows + kTileRows - 1) / kTileRows)), dim3(64 * W), lds, st, a, rows, K);
+    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3((unsigned)tile_places(a)), dim3(64 * W), lds, st, a, rows, K);
     return hipGetLastError();
 }
 
@@ -391,10 +449,17 @@ hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
     else if (a.rank <= 128) err = launch_low<EK, 8, 8>(a, rows, K, st);
     else err = launch_low<EK, 16, 4>(a, rows, K, st);
     if (err != hipSuccess) return err;
-    const int blocks = (a.C_out + 63) / 64, most = blocks < 8 ? blocks : 8, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
+    const int blocks = (a.C_out + 63) / 64, most = blocks < kChunks ? blocks : kChunks, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
     const size_t lds = (size_t)kTileRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
-    const int64_t groups = (rows + kTileRows - 1) / kTileRows * chunks;
-    SW_NOTED_LAUNCH(note_kernel("adapters_out_kernel", EK, a.rank), adapters_out_kernel<EK>, dim3((unsigned)groups), dim3(64 * kOutWaves), lds, st, a, rows, K, chunks, chunk);
+    const dim3 grid((unsigned)(tile_places(a) * chunks)), block(64 * kOutWaves);
+    const int steps = K / Matrix<EK>::STEP;
+    note_kernel("adapters_out_kernel", EK, a.rank);
+    if (steps % 4 == 0)
+        hipLaunchKernelGGL((adapters_out_kernel<EK, 4>), grid, block, lds, st, a, rows, K, chunks, chunk);
+    else if (steps % 2 == 0)
+        hipLaunchKernelGGL((adapters_out_kernel<EK, 2>), grid, block, lds, st, a, rows, K, chunks, chunk);
+    else
+        hipLaunchKernelGGL((adapters_out_kernel<EK, 1>), grid, block, lds, st, a, rows, K, chunks, chunk);
     return hipGetLastError();
 }
 
@@ -428,7 +493,7 @@ constexpr int64_t kThreadsMost = ((int64_t)1 << 32) - 1;
 bool adapters_fit(const AdapterArgs& a)
 {
     const int64_t rows = rows_of(a);
-    if (in_tiles(a)) return (rows + kTileRows - 1) / kTileRows <= kThreadsMost / (8 * 64 * kOutWaves);
+    if (in_tiles(a)) return tile_places(a) <= kThreadsMost / (kChunks * 64 * kOutWaves);
     return rows <= kThreadsMost / kRowThreads / 2 && rows <= kThreadsMost / (64 * ((a.rank + kRowRanks - 1) / kRowRanks)) - kRowThreads;
 }
 
