@@ -58,6 +58,7 @@ __device__ __forceinline__ Tile tile_at(const AdapterArgs& p, int64_t place)
 {
     if (!p.starts) {
         const int64_t each = (p.T + kTileRows - 1) / kTileRows, b = place / each, at = place % each * kTileRows;
+        if (b >= p.B) return Tile{0, 0, -1};
         return Tile{b * p.T + at, p.T - at < kTileRows ? (int)(p.T - at) : kTileRows, adapter_of(p, b)};
     }
     // (j = 0 and B + 1: the rows before the first and after the last sequence)
@@ -70,6 +71,17 @@ __device__ __forceinline__ Tile tile_at(const AdapterArgs& p, int64_t place)
     Tile t{at, left <= 0 || at < 0 ? 0 : left < kTileRows ? (int)left : kTileRows, -1};
     if (t.rows && j > 0 && j <= p.B) t.s = adapter_of(p, j - 1);
     return t;
+}
+// Workgroups follow each other over the 8 dies: each die has a run of neighbouring places, so that the tiles of a sequence find its adapter in one die's caches.
+constexpr int kDies = 8;
+struct DiePlace {
+    int64_t place;
+    int part;           // of `parts` workgroups a place
+};
+__device__ __forceinline__ DiePlace die_place(int parts)
+{
+    const unsigned die = blockIdx.x % kDies, at = blockIdx.x / kDies, run = gridDim.x / kDies / parts;
+    return DiePlace{(int64_t)die * run + at / parts, (int)(at % parts)};
 }
 int64_t tile_places(const AdapterArgs& a) { return a.starts ? a.T / kTileRows + a.B + 3 : a.B * ((a.T + kTileRows - 1) / kTileRows); }
 
@@ -119,7 +131,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     constexpr int PITCH = 16 * NT + 1, U = NT <= 4 ? 4 : NT == 8 ? 2 : 1;
     extern __shared__ float sums[];                     // [W][32][PITCH]
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
-    const Tile tile = tile_at(p, blockIdx.x);
+    const Tile tile = tile_at(p, die_place(1).place);
     if (tile.rows == 0 || tile.s < 0) return;
     const T *x[2], *rank_row[NT];
 #pragma unroll
@@ -141,7 +153,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     // A wavefront's run of whole steps, from a place on that differs between tiles: rows are often a power of two apart, and what is read of 16 rows at
     // once is in one memory channel.
     const int whole = p.C_in / M::STEP, begin = (int)((int64_t)whole * wave / W), steps = (int)((int64_t)whole * (wave + 1) / W) - begin;
-    int step = steps ? (int)(blockIdx.x % steps) : 0, done = 0;
+    int step = steps ? (int)(blockIdx.x / kDies % steps) : 0, done = 0;
     for (; done + U <= steps; done += U) {
         typename R::vec xv[U][2], av[U][NT];
 #pragma unroll
@@ -226,26 +238,29 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     }
 }
 
-// out of a tile's rows and a run of output channels, 64 of them a wavefront at a time; S steps of the rank are on their way together.  Output channels are the
-// matrix's rows; what comes of the product goes through LDS, so that y is read and out written in whole 128-byte lines.
+// out of a tile's rows and a run of output channels, 64 of them a wavefront at a time.  Output channels are the matrix's rows; what comes of the product goes
+// through LDS, so that y is read and out written in whole 128-byte lines.  ONCE: the rank is S steps.  EVEN: ranks and output channels are whole vectors.  A lane's places are 32-bit distances from the tile's first
+// row or the block's first row of b, which are the wavefront's: a block has 150 vector instructions beside its 48 products (rank 64), with 64-bit
+// addresses and rows' ends looked at everywhere it had 425, and waited for them more than for memory.
 constexpr int kOutWaves = 4, kOutPitch = 68;
-template <int EK, int S>
+template <int EK, int S, bool ONCE, bool EVEN>
 __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int chunks, int chunk)
 {
     typedef Matrix<EK> M;
     typedef typename M::R R;
     typedef typename M::T T;
     typedef typename R::vec vec;
-    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES;      // lanes a row of 64 channels, rows at a time
-    __shared__ float turned[kOutWaves][kTileRows][kOutPitch];
+    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES, HALF = 16 / RUN;  // lanes a row of 64 channels, rows at a time
+    __shared__ float turned[kOutWaves][16][kOutPitch];
     extern __shared__ float shared[];
     T* const low = reinterpret_cast<T*>(shared);        // [PARTS][32][K + VEC]
+    if constexpr (ONCE) K = S * M::STEP;
     const int pitch = K + VEC;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
-    // (workgroups that follow each other have different chunks: where there are as many as dies, or half, a die's workgroups have one, and its caches that part of b)
-    const Tile tile = tile_at(p, blockIdx.x / chunks);
+    const DiePlace at = die_place(chunks);
+    const Tile tile = tile_at(p, at.place);
     if (tile.rows == 0 || (tile.s < 0 && p.out == p.y)) return;
-    const int from = (int)(blockIdx.x % chunks) * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
+    const int from = at.part * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
     const T* const y = static_cast<const T*>(p.y) + tile.first * p.y_stride;
     T* const out = static_cast<T*>(p.out) + tile.first * p.out_stride;
     const int row = lane / LANES, column = lane % LANES * VEC;          // of a run of rows
@@ -256,9 +271,14 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
         return;
     }
     const Low<EK> source(p.work, rows, K);
-    float f[2];
+    float f[2 * HALF];
+    unsigned y_at[2 * HALF], out_at[2 * HALF];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) f[t] = source.factor[tile.first + (16 * t + m < tile.rows ? 16 * t + m : 0)];
+    for (int i = 0; i < 2 * HALF; ++i) {
+        const int r = i * RUN + row < tile.rows ? i * RUN + row : 0;
+        f[i] = source.factor[tile.first + r];
+        y_at[i] = (unsigned)(r * p.y_stride) + column, out_at[i] = (unsigned)(r * p.out_stride) + column;
+    }
     {
         const int run = K / VEC, all = kTileRows * PARTS * run;
         for (int k = threadIdx.x; k < all; k += 64 * kOutWaves) {
@@ -269,15 +289,20 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
     }
     __syncthreads();
     const T* const b = static_cast<const T*>(p.b) + (int64_t)tile.s * p.C_out * p.rank;
-    const int blocks = (to - from + 63) / 64, turn = (int)(blockIdx.x / chunks % blocks);
+    const int blocks = (to - from + 63) / 64, turn = (int)(at.place % blocks);
     for (int k = wave; k < blocks; k += kOutWaves) {
-        const int c0 = from + 64 * (k + turn < blocks ? k + turn : k + turn - blocks);
-        vec yv[kTileRows / RUN];
+        const int c0 = from + 64 * (k + turn < blocks ? k + turn : k + turn - blocks), left = to - c0;
+        const T *const y0 = y + c0, *const b0 = b + (int64_t)c0 * p.rank;
+        vec yv[2 * HALF];
+        unsigned b_at[4];
+        const bool here = EVEN && column < left;
 #pragma unroll
-        for (int i = 0; i < kTileRows / RUN; ++i) yv[i] = R::load(y + (i * RUN + row < tile.rows ? i * RUN + row : 0) * p.y_stride, c0 + column, to);
-        const T* rows_of_b[4];
+        for (int i = 0; i < 2 * HALF; ++i) {
+            if constexpr (EVEN) yv[i] = R::load(y0 + (here ? y_at[i] : y_at[i] - column));
+            else yv[i] = R::load(y0 + (y_at[i] - column), column, left);
+        }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) rows_of_b[j] = b + (int64_t)(c0 + 16 * j + m < to ? c0 + 16 * j + m : to - 1) * p.rank;
+        for (int j = 0; j < 4; ++j) b_at[j] = (16 * j + m < left ? 16 * j + m : left - 1) * p.rank;
         f32x4 acc[4][2];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -286,12 +311,19 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
         for (int k0 = 0; k0 < K; k0 += S * M::STEP) {
             vec bv[S][4];
 #pragma unroll
-            for (int u = 0; u < S; ++u)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int at = k0 + u * M::STEP;
-                    bv[u][j] = at + M::STEP <= p.rank ? R::load(rows_of_b[j] + at + q * VEC) : R::load(rows_of_b[j], at + q * VEC, p.rank);
+                for (int u = 0; u < S; ++u) {
+                    const int k1 = k0 + u * M::STEP + q * VEC;
+                    if constexpr (EVEN) bv[u][j] = R::load(b0 + b_at[j] + (k1 < p.rank ? k1 : 0));
+                    else bv[u][j] = R::load(b0 + b_at[j], k1, p.rank);
                 }
+            if (EVEN && k0 + S * M::STEP > p.rank)
+#pragma unroll
+                for (int u = 0; u < S; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (k0 + u * M::STEP + q * VEC >= p.rank) bv[u][j] = (T)0.f;
 #pragma unroll
             for (int u = 0; u < S; ++u)
 #pragma unroll
@@ -302,25 +334,31 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[j][t] = M::multiply(bv[u][j], v, acc[j][t]);
                     }
+            if constexpr (ONCE) break;
         }
-        // (a wavefront's own part of LDS: its instructions go there in their order)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int t = 0; t < 2; ++t) {
+            // (a wavefront's own part of LDS: its instructions go there in their order)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) *reinterpret_cast<f32x4*>(&turned[wave][16 * t + m][16 * j + 4 * q]) = acc[j][t] * f[t];
-        __builtin_amdgcn_wave_barrier();
+            for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(&turned[wave][m][16 * j + 4 * q]) = acc[j][t];
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int i = 0; i < kTileRows / RUN; ++i) {
-            typename R::floats v = __builtin_convertvector(yv[i], typename R::floats);
+            for (int h = 0; h < HALF; ++h) {
+                const int i = t * HALF + h;
+                typename R::floats v = __builtin_convertvector(yv[i], typename R::floats);
 #pragma unroll
-            for (int e = 0; e < VEC; e += 4) {
-                const f32x4 more = *reinterpret_cast<const f32x4*>(&turned[wave][i * RUN + row][column + e]);
+                for (int e = 0; e < VEC; e += 4) {
+                    const f32x4 more = *reinterpret_cast<const f32x4*>(&turned[wave][h * RUN + row][column + e]);
 #pragma unroll
-                for (int k4 = 0; k4 < 4; ++k4) v[e + k4] += more[k4];
+                    for (int k4 = 0; k4 < 4; ++k4) v[e + k4] = __builtin_fmaf(f[i], more[k4], v[e + k4]);
+                }
+                if (i * RUN + row < tile.rows) {
+                    if constexpr (!EVEN) R::store(out + c0 + (out_at[i] - column), column, left, v);
+                    else if (here) R::store(out + c0 + out_at[i], v);
+                }
             }
-            if (i * RUN + row < tile.rows) R::store(out + (i * RUN + row) * p.out_stride, c0 + column, to, v);
+            __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -418,12 +456,20 @@ __global__ __launch_bounds__(kRowThreads) void adapters_row_out_kernel(AdapterAr
 
 int64_t rows_of(const AdapterArgs& a) { return a.starts ? a.T : a.T * a.B; }
 
-// Tiles where a sequence has eight rows on average: a tile of few rows costs what a full one does.
-bool in_tiles(const AdapterArgs& a) { return rows_of(a) >= 8 * (int64_t)a.B; }
+// Tiles where a sequence has eight rows on average: a tile of few rows costs what a full one does.  Rows so far apart that a tile's are not within 32-bit distances
+// of each other go one by one as well.
+bool long_sequences(const AdapterArgs& a) { return rows_of(a) >= 8 * (int64_t)a.B; }
+bool in_tiles(const AdapterArgs& a)
+{
+    constexpr int64_t kFar = 1 << 24;
+    return long_sequences(a) && a.y_stride <= kFar && a.out_stride <= kFar;
+}
 
 // Single rows in one launch where a factor `a` is small enough for every workgroup of a row to read it.
 constexpr int64_t kWholeBytes = 128 << 10;
 bool whole_rows(const AdapterArgs& a, int ek) { return (int64_t)a.rank * a.C_in * elem_size(ek) <= kWholeBytes; }
+
+unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
 
 constexpr int kChunks = 4;              // workgroups for a tile's output channels
 
@@ -433,7 +479,7 @@ hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, hipStream_t st)
     const size_t lds = sizeof(float) * W * kTileRows * (16 * NT + 1);
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_low_kernel<EK, NT, W>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (allowed != hipSuccess) return allowed;
-    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3((unsigned)tile_places(a)), dim3(64 * W), lds, st, a, rows, K);
+    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3(die_groups(a, 1)), dim3(64 * W), lds, st, a, rows, K);
     return hipGetLastError();
 }
 
@@ -451,15 +497,20 @@ hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
     if (err != hipSuccess) return err;
     const int blocks = (a.C_out + 63) / 64, most = blocks < kChunks ? blocks : kChunks, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
     const size_t lds = (size_t)kTileRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
-    const dim3 grid((unsigned)(tile_places(a) * chunks)), block(64 * kOutWaves);
+    const dim3 grid(die_groups(a, chunks)), block(64 * kOutWaves);
     const int steps = K / Matrix<EK>::STEP;
     note_kernel("adapters_out_kernel", EK, a.rank);
-    if (steps % 4 == 0)
-        hipLaunchKernelGGL((adapters_out_kernel<EK, 4>), grid, block, lds, st, a, rows, K, chunks, chunk);
-    else if (steps % 2 == 0)
-        hipLaunchKernelGGL((adapters_out_kernel<EK, 2>), grid, block, lds, st, a, rows, K, chunks, chunk);
-    else
-        hipLaunchKernelGGL((adapters_out_kernel<EK, 1>), grid, block, lds, st, a, rows, K, chunks, chunk);
+    auto launch = [&](auto size, auto once, auto even) {
+        hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even()>), grid, block, lds, st, a, rows, K, chunks, chunk);
+    };
+    constexpr auto yes = std::true_type();
+    constexpr auto no = std::false_type();
+    if (a.rank % Row<EK>::VEC || a.C_out % Row<EK>::VEC) launch(std::integral_constant<int, 1>(), no, no);
+    else if (steps == 1) launch(std::integral_constant<int, 1>(), yes, yes);
+    else if (steps == 2) launch(std::integral_constant<int, 2>(), yes, yes);
+    else if (steps == 4) launch(std::integral_constant<int, 4>(), yes, yes);
+    else if (steps % 2 == 0) launch(std::integral_constant<int, 2>(), no, yes);
+    else launch(std::integral_constant<int, 1>(), no, yes);
     return hipGetLastError();
 }
 
@@ -493,14 +544,14 @@ constexpr int64_t kThreadsMost = ((int64_t)1 << 32) - 1;
 bool adapters_fit(const AdapterArgs& a)
 {
     const int64_t rows = rows_of(a);
-    if (in_tiles(a)) return tile_places(a) <= kThreadsMost / (kChunks * 64 * kOutWaves);
+    if (long_sequences(a)) return tile_places(a) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
     return rows <= kThreadsMost / kRowThreads / 2 && rows <= kThreadsMost / (64 * ((a.rank + kRowRanks - 1) / kRowRanks)) - kRowThreads;
 }
 
 int64_t adapters_workspace(const AdapterArgs& a, int ek)
 {
     const int64_t rows = rows_of(a);
-    if (in_tiles(a)) return rows * (padded_rank(a.rank, ek) * (ek == kElemF32 ? 4 : 6) + 4);
+    if (long_sequences(a)) return rows * (padded_rank(a.rank, ek) * (ek == kElemF32 ? 4 : 6) + 4);
     return whole_rows(a, ek) ? 0 : rows * a.rank * 4;
 }
 
