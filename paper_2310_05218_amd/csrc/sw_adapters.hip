@@ -47,28 +47,29 @@ __device__ __forceinline__ int adapter_of_row(const AdapterArgs& p, int64_t row)
     return b < 0 || b >= p.B ? -1 : adapter_of(p, b);
 }
 
-constexpr int kTileRows = 32;
+constexpr int kLowRows = 32, kOutRows = 32;        // of a tile, in the two products
 
 // A tile's rows (none: 0) and their adapter (-1: none).
 struct Tile {
     int64_t first;
     int rows, s;
 };
+template <int ROWS>
 __device__ __forceinline__ Tile tile_at(const AdapterArgs& p, int64_t place)
 {
     if (!p.starts) {
-        const int64_t each = (p.T + kTileRows - 1) / kTileRows, b = place / each, at = place % each * kTileRows;
+        const int64_t each = (p.T + ROWS - 1) / ROWS, b = place / each, at = place % each * ROWS;
         if (b >= p.B) return Tile{0, 0, -1};
-        return Tile{b * p.T + at, p.T - at < kTileRows ? (int)(p.T - at) : kTileRows, adapter_of(p, b)};
+        return Tile{b * p.T + at, p.T - at < ROWS ? (int)(p.T - at) : ROWS, adapter_of(p, b)};
     }
     // (j = 0 and B + 1: the rows before the first and after the last sequence)
     auto first = [&](int j) {
         const int64_t v = j == 0 ? 0 : p.starts[j - 1];
         return v < 0 ? 0 : v > p.T ? p.T : v;
     };
-    const int found = at_or_before(p.B + 2, place, [&](int j) { return first(j) / kTileRows + j; }), j = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
-    const int64_t begin = first(j), end = j == p.B + 1 ? p.T : first(j + 1), at = begin + (place - (begin / kTileRows + j)) * kTileRows, left = end - at;
-    Tile t{at, left <= 0 || at < 0 ? 0 : left < kTileRows ? (int)left : kTileRows, -1};
+    const int found = at_or_before(p.B + 2, place, [&](int j) { return first(j) / ROWS + j; }), j = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
+    const int64_t begin = first(j), end = j == p.B + 1 ? p.T : first(j + 1), at = begin + (place - (begin / ROWS + j)) * ROWS, left = end - at;
+    Tile t{at, left <= 0 || at < 0 ? 0 : left < ROWS ? (int)left : ROWS, -1};
     if (t.rows && j > 0 && j <= p.B) t.s = adapter_of(p, j - 1);
     return t;
 }
@@ -83,7 +84,7 @@ __device__ __forceinline__ DiePlace die_place(int parts)
     const unsigned die = blockIdx.x % kDies, at = blockIdx.x / kDies, run = gridDim.x / kDies / parts;
     return DiePlace{(int64_t)die * run + at / parts, (int)(at % parts)};
 }
-int64_t tile_places(const AdapterArgs& a) { return a.starts ? a.T / kTileRows + a.B + 3 : a.B * ((a.T + kTileRows - 1) / kTileRows); }
+int64_t tile_places(const AdapterArgs& a, int rows) { return a.starts ? a.T / rows + a.B + 3 : a.B * ((a.T + rows - 1) / rows); }
 
 // ---- tiles of rows ----------------------------------------------------------------------------------------------------------------------------
 
@@ -107,23 +108,29 @@ struct Matrix {
     }
 };
 
-// The rank as the second product has it.
-constexpr int padded_rank(int rank, int ek) { return ek == kElemF32 ? (rank + 15) / 16 * 16 : (rank + 31) / 32 * 32; }
-
-// { low [rows][PARTS][K], a factor for each row }
-template <int EK>
-struct Low {
-    typename Matrix<EK>::T* low;
-    float* factor;
-    __host__ __device__ Low(void* work, int64_t rows, int K)
-        : low(static_cast<typename Matrix<EK>::T*>(work)), factor(reinterpret_cast<float*>(low + rows * Matrix<EK>::PARTS * K))
-    {
+// Two steps of 16 rows of an operand.  A step's vectors are 64 bytes of each row, half of a line: so one instruction has eight rows' whole lines, lanes m and m + 8 of
+// each 16 both halves of a row, another the other eight, and they change halves (6100 rows of 2048, rank 64, half: 16.9 us, in halves of lines 18.7).
+template <class V>
+__device__ __forceinline__ void change_halves(V& a, V& b)
+{
+    typedef int words __attribute__((ext_vector_type(4)));
+    words wa = __builtin_bit_cast(words, a), wb = __builtin_bit_cast(words, b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int was = wa[k];
+        wa[k] = __builtin_amdgcn_update_dpp(was, wb[k], 0x128, 0xf, 0xc, false);       // lanes 8 ... 15: b of lanes 0 ... 7
+        wb[k] = __builtin_amdgcn_update_dpp(wb[k], was, 0x128, 0xf, 0x3, false);       // lanes 0 ... 7: a of lanes 8 ... 15
     }
-};
+    a = __builtin_bit_cast(V, wa), b = __builtin_bit_cast(V, wb);
+}
 
-// low of a tile's rows for up to 16 NT ranks, the input channels shared out to W wavefronts, U steps of them on their way together.
+// The rank as the second product has it.
+constexpr int padded_rank(int rank) { return (rank + 31) / 32 * 32; }
+
+// A part of low of a tile's rows for up to 16 NT ranks: a run of the input channels, shared out to W wavefronts, U steps of them on their way together.  work:
+// [parts][rows][K] fp32.
 template <int EK, int NT, int W>
-__global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int64_t rows, int K)
+__global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int64_t rows, int K, int parts)
 {
     typedef Matrix<EK> M;
     typedef typename M::R R;
@@ -131,14 +138,22 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     constexpr int PITCH = 16 * NT + 1, U = NT <= 4 ? 4 : NT == 8 ? 2 : 1;
     extern __shared__ float sums[];                     // [W][32][PITCH]
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
-    const Tile tile = tile_at(p, die_place(1).place);
+    const DiePlace place = die_place(parts);
+    const Tile tile = tile_at<kLowRows>(p, place.place);
     if (tile.rows == 0 || tile.s < 0) return;
-    const T *x[2], *rank_row[NT];
+    const T *const x = static_cast<const T*>(p.x) + tile.first * p.x_stride, *const a = static_cast<const T*>(p.a) + (int64_t)tile.s * p.rank * p.C_in;
+    // where a lane's vectors of two steps are (change_halves), from the tile's and the factor's first row
+    const int pair = (q + m / 8 * 4) * R::VEC;
+    unsigned x_at[2][2], a_at[NT][2];
+    auto x_row = [&](int r) { return (unsigned)((r < tile.rows ? r : 0) * p.x_stride); };
+    auto a_row = [&](int r) { return (unsigned)((r < p.rank ? r : p.rank - 1) * p.C_in); };
 #pragma unroll
-    for (int t = 0; t < 2; ++t) x[t] = static_cast<const T*>(p.x) + (tile.first + (16 * t + m < tile.rows ? 16 * t + m : 0)) * p.x_stride + q * R::VEC;
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        rank_row[n] = static_cast<const T*>(p.a) + ((int64_t)tile.s * p.rank + (16 * n + m < p.rank ? 16 * n + m : p.rank - 1)) * p.C_in + q * R::VEC;
+        for (int t = 0; t < 2; ++t) x_at[t][h] = x_row(16 * t + 8 * h + m % 8) + pair;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) a_at[n][h] = a_row(16 * n + 8 * h + m % 8) + pair;
+    }
     f32x4 acc[2][NT];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -152,89 +167,64 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     };
     // A wavefront's run of whole steps, from a place on that differs between tiles: rows are often a power of two apart, and what is read of 16 rows at
     // once is in one memory channel.
-    const int whole = p.C_in / M::STEP, begin = (int)((int64_t)whole * wave / W), steps = (int)((int64_t)whole * (wave + 1) / W) - begin;
-    int step = steps ? (int)(blockIdx.x / kDies % steps) : 0, done = 0;
-    for (; done + U <= steps; done += U) {
-        typename R::vec xv[U][2], av[U][NT];
+    const int whole = p.C_in / (2 * M::STEP), run = place.part * W + wave, runs = parts * W;       // in pairs of steps
+    const int begin = (int)((int64_t)whole * run / runs), steps = (int)((int64_t)whole * (run + 1) / runs) - begin;
+    int step = steps ? (int)(place.place % steps) : 0, done = 0;
+    auto add_pairs = [&](auto u_) {
+        constexpr int U2 = u_();
+        typename R::vec xv[U2][2][2], av[U2][2][NT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = (begin + step) * M::STEP;
+        for (int u = 0; u < U2; ++u) {
+            const T *const xs = x + (begin + step) * 2 * M::STEP, *const as = a + (begin + step) * 2 * M::STEP;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) xv[u][t] = R::load(x[t] + at);
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) av[u][n] = R::load(rank_row[n] + at);
+                for (int t = 0; t < 2; ++t) xv[u][h][t] = R::load(xs + x_at[t][h]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) av[u][h][n] = R::load(as + a_at[n][h]);
+            }
             step = step + 1 < steps ? step + 1 : 0;
         }
+        __builtin_amdgcn_sched_barrier(0);          // (all of them on their way before the first product)
 #pragma unroll
-        for (int u = 0; u < U; ++u) add(xv[u], av[u]);
-    }
-    for (; done < steps; ++done) {
-        typename R::vec xv[2], av[NT];
-        const int at = (begin + step) * M::STEP;
+        for (int u = 0; u < U2; ++u) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t] + at);
+            for (int t = 0; t < 2; ++t) change_halves(xv[u][0][t], xv[u][1][t]);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n] + at);
-        step = step + 1 < steps ? step + 1 : 0;
-        add(xv, av);
-    }
-    if (wave == W - 1 && whole * M::STEP < p.C_in) {
-        typename R::vec xv[2], av[NT];
-        const int at = whole * M::STEP, left = p.C_in - q * R::VEC;
+            for (int n = 0; n < NT; ++n) change_halves(av[u][0][n], av[u][1][n]);
+            add(xv[u][0], av[u][0]);
+            add(xv[u][1], av[u][1]);
+        }
+    };
+    constexpr int U2 = U / 2 > 0 ? U / 2 : 1;
+    for (; done + U2 <= steps; done += U2) add_pairs(std::integral_constant<int, U2>());
+    if constexpr (U2 > 1)
+        for (; done < steps; ++done) add_pairs(std::integral_constant<int, 1>());
+    if (run == runs - 1)
+        for (int c = whole * 2 * M::STEP; c < p.C_in; c += M::STEP) {
+            typename R::vec xv[2], av[NT];
+            const int at = c + q * R::VEC;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) xv[t] = R::load(x[t], at, left);
+            for (int t = 0; t < 2; ++t) xv[t] = R::load(x + x_row(16 * t + m), at, p.C_in);
 #pragma unroll
-        for (int n = 0; n < NT; ++n) av[n] = R::load(rank_row[n], at, left);
-        add(xv, av);
-    }
+            for (int n = 0; n < NT; ++n) av[n] = R::load(a + a_row(16 * n + m), at, p.C_in);
+            add(xv, av);
+        }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[(wave * kTileRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
+            for (int i = 0; i < 4; ++i) sums[(wave * kLowRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
     __syncthreads();
-    // 16 lanes a row
-    const Low<EK> to(p.work, rows, K);
-    const float factor = p.scales ? p.scales[tile.s] : 1.f;
-    for (int r = threadIdx.x / 16; r < tile.rows; r += 4 * W) {
-        float v[NT], scale = 1.f;
+    float* const low = static_cast<float*>(p.work) + (place.part * rows + tile.first) * K;
+    for (int k = threadIdx.x; k < tile.rows * K; k += 64 * W) {
+        const int r = k / K, n = k % K;
+        float v = 0.f;
+        if (n < p.rank)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            v[n] = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) v[n] += sums[(w * kTileRows + r) * PITCH + 16 * n + m];
-            if (16 * n + m >= p.rank) v[n] = 0.f;
-        }
-        if constexpr (EK == kElemF16) {
-            float most = 0.f;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) most = fmaxf(most, fabsf(v[n]));
-#pragma unroll
-            for (int d = 1; d < 16; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 16));
-            // 2^e with 2^13 <= most 2^-e < 2^14; rows of zeros, and of what is not finite, as they are
-            int e = most > 0.f && most < 3.4e38f ? __builtin_amdgcn_frexp_expf(most) - 14 : 0;
-            e = e < -100 ? -100 : e;
-            scale = __builtin_amdgcn_ldexpf(1.f, e);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) v[n] *= __builtin_amdgcn_ldexpf(1.f, -e);
-        }
-        T* const low = to.low + (tile.first + r) * M::PARTS * K;
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if (16 * n + m >= K) continue;
-            float rest = v[n];
-#pragma unroll
-            for (int k = 0; k < M::PARTS; ++k) {
-                const T one = (T)rest;
-                low[k * K + 16 * n + m] = one;
-                rest -= (float)one;
-            }
-        }
-        for (int n = 16 * NT + m; n < K; n += 16)
-#pragma unroll
-            for (int k = 0; k < M::PARTS; ++k) low[k * K + n] = (T)0.f;
-        if (m == 0) to.factor[tile.first + r] = scale * factor;
+            for (int w = 0; w < W; ++w) v += sums[(w * kLowRows + r) * PITCH + n];
+        low[k] = v;
     }
 }
 
@@ -244,13 +234,13 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
 // addresses and rows' ends looked at everywhere it had 425, and waited for them more than for memory.
 constexpr int kOutWaves = 4, kOutPitch = 68;
 template <int EK, int S, bool ONCE, bool EVEN>
-__global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int chunks, int chunk)
+__global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int parts, int chunks, int chunk)
 {
     typedef Matrix<EK> M;
     typedef typename M::R R;
     typedef typename M::T T;
     typedef typename R::vec vec;
-    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES, HALF = 16 / RUN;  // lanes a row of 64 channels, rows at a time
+    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES, PER = 16 / RUN, TS = kOutRows / 16;  // lanes a row of 64 channels, rows at a time
     __shared__ float turned[kOutWaves][16][kOutPitch];
     extern __shared__ float shared[];
     T* const low = reinterpret_cast<T*>(shared);        // [PARTS][32][K + VEC]
@@ -258,7 +248,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
     const int pitch = K + VEC;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
     const DiePlace at = die_place(chunks);
-    const Tile tile = tile_at(p, at.place);
+    const Tile tile = tile_at<kOutRows>(p, at.place);
     if (tile.rows == 0 || (tile.s < 0 && p.out == p.y)) return;
     const int from = at.part * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
     const T* const y = static_cast<const T*>(p.y) + tile.first * p.y_stride;
@@ -270,44 +260,75 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
                 R::store(out + r * p.out_stride, c, to, __builtin_convertvector(R::load(y + r * p.y_stride, c, to), typename R::floats));
         return;
     }
-    const Low<EK> source(p.work, rows, K);
-    float f[2 * HALF];
-    unsigned y_at[2 * HALF], out_at[2 * HALF];
-#pragma unroll
-    for (int i = 0; i < 2 * HALF; ++i) {
-        const int r = i * RUN + row < tile.rows ? i * RUN + row : 0;
-        f[i] = source.factor[tile.first + r];
-        y_at[i] = (unsigned)(r * p.y_stride) + column, out_at[i] = (unsigned)(r * p.out_stride) + column;
-    }
+    // low's parts are added and, of 16-bit tensors, split, eight lanes a row
+    __shared__ float factor[kOutRows];
     {
-        const int run = K / VEC, all = kTileRows * PARTS * run;
-        for (int k = threadIdx.x; k < all; k += 64 * kOutWaves) {
-            const int r = k / (PARTS * run), part = k / run % PARTS, c = k % run * VEC;
-            *reinterpret_cast<vec*>(low + (part * kTileRows + r) * pitch + c) =
-                *reinterpret_cast<const vec*>(source.low + ((tile.first + (r < tile.rows ? r : 0)) * PARTS + part) * K + c);
+        const float scale = p.scales ? p.scales[tile.s] : 1.f;
+        const int r = threadIdx.x / 8, eighth = threadIdx.x % 8;
+        static_assert(kOutRows * 8 == 64 * kOutWaves, "a row of low for every eight threads");
+        const float* const source = static_cast<const float*>(p.work) + (tile.first + (r < tile.rows ? r : 0)) * K;
+        auto values = [&](int c) {
+            f32x4 v = *reinterpret_cast<const f32x4*>(source + c);
+            for (int n = 1; n < parts; ++n) v += *reinterpret_cast<const f32x4*>(source + n * rows * K + c);
+            return v;
+        };
+        float back = 1.f, by = scale;
+        if constexpr (EK == kElemF16) {
+            float most = 0.f;
+            for (int c = 4 * eighth; c < K; c += 32) {
+                const f32x4 v = values(c);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = fmaxf(most, fabsf(v[e]));
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, 8));
+            // 2^e with 2^13 <= most 2^-e < 2^14; rows of zeros, and of what is not finite, as they are
+            int e = most > 0.f && most < 3.4e38f ? __builtin_amdgcn_frexp_expf(most) - 14 : 0;
+            e = e < -100 ? -100 : e;
+            back = __builtin_amdgcn_ldexpf(1.f, -e), by *= __builtin_amdgcn_ldexpf(1.f, e);
         }
+        for (int c = 4 * eighth; c < K; c += 32) {
+            f32x4 rest = values(c) * back;
+#pragma unroll
+            for (int n = 0; n < PARTS; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const T one = (T)rest[e];
+                    low[(n * kOutRows + r) * pitch + c + e] = one;
+                    rest[e] -= (float)one;
+                }
+        }
+        if (eighth == 0) factor[r] = by;
     }
     __syncthreads();
+    float f[TS * PER];
+    unsigned y_at[TS * PER], out_at[TS * PER];
+#pragma unroll
+    for (int i = 0; i < TS * PER; ++i) {
+        const int r = i * RUN + row < tile.rows ? i * RUN + row : 0;
+        f[i] = factor[i * RUN + row];
+        y_at[i] = (unsigned)(r * p.y_stride) + column, out_at[i] = (unsigned)(r * p.out_stride) + column;
+    }
     const T* const b = static_cast<const T*>(p.b) + (int64_t)tile.s * p.C_out * p.rank;
     const int blocks = (to - from + 63) / 64, turn = (int)(at.place % blocks);
     for (int k = wave; k < blocks; k += kOutWaves) {
         const int c0 = from + 64 * (k + turn < blocks ? k + turn : k + turn - blocks), left = to - c0;
         const T *const y0 = y + c0, *const b0 = b + (int64_t)c0 * p.rank;
-        vec yv[2 * HALF];
+        vec yv[TS * PER];
         unsigned b_at[4];
         const bool here = EVEN && column < left;
 #pragma unroll
-        for (int i = 0; i < 2 * HALF; ++i) {
+        for (int i = 0; i < TS * PER; ++i) {
             if constexpr (EVEN) yv[i] = R::load(y0 + (here ? y_at[i] : y_at[i] - column));
             else yv[i] = R::load(y0 + (y_at[i] - column), column, left);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) b_at[j] = (16 * j + m < left ? 16 * j + m : left - 1) * p.rank;
-        f32x4 acc[4][2];
+        f32x4 acc[4][TS];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) acc[j][t] = 0.f;
+            for (int t = 0; t < TS; ++t) acc[j][t] = 0.f;
         for (int k0 = 0; k0 < K; k0 += S * M::STEP) {
             vec bv[S][4];
 #pragma unroll
@@ -327,24 +348,24 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
 #pragma unroll
             for (int u = 0; u < S; ++u)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < TS; ++t)
 #pragma unroll
                     for (int n = 0; n < PARTS; ++n) {
-                        const vec v = *reinterpret_cast<const vec*>(low + (n * kTileRows + 16 * t + m) * pitch + k0 + u * M::STEP + q * VEC);
+                        const vec v = *reinterpret_cast<const vec*>(low + (n * kOutRows + 16 * t + m) * pitch + k0 + u * M::STEP + q * VEC);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[j][t] = M::multiply(bv[u][j], v, acc[j][t]);
                     }
             if constexpr (ONCE) break;
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < TS; ++t) {
             // (a wavefront's own part of LDS: its instructions go there in their order)
 #pragma unroll
             for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(&turned[wave][m][16 * j + 4 * q]) = acc[j][t];
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int h = 0; h < HALF; ++h) {
-                const int i = t * HALF + h;
+            for (int h = 0; h < PER; ++h) {
+                const int i = t * PER + h;
                 typename R::floats v = __builtin_convertvector(yv[i], typename R::floats);
 #pragma unroll
                 for (int e = 0; e < VEC; e += 4) {
@@ -376,16 +397,38 @@ __device__ __forceinline__ void dots(const AdapterArgs& p, int64_t row, int s, i
         a[j] = static_cast<const T*>(p.a) + ((int64_t)s * p.rank + (k + j < p.rank ? k + j : p.rank - 1)) * p.C_in;
         sum[j] = 0.f;
     }
-#pragma unroll 4
-    for (int c = threadIdx.x % 64 * R::VEC; c < p.C_in; c += 64 * R::VEC) {
-        const auto xv = __builtin_convertvector(R::load(x, c, p.C_in), typename R::floats);
+    const int lane = threadIdx.x % 64;
+    // U runs of 64 vectors, all on their way before the first is added
+    auto add = [&](auto u_, int c) {
+        constexpr int U = u_();
+        typename R::vec xv[U], av[U][N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const auto av = __builtin_convertvector(R::load(a[j], c, p.C_in), typename R::floats);
+        for (int u = 0; u < U; ++u) {
+            xv[u] = R::load(x + c + u * 64 * R::VEC);
 #pragma unroll
-            for (int e = 0; e < R::VEC; ++e) sum[j] = __builtin_fmaf(xv[e], av[e], sum[j]);
+            for (int j = 0; j < N; ++j) av[u][j] = R::load(a[j] + c + u * 64 * R::VEC);
         }
-    }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const auto xf = __builtin_convertvector(xv[u], typename R::floats);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const auto af = __builtin_convertvector(av[u][j], typename R::floats);
+#pragma unroll
+                for (int e = 0; e < R::VEC; ++e) sum[j] = __builtin_fmaf(xf[e], af[e], sum[j]);
+            }
+        }
+    };
+    // whole runs, a part of one, and what is left, an element a lane (rows' ends looked at everywhere would have a load wait for the one before)
+    constexpr int kRun = 64 * R::VEC, kMany = 4;
+    int c = 0;
+    for (; c + kMany * kRun <= p.C_in; c += kMany * kRun) add(std::integral_constant<int, kMany>(), c + lane * R::VEC);
+    for (; c + lane * R::VEC + R::VEC <= p.C_in; c += kRun) add(std::integral_constant<int, 1>(), c + lane * R::VEC);
+    const int last = p.C_in / R::VEC * R::VEC + lane;
+    if (last < p.C_in)
+#pragma unroll
+        for (int j = 0; j < N; ++j) sum[j] = __builtin_fmaf((float)x[last], (float)a[j][last], sum[j]);
 #pragma unroll
     for (int j = 0; j < N; ++j) sum[j] = lanes_sum<64>(sum[j]);
 }
@@ -443,11 +486,14 @@ __global__ __launch_bounds__(kRowThreads) void adapters_row_out_kernel(AdapterAr
         const T* const b = static_cast<const T*>(p.b) + ((int64_t)s * p.C_out + c) * p.rank;
         const float yc = (float)y[c];
         float sum = 0.f;
-        for (int k = 0; k < p.rank; k += R::VEC) {
-            const auto bv = __builtin_convertvector(R::load(b, k, p.rank), typename R::floats);
+        const int whole = p.rank / R::VEC * R::VEC;
+#pragma unroll 4
+        for (int k = 0; k < whole; k += R::VEC) {
+            const auto bv = __builtin_convertvector(R::load(b + k), typename R::floats);
 #pragma unroll
-            for (int e = 0; e < R::VEC; ++e) sum = __builtin_fmaf(k + e < p.rank ? low[k + e] : 0.f, bv[e], sum);
+            for (int e = 0; e < R::VEC; ++e) sum = __builtin_fmaf(low[k + e], bv[e], sum);
         }
+        for (int k = whole; k < p.rank; ++k) sum = __builtin_fmaf(low[k], (float)b[k], sum);
         out[c] = (T)__builtin_fmaf(scale, sum, yc);
     }
 }
@@ -462,24 +508,44 @@ bool long_sequences(const AdapterArgs& a) { return rows_of(a) >= 8 * (int64_t)a.
 bool in_tiles(const AdapterArgs& a)
 {
     constexpr int64_t kFar = 1 << 24;
-    return long_sequences(a) && a.y_stride <= kFar && a.out_stride <= kFar;
+    return long_sequences(a) && a.x_stride <= kFar && a.y_stride <= kFar && a.out_stride <= kFar;
 }
 
-// Single rows in one launch where a factor `a` is small enough for every workgroup of a row to read it.
-constexpr int64_t kWholeBytes = 128 << 10;
-bool whole_rows(const AdapterArgs& a, int ek) { return (int64_t)a.rank * a.C_in * elem_size(ek) <= kWholeBytes; }
+// Single rows: workgroups for every CU, several a row where rows are few.  In one launch where every workgroup of a row reads its factor `a`, as long as that is little
+// in all (64 rows of rank 16 on 2048 channels bf16, 17 MB: 6.4 us, in two launches 7.2; fp32, 34 MB: 14 and 8.6).
+constexpr int kCUs = 256;
+constexpr int64_t kReadMost = 1 << 24;
+int row_chunks(const AdapterArgs& a, int groups)
+{
+    const int64_t rows = rows_of(a), want = (groups + rows - 1) / rows, most = (a.C_out + kRowThreads - 1) / kRowThreads;
+    return (int)(want < most ? want : most);
+}
+bool whole_rows(const AdapterArgs& a, int ek)
+{
+    const int64_t factor = (int64_t)a.rank * a.C_in * elem_size(ek), rows = rows_of(a);
+    return factor <= kReadMost / row_chunks(a, kCUs) / rows;
+}
 
-unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
+unsigned die_groups(const AdapterArgs& a, int rows, int parts) { return (unsigned)((tile_places(a, rows) + kDies - 1) / kDies * kDies * parts); }
 
 constexpr int kChunks = 4;              // workgroups for a tile's output channels
 
-template <int EK, int NT, int W>
-hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, hipStream_t st)
+// Workgroups for a tile's input channels, where tiles are too few for the chip: at least 32 steps each.
+int low_parts(const AdapterArgs& a, int ek)
 {
-    const size_t lds = sizeof(float) * W * kTileRows * (16 * NT + 1);
+    const int64_t places = tile_places(a, kLowRows), steps = a.C_in / (ek == kElemF32 ? 16 : 32);
+    int64_t parts = kCUs / places;
+    if (parts > steps / 32) parts = steps / 32;
+    return (int)(parts < 1 ? 1 : parts);
+}
+
+template <int EK, int NT, int W>
+hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, int parts, hipStream_t st)
+{
+    const size_t lds = sizeof(float) * W * kLowRows * (16 * NT + 1);
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_low_kernel<EK, NT, W>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (allowed != hipSuccess) return allowed;
-    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3(die_groups(a, 1)), dim3(64 * W), lds, st, a, rows, K);
+    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3(die_groups(a, kLowRows, parts)), dim3(64 * W), lds, st, a, rows, K, parts);
     return hipGetLastError();
 }
 
@@ -487,21 +553,21 @@ template <int EK>
 hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
 {
     const int64_t rows = rows_of(a);
-    const int K = padded_rank(a.rank, EK);
+    const int K = padded_rank(a.rank), parts = low_parts(a, EK);
     hipError_t err;
-    if (a.rank <= 16) err = launch_low<EK, 1, 8>(a, rows, K, st);
-    else if (a.rank <= 32) err = launch_low<EK, 2, 8>(a, rows, K, st);
-    else if (a.rank <= 64) err = launch_low<EK, 4, 8>(a, rows, K, st);
-    else if (a.rank <= 128) err = launch_low<EK, 8, 8>(a, rows, K, st);
-    else err = launch_low<EK, 16, 4>(a, rows, K, st);
+    if (a.rank <= 16) err = launch_low<EK, 1, 8>(a, rows, K, parts, st);
+    else if (a.rank <= 32) err = launch_low<EK, 2, 8>(a, rows, K, parts, st);
+    else if (a.rank <= 64) err = launch_low<EK, 4, 8>(a, rows, K, parts, st);
+    else if (a.rank <= 128) err = launch_low<EK, 8, 8>(a, rows, K, parts, st);
+    else err = launch_low<EK, 16, 4>(a, rows, K, parts, st);
     if (err != hipSuccess) return err;
     const int blocks = (a.C_out + 63) / 64, most = blocks < kChunks ? blocks : kChunks, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
-    const size_t lds = (size_t)kTileRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
-    const dim3 grid(die_groups(a, chunks)), block(64 * kOutWaves);
+    const size_t lds = (size_t)kOutRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
+    const dim3 grid(die_groups(a, kOutRows, chunks)), block(64 * kOutWaves);
     const int steps = K / Matrix<EK>::STEP;
     note_kernel("adapters_out_kernel", EK, a.rank);
     auto launch = [&](auto size, auto once, auto even) {
-        hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even()>), grid, block, lds, st, a, rows, K, chunks, chunk);
+        hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even()>), grid, block, lds, st, a, rows, K, parts, chunks, chunk);
     };
     constexpr auto yes = std::true_type();
     constexpr auto no = std::false_type();
@@ -524,10 +590,8 @@ hipError_t launch_rows(const AdapterArgs& a, hipStream_t st)
         hipLaunchKernelGGL(adapters_row_low_kernel<EK>, dim3((unsigned)((rows * each + kRowThreads / 64 - 1) / (kRowThreads / 64))), dim3(kRowThreads), 0, st, a, rows, each);
         if (const hipError_t err = hipGetLastError()) return err;
     }
-    // workgroups for every CU, several a row where rows are few
-    constexpr int kGroups = 512;
-    const int64_t want = (kGroups + rows - 1) / rows, most = (a.C_out + kRowThreads - 1) / kRowThreads;
-    const int per = (int)((most + (want < most ? want : most) - 1) / (want < most ? want : most)), chunk = per * kRowThreads, chunks = (a.C_out + chunk - 1) / chunk;
+    const int most = (a.C_out + kRowThreads - 1) / kRowThreads, want = row_chunks(a, whole ? kCUs : 2 * kCUs);
+    const int chunk = (most + want - 1) / want * kRowThreads, chunks = (a.C_out + chunk - 1) / chunk;
     const dim3 grid((unsigned)(rows * chunks)), block(kRowThreads);
     note_kernel("adapters_row_out_kernel", EK, whole);
     if (whole)
@@ -544,14 +608,14 @@ constexpr int64_t kThreadsMost = ((int64_t)1 << 32) - 1;
 bool adapters_fit(const AdapterArgs& a)
 {
     const int64_t rows = rows_of(a);
-    if (long_sequences(a)) return tile_places(a) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
+    if (long_sequences(a)) return tile_places(a, kLowRows) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
     return rows <= kThreadsMost / kRowThreads / 2 && rows <= kThreadsMost / (64 * ((a.rank + kRowRanks - 1) / kRowRanks)) - kRowThreads;
 }
 
 int64_t adapters_workspace(const AdapterArgs& a, int ek)
 {
     const int64_t rows = rows_of(a);
-    if (long_sequences(a)) return rows * (padded_rank(a.rank, ek) * (ek == kElemF32 ? 4 : 6) + 4);
+    if (long_sequences(a)) return low_parts(a, ek) * rows * padded_rank(a.rank) * 4;
     return whole_rows(a, ek) ? 0 : rows * a.rank * 4;
 }
 
