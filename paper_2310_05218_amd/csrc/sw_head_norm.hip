@@ -55,10 +55,10 @@ struct Task {
     int chunk;
     int64_t step_rows;
     int step_chunks, chunks;
-    __device__ __forceinline__ Task(int64_t first, int64_t step, int chunks_) : chunks(chunks_)
+    __device__ __forceinline__ Task(unsigned first, unsigned step, unsigned chunks_) : chunks((int)chunks_)
     {
-        row = first / chunks, chunk = (int)(first % chunks);
-        step_rows = step / chunks, step_chunks = (int)(step % chunks);
+        row = first / chunks_, chunk = (int)(first % chunks_);
+        step_rows = step / chunks_, step_chunks = (int)(step % chunks_);
     }
     __device__ __forceinline__ void next()
     {
@@ -171,39 +171,43 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs p, Hea
     const HeadNormSide side = which ? p.side[1] : p.side[0];
     const H at(lane, p.D, p.pairs);
     floats wu, ww, su = 0.f, sw = 0.f;
-    at.weights(side.weight, wu, ww);
-    double frequency[VEC];
-#pragma unroll
-    for (int m = 0; m < VEC; ++m) frequency[m] = at.pair < 0 ? 0. : (double)p.frequencies[at.pair + m];
     const float inv = 1.f / (float)p.D;
     const int64_t rows = p.B * p.T;
-    Task task((int64_t)block * kGroups + threadIdx.x / G, (int64_t)(which ? groups.groups[1] : groups.groups[0]) * kGroups, which ? groups.chunks[1] : groups.chunks[0]);
+    Task task(block * kGroups + threadIdx.x / G, (which ? groups.groups[1] : groups.groups[0]) * kGroups, which ? groups.chunks[1] : groups.chunks[0]);
+    struct Operands {
+        typename H::Raw x, dy;
+    };
+    at.weights(side.weight, wu, ww);
     // (lanes of a group go on together; those of a wavefront's other groups may have ended)
     for (; task.row < rows; task.next()) {
         const int64_t batch = p.B == 1 ? 0 : task.row / p.T, token = task.row - batch * p.T;
         const T *x = row_of<T>(side.x, batch, token), *dy = BACKWARD ? row_of<T>(side.dy, batch, token) : nullptr;
         T* y = const_cast<T*>(row_of<T>(side.y, batch, token));
-        typename H::Raw raw = at.load(x + task.chunk * side.x.head), raw_dy;
-        if constexpr (BACKWARD) raw_dy = at.load(dy + task.chunk * side.dy.head);
+        auto fetch = [&](Operands& o, int head) {
+            if (head >= side.heads) return;
+            o.x = at.load(x + head * side.x.head);
+            if constexpr (BACKWARD) o.dy = at.load(dy + head * side.dy.head);
+        };
+        // two heads on their way beside the one that is worked on
+        Operands one, two;
+        fetch(one, task.chunk);
+        fetch(two, task.chunk + task.chunks);
         const int position = p.positions ? p.positions[task.row] : (int)token;
         floats c, s;
 #pragma unroll
         for (int m = 0; m < VEC; ++m) {
             float cm, sm;
-            turn(position, frequency[m], &cm, &sm);
+            turn(position, at.pair < 0 ? 0. : (double)p.frequencies[at.pair + m], &cm, &sm);
             c[m] = cm, s[m] = sm;
         }
-        for (int head = task.chunk; head < side.heads; head += task.chunks) {
-            floats u, w;
-            H::split(raw, u, w);
-            const int64_t next = head + task.chunks < side.heads ? head + task.chunks : head;
-            raw = at.load(x + next * side.x.head);
+        auto work = [&](Operands& o, int head) {
+            floats u, w, du, dw;
+            H::split(o.x, u, w);
+            if constexpr (BACKWARD) H::split(o.dy, du, dw);
+            fetch(o, head + 2 * task.chunks);
             const float r = 1.f / sqrtf(lanes_sum<G>(at.dot(u, w, u, w)) * inv + p.eps);
             u *= r, w *= r;
             if constexpr (BACKWARD) {
-                floats du, dw;
-                H::split(raw_dy, du, dw);
-                raw_dy = at.load(dy + next * side.dy.head);
                 floats gu = du * c + dw * s, gw = dw * c - du * s;
                 su += gu * u, sw += gw * w;
                 gu *= wu, gw *= ww;
@@ -213,6 +217,10 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs p, Hea
                 u *= wu, w *= ww;
                 at.store(y + head * side.y.head, u * c - w * s, u * s + w * c);
             }
+        };
+        for (int head = task.chunk; head < side.heads; head += 2 * task.chunks) {
+            work(one, head);
+            if (head + task.chunks < side.heads) work(two, head + task.chunks);
         }
     }
     if constexpr (BACKWARD) {
@@ -261,7 +269,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_any_kernel(HeadNormArgs p,
         weight[k] = e < p.D && side.weight ? side.weight[e] : 1.f;
     }
     const int64_t rows = p.B * p.T;
-    Task task((int64_t)block * (kThreads / 64) + wave, (int64_t)(which ? groups.groups[1] : groups.groups[0]) * (kThreads / 64), which ? groups.chunks[1] : groups.chunks[0]);
+    Task task(block * (kThreads / 64) + wave, (which ? groups.groups[1] : groups.groups[0]) * (kThreads / 64), which ? groups.chunks[1] : groups.chunks[0]);
     for (; task.row < rows; task.next()) {
         const int64_t batch = p.B == 1 ? 0 : task.row / p.T, token = task.row - batch * p.T;
         const int position = p.positions ? p.positions[task.row] : (int)token;
