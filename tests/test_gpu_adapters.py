@@ -197,3 +197,19 @@ def test_another_stream_and_graphs(sw):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(out, want))
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_offsets_beyond_32_bits(sw, packed):
+    """Rows so far apart that their places take more than 32 bits of bytes."""
+    rows, far = 16, (1 << 28) + 16
+    x, a, b, y, scales = make(rows, 2, 64, 72, 8, "bf16", 6)
+    big = torch.zeros(rows * far, dtype=torch.bfloat16, device="cuda")
+    X, Y = big.as_strided((rows, 64), (far, 1)), big[64:].as_strided((rows, 72), (far, 1))
+    X.copy_(x), Y.copy_(y)
+    slots = i32([1, 0]) if packed else i32([k % 2 for k in range(rows)])
+    args = scales.cuda(), slots, i32([0, 5, rows]) if packed else None
+    of = [1] * 5 + [0] * 11 if packed else [k % 2 for k in range(rows)]
+    check(sw.sw_adapters(X, a.cuda(), b.cuda(), y.cuda(), *args), x, a, b, y, scales, of, "bf16")
+    check(sw.sw_adapters(X, a.cuda(), b.cuda(), Y, *args, out=Y), x, a, b, y, scales, of, "bf16")
+    assert torch.equal(X.cpu(), x)

@@ -391,3 +391,24 @@ def test_calls_side_by_side(sw):
             sw.sw_gated_recurrence(*args, out=o[k], stream=st)
     torch.cuda.synchronize()
     assert all(torch.equal(v, want) for o in outs for v in o)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_offsets_beyond_32_bits(sw, t):
+    """Tokens and sequences so far apart that their places take more than 32 bits of bytes."""
+    T, C = 5, 40
+    far = (1 << 30) // (2 if t == "f32" else 1) + 8
+    x, r, i, dh, ld, _, _ = make(T, C, t, 2)
+    big = torch.zeros(T * far, dtype=TYPES[t], device="cuda")
+    X = big.as_strided((T, C), (far, 1))
+    X.copy_(x)
+    args = r[None].cuda(), i[None].cuda(), ld.cuda()
+    want = sw.sw_gated_recurrence(x[None].cuda(), *args)
+    assert torch.equal(sw.sw_gated_recurrence(X[None], *args), want)
+    grads = sw.sw_gated_recurrence_backward(dh[None].cuda(), x[None].cuda(), *args, want)
+    assert all(torch.equal(a, b) for a, b in zip(sw.sw_gated_recurrence_backward(dh[None].cuda(), X[None], *args, want), grads))
+    sw.sw_gated_recurrence(x[None].cuda(), *args, out=X[None])
+    assert torch.equal(X, want[0])
+    rows = sw.sw_gated_recurrence(x[:, None].cuda(), r[:, None].cuda(), i[:, None].cuda(), ld.cuda())
+    X.copy_(x)
+    assert torch.equal(sw.sw_gated_recurrence(X[:, None], r[:, None].cuda(), i[:, None].cuda(), ld.cuda()), rows)
