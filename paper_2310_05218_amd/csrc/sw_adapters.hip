@@ -567,17 +567,20 @@ hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
     const int steps = K / Matrix<EK>::STEP;
     note_kernel("adapters_out_kernel", EK, a.rank);
     auto launch = [&](auto size, auto once, auto even) {
+        static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_out_kernel<EK, size(), once(), even()>),
+                                                              hipFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
+        if (allowed != hipSuccess) return allowed;
         hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even()>), grid, block, lds, st, a, rows, K, parts, chunks, chunk);
+        return hipGetLastError();
     };
     constexpr auto yes = std::true_type();
     constexpr auto no = std::false_type();
-    if (a.rank % Row<EK>::VEC || a.C_out % Row<EK>::VEC) launch(std::integral_constant<int, 1>(), no, no);
-    else if (steps == 1) launch(std::integral_constant<int, 1>(), yes, yes);
-    else if (steps == 2) launch(std::integral_constant<int, 2>(), yes, yes);
-    else if (steps == 4) launch(std::integral_constant<int, 4>(), yes, yes);
-    else if (steps % 2 == 0) launch(std::integral_constant<int, 2>(), no, yes);
-    else launch(std::integral_constant<int, 1>(), no, yes);
-    return hipGetLastError();
+    if (a.rank % Row<EK>::VEC || a.C_out % Row<EK>::VEC) return launch(std::integral_constant<int, 1>(), no, no);
+    if (steps == 1) return launch(std::integral_constant<int, 1>(), yes, yes);
+    if (steps == 2) return launch(std::integral_constant<int, 2>(), yes, yes);
+    if (steps == 4) return launch(std::integral_constant<int, 4>(), yes, yes);
+    if (steps % 2 == 0) return launch(std::integral_constant<int, 2>(), no, yes);
+    return launch(std::integral_constant<int, 1>(), no, yes);
 }
 
 template <int EK>

@@ -306,8 +306,9 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     return t;
 }
 
-// channels a lane has
-int lane_channels(const RecurrenceBatch& n, int ek) { return ek == kElemF32 || n.C < 2 ? 1 : 2; }
+// Channels a lane has.  The last lane of an odd width shares one with its neighbour; where that would be another workgroup's, which may have written a state in place
+// that this one has not read, lanes have one channel.
+int lane_channels(const RecurrenceBatch& n, int ek) { return ek == kElemF32 || n.C % (64 * 2) == 1 ? 1 : 2; }
 
 hipError_t clear_chain(void* work, int64_t words, hipStream_t st)
 {

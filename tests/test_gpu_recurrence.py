@@ -412,3 +412,24 @@ def test_offsets_beyond_32_bits(sw, t):
     rows = sw.sw_gated_recurrence(x[:, None].cuda(), r[:, None].cuda(), i[:, None].cuda(), ld.cuda())
     X.copy_(x)
     assert torch.equal(sw.sw_gated_recurrence(X[:, None], r[:, None].cuda(), i[:, None].cuda(), ld.cuda()), rows)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C", [1, 2, 3, 65, 127, 128, 129, 131, 255, 257, 385])
+@pytest.mark.parametrize("packed", [False, True])
+def test_states_in_place(sw, C, packed, t):
+    """States and gradients of states that replace what they come from, at widths whose last channels are a lane's or a workgroup's of their own: several times over,
+    the same bits as into tensors of their own."""
+    B, T = 6, 300
+    x, r, i, dh, ld, s0, df = make(B * T, C, t, C, B)
+    shape = (lambda v: v.cuda()) if packed else (lambda v: v.reshape(B, T, C).cuda())
+    args = shape(x), shape(r), shape(i), ld.cuda()
+    starts = torch.arange(0, (B + 1) * T, T).int().cuda() if packed else None
+    final, d_state = torch.empty(B, C, device="cuda"), torch.empty(B, C, device="cuda")
+    h = sw.sw_gated_recurrence(*args, starts=starts, state=s0.cuda(), final_state=final)
+    grads = sw.sw_gated_recurrence_backward(shape(dh), *args, h, starts=starts, state=s0.cuda(), d_final_state=df.cuda(), d_state=d_state)
+    for _ in range(5):
+        s, d = s0.cuda(), df.cuda()
+        assert torch.equal(sw.sw_gated_recurrence(*args, starts=starts, state=s, final_state=s), h) and torch.equal(s, final)
+        again = sw.sw_gated_recurrence_backward(shape(dh), *args, h, starts=starts, state=s0.cuda(), d_final_state=d, d_state=d)
+        assert all(torch.equal(a, b) for a, b in zip(again, grads)) and torch.equal(d, d_state)
