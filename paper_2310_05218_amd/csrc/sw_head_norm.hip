@@ -49,6 +49,13 @@ struct HeadGroups {
     __host__ __device__ int all() const { return groups[0] + groups[1]; }
 };
 
+// Where a workgroup's sums go: a row of them to be folded or, of a single workgroup a side, the result; null: not wanted.
+__device__ __forceinline__ float* sums_of(const HeadNormArgs& p, const HeadGroups& groups, bool which)
+{
+    if (groups.all() == 2) return which ? p.side[1].dweight : p.side[0].dweight;
+    return p.work ? static_cast<float*>(p.work) + (int64_t)blockIdx.x * p.D : nullptr;
+}
+
 // A group's row and chunk, on from one to the next a launch apart.
 struct Task {
     int64_t row;
@@ -224,7 +231,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs p, Hea
         }
     }
     if constexpr (BACKWARD) {
-        if (!p.work) return;
+        if (!sums_of(p, groups, which)) return;
         // the sums of a workgroup's groups of lanes, an element a thread
         __shared__ float lds[kGroups][G][2 * VEC + 1];
         floats a, b;
@@ -239,7 +246,7 @@ __global__ __launch_bounds__(kThreads) void head_norm_kernel(HeadNormArgs p, Hea
         float sum = 0.f;
         for (int g = 0; g < kGroups; ++g) sum += lds[g][e / (2 * VEC)][m];
         // (lanes that share an element have the same sum of it)
-        if (of.skip < VEC) static_cast<float*>(p.work)[(int64_t)blockIdx.x * p.D + (m < VEC ? of.first + m : of.second + m - VEC)] = sum;
+        if (of.skip < VEC) sums_of(p, groups, which)[m < VEC ? of.first + m : of.second + m - VEC] = sum;
     }
 }
 
@@ -327,12 +334,12 @@ __global__ __launch_bounds__(kThreads) void head_norm_any_kernel(HeadNormArgs p,
         }
     }
     if constexpr (BACKWARD) {
-        if (!p.work) return;
+        if (!sums_of(p, groups, which)) return;
 #pragma unroll
         for (int k = 0; k < kMost; ++k) lds[wave][lane + 64 * k] = sums[k];
         __syncthreads();
         const int e = threadIdx.x;
-        if (e < p.D) static_cast<float*>(p.work)[(int64_t)blockIdx.x * p.D + e] = lds[0][e] + lds[1][e] + lds[2][e] + lds[3][e];
+        if (e < p.D) sums_of(p, groups, which)[e] = lds[0][e] + lds[1][e] + lds[2][e] + lds[3][e];
     }
 }
 
@@ -358,7 +365,7 @@ constexpr int kForwardWaves = 8192, kBackwardGroups = 1024;
 // Heads of a row go to several groups of lanes as far as wavefronts are few, to one at most kHeads at a time otherwise; workgroups are what the chip holds.
 HeadGroups head_groups(const HeadNormArgs& a, int lanes, int most_groups)
 {
-    constexpr int kHeads = 8;
+    constexpr int kHeads = 8, kFew = 2;
     const int per = kThreads / lanes;
     const int64_t rows = a.B * a.T;
     HeadGroups g;
@@ -369,6 +376,11 @@ HeadGroups head_groups(const HeadNormArgs& a, int lanes, int most_groups)
         each = each < 1 ? 1 : each > kHeads ? kHeads : each;
         g.chunks[i] = (int)((heads + each - 1) / each);
         want[i] = (rows * g.chunks[i] + per - 1) / per;
+    }
+    // (of few heads a workgroup a side has all: gradients of weights then need no other launch)
+    if (want[0] <= kFew && want[1] <= kFew && most_groups == kBackwardGroups) {
+        g.groups[0] = g.groups[1] = 1;
+        return g;
     }
     // (in proportion to the heads there are)
     for (int i = 0; i < 2; ++i) {
@@ -432,7 +444,7 @@ hipError_t launch_head_norm_backward(const HeadNormArgs& args, int ek, hipStream
                     hipLaunchKernelGGL((head_norm_kernel<e(), lanes(), false, true>), grid, block, 0, st, a, g);
             }
             if (const hipError_t err = hipGetLastError()) return err;
-            if (!a.work) return hipSuccess;
+            if (!a.work || g.all() == 2) return hipSuccess;
             const float* partial = static_cast<const float*>(a.work);
             return launch_fold(FoldArgs{{{partial, g.groups[0], a.side[0].dweight}, {partial + (int64_t)g.groups[0] * a.D, g.groups[1], a.side[1].dweight}}, a.D}, st);
         });

@@ -7,6 +7,22 @@ namespace swconv {
 
 namespace {
 
+// A wavefront's rows: `rows` of them from `first` on, of a sequence (none where a workgroup has places for more short ones than there are).
+struct Sequence {
+    int64_t batch, first;
+    int rows;
+    __device__ __forceinline__ Sequence(const Tiles& tiles, const Place& at, int wave, int64_t T, int R, bool backwards = false)
+    {
+        batch = at.batch * tiles.per + wave / tiles.waves;
+        const int along = wave % tiles.waves;
+        const int64_t segment = backwards ? tiles.segments - 1 - at.segment : at.segment;
+        first = (segment * tiles.waves + (backwards ? tiles.waves - 1 - along : along)) * R;
+        const int64_t left = batch < tiles.batches ? T - first : 0;
+        rows = left < 0 ? 0 : left < R ? (int)left : R;
+        batch = batch < tiles.batches ? batch : tiles.batches - 1;
+    }
+};
+
 constexpr int kForwardRows = 8, kForwardWaves = 16;
 
 // A tile of V channels a lane: decays and terms of its rows in registers, read once, the carry, then the rows' states.
@@ -20,19 +36,20 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
     __shared__ unsigned ticket;
     const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
     const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = tiles.waves;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const Sequence of(tiles, at, wave, p.n.T, R);
     // (the last lanes of a width that is no whole number of groups share channels, with equal results)
     int channel = at.group * group_width<V>() + lane * V;
     channel = channel < p.n.C - V ? channel : p.n.C - V;
-    const int64_t first = ((int64_t)at.segment * waves + wave) * R, left = p.n.T - first;
-    const int rows = left < 0 ? 0 : left < R ? (int)left : R;
+    const int64_t first = of.first;
+    const int rows = of.rows;
     float log_decay[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]);
     typename L::vec x[R], r[R], i[R];
-    L::template load<R>(p.decay_gate, at.batch, first, p.n.T, channel, r);
-    L::template load<R>(p.input_gate, at.batch, first, p.n.T, channel, i);
-    L::template load<R>(p.x, at.batch, first, p.n.T, channel, x);
+    L::template load<R>(p.decay_gate, of.batch, first, p.n.T, channel, r);
+    L::template load<R>(p.input_gate, of.batch, first, p.n.T, channel, i);
+    L::template load<R>(p.x, of.batch, first, p.n.T, channel, x);
     PackedRows packed{0, 0, 0, 0, -1};
     if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
     float a[R][V], b[R][V];
@@ -65,7 +82,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
                     for (int v = 0; v < V; ++v) b[k][v] = 0.f;
             }
     } else if (first == 0) {
-        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        const int entry = p.n.slots ? p.n.slots[of.batch] : (int)of.batch;
         begin(0, entry < p.n.n_states ? entry : -1);
     }
     const unsigned cut = packed.begins | packed.outside;
@@ -81,13 +98,13 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
     }
     __syncthreads();
     float h[V];
-    carry_in<V, kForwardWaves>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, h);
+    carry_in<V, kForwardWaves>(chain, tiles, at, of.batch * p.n.C + channel, wave, pairs, met, h);
     auto keep = [&](int entry) {
         if (p.final_state && entry >= 0)
 #pragma unroll
             for (int v = 0; v < V; ++v) p.final_state[(int64_t)entry * p.n.C + channel + v] = h[v];
     };
-    T* out = static_cast<T*>(const_cast<void*>(p.h.p)) + at.batch * p.h.batch + first * p.h.token;
+    T* out = static_cast<T*>(const_cast<void*>(p.h.p)) + of.batch * p.h.batch + first * p.h.token;
 #pragma unroll
     for (int k = 0; k < R; ++k, out += p.h.token) {
         if (k >= rows) continue;
@@ -106,39 +123,40 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
                 keep(entry);
             });
     } else if (rows > 0 && first + rows == p.n.T) {
-        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        const int entry = p.n.slots ? p.n.slots[of.batch] : (int)of.batch;
         keep(entry < p.n.n_states ? entry : -1);
     }
 }
 
-constexpr int kBackwardRows = 8, kBackwardWaves = 8;
+constexpr int kBackwardRows = 8;
 
 // The same backwards in time: what a token passes on to the one before is c' = a (dh + c).  A workgroup's first wavefront has its last rows.
-template <int EK, int V, bool PACKED>
-__global__ __launch_bounds__(64 * kBackwardWaves) void recurrence_backward_kernel(RecurrenceBackwardArgs p, Tiles tiles, float* partial)
+template <int EK, int V, bool PACKED, int W>
+__global__ __launch_bounds__(64 * W) void recurrence_backward_kernel(RecurrenceBackwardArgs p, Tiles tiles, float* partial)
 {
     typedef Lane<EK, V> L;
     typedef typename L::T T;
     constexpr int R = kBackwardRows;
-    __shared__ float2 pairs[kBackwardWaves][V][64], met[kBackwardWaves][V][64];
+    __shared__ float2 pairs[W][V][64], met[W][V][64];
     __shared__ unsigned ticket;
     const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
     const Place at = place_of(tiles, take_ticket(tiles, chain, &ticket));
-    const int64_t part = at.segment * tiles.batches + at.batch, segment = tiles.segments - 1 - at.segment;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = tiles.waves;
+    const int64_t part = at.segment * tiles.side() + at.batch;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), waves = blockDim.x / 64;
+    const Sequence of(tiles, at, wave, p.n.T, R, true);
     int channel = at.group * group_width<V>() + lane * V;
     channel = channel < p.n.C - V ? channel : p.n.C - V;
-    const int64_t first = (segment * waves + (waves - 1 - wave)) * R, left = p.n.T - first;
-    const int rows = left < 0 ? 0 : left < R ? (int)left : R;
+    const int64_t first = of.first;
+    const int rows = of.rows;
     float log_decay[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]), sum[v] = 0.f;
     typename L::vec dh[R], x[R], r[R], i[R], h[R];
-    L::template load<R>(p.decay_gate, at.batch, first, p.n.T, channel, r);
-    L::template load<R>(p.dh, at.batch, first, p.n.T, channel, dh);
-    L::template load<R>(p.input_gate, at.batch, first, p.n.T, channel, i);
-    L::template load<R>(p.x, at.batch, first, p.n.T, channel, x);
-    L::template load<R>(p.h, at.batch, first - 1, p.n.T, channel, h);        // the state before each row
+    L::template load<R>(p.decay_gate, of.batch, first, p.n.T, channel, r);
+    L::template load<R>(p.dh, of.batch, first, p.n.T, channel, dh);
+    L::template load<R>(p.input_gate, of.batch, first, p.n.T, channel, i);
+    L::template load<R>(p.x, of.batch, first, p.n.T, channel, x);
+    L::template load<R>(p.h, of.batch, first - 1, p.n.T, channel, h);        // the state before each row
     PackedRows packed{0, 0, 0, 0, -1};
     if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
     float a[R][V], u[R][V];
@@ -173,7 +191,7 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void recurrence_backward_kerne
     } else if (rows > 0 && first + rows == p.n.T) {
 #pragma unroll
         for (int k = 0; k < R; ++k)
-            if (k == rows - 1) end(k, at.batch);
+            if (k == rows - 1) end(k, of.batch);
     }
     const unsigned cut = packed.ends | packed.outside;
     // dh and what the next token passes on
@@ -188,14 +206,14 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void recurrence_backward_kerne
     }
     __syncthreads();
     float c[V];
-    carry_in<V, kBackwardWaves>(chain, tiles, at, at.batch * p.n.C + channel, wave, pairs, met, c);
+    carry_in<V, W>(chain, tiles, at, of.batch * p.n.C + channel, wave, pairs, met, c);
     auto entry_of = [&]() {
-        const int entry = p.n.slots ? p.n.slots[at.batch] : (int)at.batch;
+        const int entry = p.n.slots ? p.n.slots[of.batch] : (int)of.batch;
         return entry < p.n.n_states ? entry : -1;
     };
-    T* const dx = static_cast<T*>(const_cast<void*>(p.dx.p)) + at.batch * p.dx.batch + first * p.dx.token + channel;
-    T* const dr = static_cast<T*>(const_cast<void*>(p.d_decay_gate.p)) + at.batch * p.d_decay_gate.batch + first * p.d_decay_gate.token + channel;
-    T* const di = static_cast<T*>(const_cast<void*>(p.d_input_gate.p)) + at.batch * p.d_input_gate.batch + first * p.d_input_gate.token + channel;
+    T* const dx = static_cast<T*>(const_cast<void*>(p.dx.p)) + of.batch * p.dx.batch + first * p.dx.token + channel;
+    T* const dr = static_cast<T*>(const_cast<void*>(p.d_decay_gate.p)) + of.batch * p.d_decay_gate.batch + first * p.d_decay_gate.token + channel;
+    T* const di = static_cast<T*>(const_cast<void*>(p.d_input_gate.p)) + of.batch * p.d_input_gate.batch + first * p.d_input_gate.token + channel;
 #pragma unroll
     for (int k = R - 1; k >= 0; --k) {
         if (k >= rows) continue;
@@ -229,7 +247,7 @@ __global__ __launch_bounds__(64 * kBackwardWaves) void recurrence_backward_kerne
         L::store(dr + k * p.d_decay_gate.token, gr);
         L::store(di + k * p.d_input_gate.token, gi);
         if (begins && p.d_state) {
-            const int64_t sequence = PACKED ? __builtin_amdgcn_readlane(packed.sequence, k) : at.batch;
+            const int64_t sequence = PACKED ? __builtin_amdgcn_readlane(packed.sequence, k) : of.batch;
 #pragma unroll
             for (int v = 0; v < V; ++v) p.d_state[sequence * p.n.C + channel + v] = c[v];
         }
@@ -300,10 +318,20 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     t.waves = most < waves ? (int)most : waves;
     t.segments = (most + t.waves - 1) / t.waves;
     t.batches = packed ? 1 : n.B;
+    t.per = t.segments > 1 || t.batches == 1 ? 1 : waves / t.waves;
+    if (t.per > t.batches) t.per = (int)t.batches;
     // Of a launch that fills the chip neighbours run at the same time and carries go quickly from one to the next, but what is read of pairs is taken from the
     // rows' bandwidth; others wait for their chain alone (bf16, 8192 tokens: 4096 channels 67.5 us with blocks of 4 and 71 with 16, 512 channels 30 and 22).
     t.block = t.count() > kResident ? 4 : waves;
     return t;
+}
+
+// Workgroups of 8 wavefronts backwards, two on a CU (4 x 4096 x 2048 bf16: 133 us, of 16 wavefronts 152), of 16 where a long chain alone takes the time (8192 x 512: 50
+// and 34).
+Tiles backward_tiles(const RecurrenceBatch& n, bool packed, int V)
+{
+    const Tiles t = tiles_of(n, packed, V, kBackwardRows, 8);
+    return t.segments > 32 && t.count() <= kResident ? tiles_of(n, packed, V, kBackwardRows, 16) : t;
 }
 
 // Channels a lane has.  The last lane of an odd width shares one with its neighbour; where that would be another workgroup's, which may have written a state in place
@@ -335,8 +363,8 @@ int64_t chain_bytes(const Tiles& t, int C) { return (8 * chain_words(t, C) + 15)
 bool recurrence_fits(const RecurrenceBatch& n, bool packed, int ek)
 {
     const int V = lane_channels(n, ek);
-    for (const Tiles& t : {tiles_of(n, packed, V, kForwardRows, kForwardWaves), tiles_of(n, packed, V, kBackwardRows, kBackwardWaves)})
-        if (t.segments >= 1 << 22 || t.batches > ((int64_t)1 << 31) / t.segments || t.count() >= ((int64_t)1 << 26) / t.waves) return false;    // 2^32 threads
+    for (const Tiles& t : {tiles_of(n, packed, V, kForwardRows, kForwardWaves), backward_tiles(n, packed, V)})
+        if (t.segments >= 1 << 22 || t.batches > ((int64_t)1 << 31) / t.segments || t.count() >= ((int64_t)1 << 26) / (t.waves * t.per)) return false;    // 2^32 threads
     return true;
 }
 
@@ -346,8 +374,8 @@ int64_t recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek)
 }
 int64_t recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek)
 {
-    const Tiles t = tiles_of(n, packed, lane_channels(n, ek), kBackwardRows, kBackwardWaves);
-    return chain_bytes(t, n.C) + t.segments * t.batches * n.C * 4;
+    const Tiles t = backward_tiles(n, packed, lane_channels(n, ek));
+    return chain_bytes(t, n.C) + (t.segments * t.side() > 1 ? t.segments * t.side() * n.C * 4 : 0);
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
@@ -358,7 +386,7 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
     return with_elem(ek, [&](auto e) {
         note_kernel("recurrence_kernel", ek, V, a.n.starts != nullptr);
         with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
-            hipLaunchKernelGGL((recurrence_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves), 0, st, a, tiles);
+            hipLaunchKernelGGL((recurrence_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves * tiles.per), 0, st, a, tiles);
         });
         return hipGetLastError();
     });
@@ -367,17 +395,23 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, hipStream_t st)
 {
     const int V = lane_channels(a.n, ek);
-    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kBackwardRows, kBackwardWaves);
+    const Tiles tiles = backward_tiles(a.n, a.n.starts != nullptr, V);
     if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
-    float* const partial = reinterpret_cast<float*>(static_cast<char*>(a.work) + chain_bytes(tiles, a.n.C));
+    // (one row of sums needs no other launch)
+    const int parts = (int)(tiles.segments * tiles.side());
+    float* const partial = parts == 1 ? a.d_log_decay : reinterpret_cast<float*>(static_cast<char*>(a.work) + chain_bytes(tiles, a.n.C));
     return with_elem(ek, [&](auto e) {
-        note_kernel("recurrence_backward_kernel", ek, V, a.n.starts != nullptr);
+        note_kernel("recurrence_backward_kernel", ek, V, a.n.starts != nullptr, tiles.waves * tiles.per);
         with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
-            hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves), 0, st, a, tiles, partial);
+            const dim3 grid((unsigned)tiles.count()), block(64 * tiles.waves * tiles.per);
+            if (block.x > 8 * 64)
+                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed(), 16>), grid, block, 0, st, a, tiles, partial);
+            else
+                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed(), 8>), grid, block, 0, st, a, tiles, partial);
         });
         if (const hipError_t err = hipGetLastError()) return err;
-        if (!a.d_log_decay) return hipSuccess;
-        return launch_fold(FoldArgs{{{partial, (int)(tiles.segments * tiles.batches), a.d_log_decay}, {nullptr, 0, nullptr}}, a.n.C}, st);
+        if (!a.d_log_decay || parts == 1) return hipSuccess;
+        return launch_fold(FoldArgs{{{partial, parts, a.d_log_decay}, {nullptr, 0, nullptr}}, a.n.C}, st);
     });
 }
 

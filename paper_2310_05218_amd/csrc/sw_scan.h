@@ -19,10 +19,11 @@ typedef unsigned long long Word;
 constexpr float kCut = -1.f;            // A of rows among which a sequence begins: nothing from before reaches their end (decays are >= 0)
 
 struct Tiles {
-    int groups, waves;                  // channel groups; wavefronts of a workgroup
+    int groups, waves, per;             // channel groups; wavefronts along a sequence; short sequences that a workgroup has side by side
     int block;                          // workgroups from one carry that is passed on to the next, at most W
     int64_t segments, batches;          // workgroups along a sequence; sequences (1: packed)
-    int64_t count() const { return groups * segments * batches; }
+    __host__ __device__ int64_t side() const { return (batches + per - 1) / per; }
+    int64_t count() const { return groups * segments * side(); }
 };
 
 // V channels of 64 lanes
@@ -153,12 +154,13 @@ __device__ __forceinline__ void incoming(const Chain& chain, int segment, int64_
 // A workgroup's place.
 struct Place {
     int segment, group;
-    int64_t batch;
+    int64_t batch;                      // of sequences, or of `per` of them
 };
 __device__ __forceinline__ Place place_of(const Tiles& tiles, int64_t ticket)
 {
     const int64_t rest = ticket / tiles.groups;
-    return Place{(int)(rest / tiles.batches), (int)(ticket % tiles.groups), rest % tiles.batches};
+    const int64_t side = tiles.side();
+    return Place{(int)(rest / side), (int)(ticket % tiles.groups), rest % side};
 }
 __device__ __forceinline__ int64_t take_ticket(const Tiles& tiles, const Chain& chain, unsigned* shared)
 {
@@ -194,7 +196,7 @@ __device__ __forceinline__ void carry_in(const Chain& chain, const Tiles& tiles,
 #pragma unroll
             for (int v = 0; v < V; ++v) publish(chain.carry(place.segment, at + v), carry_word(after(A[v], B[v], c[v])));
     }
-    for (int w = 0; w < wave; ++w)
+    for (int w = wave - wave % tiles.waves; w < wave; ++w)
 #pragma unroll
         for (int v = 0; v < V; ++v) c[v] = after(pairs[w][v][lane].x, pairs[w][v][lane].y, c[v]);
 }
