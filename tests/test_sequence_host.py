@@ -67,26 +67,26 @@ def test_recurrence_refusals(L):
 
 
 def test_recurrence_backward_refusals(L):
-    d0 = dict(T=10, C=16, B=2, n_states=2, type=B.SW_F32)
+    d0 = dict(T=1000, C=16, B=2, n_states=2, type=B.SW_F32)
     need = L.sw_gated_recurrence_backward_workspace_bytes(B.SwGatedRecurrenceDims(**d0), 0)
     assert need > 0
 
     def f(t=None, g=AT[8], state=AT[9], df=AT[10], dl=AT[11], ds=AT[12], s=None, work=AT[13], bytes_=need, slots=None, starts=None, **k):
-        t, s = t or AT[:8], s or [(160, 16, 0)] * 8
+        t, s = t or AT[:8], s or [(16000, 16, 0)] * 8
         dims = B.SwGatedRecurrenceDims(**{**d0, **k})
         return L.sw_gated_recurrence_backward(t[0], t[1], t[2], t[3], g, t[4], state, df, t[5], t[6], t[7], dl, ds, slots, starts, dims, strides(*s), work, bytes_, None)
 
     for i in range(8):
         assert f(t=replaced(AT[:8], i, None)) == B.SW_ERR_NULL
         assert f(t=replaced(AT[:8], i, AT[i] + 2)) == B.SW_ERR_ALIGN
-    for bad in BAD_EXTENTS + [dict(s=[(160, 16, 0)] * 7 + [(160, 8, 0)])]:
+    for bad in BAD_EXTENTS + [dict(s=[(16000, 16, 0)] * 7 + [(16000, 8, 0)])]:
         assert f(**bad) == B.SW_ERR_SHAPE, bad
     for bad in (dict(work=None), dict(bytes_=need - 1), dict(work=AT[13] + 4)):
         assert f(**bad) == B.SW_ERR_WORKSPACE, bad
     for bad in (dict(t=replaced(AT[:8], 5, AT[0])), dict(t=replaced(AT[:8], 6, AT[5])), dict(t=replaced(AT[:8], 7, AT[5] + 64)), dict(ds=AT[9]), dict(dl=AT[8]),
                 dict(ds=AT[10] + 64), dict(work=AT[7]), dict(dl=AT[12])):
         assert f(**bad) == B.SW_ERR_ALIAS, bad
-    assert f(t=[*AT[:5], AT[5], AT[5] + 60, AT[5] + 128], s=[(160, 16, 0)] * 5 + [(480, 48, 0)] * 3) == B.SW_ERR_ALIAS
+    assert f(t=[*AT[:5], AT[5], AT[5] + 60, AT[5] + 128], s=[(16000, 16, 0)] * 5 + [(48000, 48, 0)] * 3) == B.SW_ERR_ALIAS
 
 
 def test_recurrence_step_refusals(L):
