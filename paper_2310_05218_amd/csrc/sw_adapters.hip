@@ -47,29 +47,28 @@ __device__ __forceinline__ int adapter_of_row(const AdapterArgs& p, int64_t row)
     return b < 0 || b >= p.B ? -1 : adapter_of(p, b);
 }
 
-constexpr int kLowRows = 32, kOutRows = 32;        // of a tile, in the two products
+constexpr int kTileRows = 32;
 
 // A tile's rows (none: 0) and their adapter (-1: none).
 struct Tile {
     int64_t first;
     int rows, s;
 };
-template <int ROWS>
 __device__ __forceinline__ Tile tile_at(const AdapterArgs& p, int64_t place)
 {
     if (!p.starts) {
-        const int64_t each = (p.T + ROWS - 1) / ROWS, b = place / each, at = place % each * ROWS;
+        const int64_t each = (p.T + kTileRows - 1) / kTileRows, b = place / each, at = place % each * kTileRows;
         if (b >= p.B) return Tile{0, 0, -1};
-        return Tile{b * p.T + at, p.T - at < ROWS ? (int)(p.T - at) : ROWS, adapter_of(p, b)};
+        return Tile{b * p.T + at, p.T - at < kTileRows ? (int)(p.T - at) : kTileRows, adapter_of(p, b)};
     }
     // (j = 0 and B + 1: the rows before the first and after the last sequence)
     auto first = [&](int j) {
         const int64_t v = j == 0 ? 0 : p.starts[j - 1];
         return v < 0 ? 0 : v > p.T ? p.T : v;
     };
-    const int found = at_or_before(p.B + 2, place, [&](int j) { return first(j) / ROWS + j; }), j = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
-    const int64_t begin = first(j), end = j == p.B + 1 ? p.T : first(j + 1), at = begin + (place - (begin / ROWS + j)) * ROWS, left = end - at;
-    Tile t{at, left <= 0 || at < 0 ? 0 : left < ROWS ? (int)left : ROWS, -1};
+    const int found = at_or_before(p.B + 2, place, [&](int j) { return first(j) / kTileRows + j; }), j = __builtin_amdgcn_readfirstlane(found > 0 ? found - 1 : 0);
+    const int64_t begin = first(j), end = j == p.B + 1 ? p.T : first(j + 1), at = begin + (place - (begin / kTileRows + j)) * kTileRows, left = end - at;
+    Tile t{at, left <= 0 || at < 0 ? 0 : left < kTileRows ? (int)left : kTileRows, -1};
     if (t.rows && j > 0 && j <= p.B) t.s = adapter_of(p, j - 1);
     return t;
 }
@@ -84,7 +83,7 @@ __device__ __forceinline__ DiePlace die_place(int parts)
     const unsigned die = blockIdx.x % kDies, at = blockIdx.x / kDies, run = gridDim.x / kDies / parts;
     return DiePlace{(int64_t)die * run + at / parts, (int)(at % parts)};
 }
-int64_t tile_places(const AdapterArgs& a, int rows) { return a.starts ? a.T / rows + a.B + 3 : a.B * ((a.T + rows - 1) / rows); }
+int64_t tile_places(const AdapterArgs& a) { return a.starts ? a.T / kTileRows + a.B + 3 : a.B * ((a.T + kTileRows - 1) / kTileRows); }
 
 // ---- tiles of rows ----------------------------------------------------------------------------------------------------------------------------
 
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
     extern __shared__ float sums[];                     // [W][32][PITCH]
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
     const DiePlace place = die_place(parts);
-    const Tile tile = tile_at<kLowRows>(p, place.place);
+    const Tile tile = tile_at(p, place.place);
     if (tile.rows == 0 || tile.s < 0) return;
     const T *const x = static_cast<const T*>(p.x) + tile.first * p.x_stride, *const a = static_cast<const T*>(p.a) + (int64_t)tile.s * p.rank * p.C_in;
     // where a lane's vectors of two steps are (change_halves), from the tile's and the factor's first row
@@ -215,7 +214,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[(wave * kLowRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
+            for (int i = 0; i < 4; ++i) sums[(wave * kTileRows + 16 * t + 4 * q + i) * PITCH + 16 * n + m] = acc[t][n][i];
     __syncthreads();
     float* const low = static_cast<float*>(p.work) + (place.part * rows + tile.first) * K;
     for (int k = threadIdx.x; k < tile.rows * K; k += 64 * W) {
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
         float v = 0.f;
         if (n < p.rank)
 #pragma unroll
-            for (int w = 0; w < W; ++w) v += sums[(w * kLowRows + r) * PITCH + n];
+            for (int w = 0; w < W; ++w) v += sums[(w * kTileRows + r) * PITCH + n];
         low[k] = v;
     }
 }
@@ -240,7 +239,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
     typedef typename M::R R;
     typedef typename M::T T;
     typedef typename R::vec vec;
-    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES, PER = 16 / RUN, TS = kOutRows / 16;  // lanes a row of 64 channels, rows at a time
+    constexpr int VEC = R::VEC, PARTS = M::PARTS, LANES = 64 / VEC, RUN = 64 / LANES, PER = 16 / RUN, TS = kTileRows / 16;  // lanes a row of 64 channels, rows at a time
     __shared__ float turned[kOutWaves][16][kOutPitch];
     extern __shared__ float shared[];
     T* const low = reinterpret_cast<T*>(shared);        // [PARTS][32][K + VEC]
@@ -248,7 +247,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
     const int pitch = K + VEC;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), m = lane % 16, q = lane / 16;
     const DiePlace at = die_place(chunks);
-    const Tile tile = tile_at<kOutRows>(p, at.place);
+    const Tile tile = tile_at(p, at.place);
     if (tile.rows == 0 || (tile.s < 0 && p.out == p.y)) return;
     const int from = at.part * chunk, to = from + chunk < p.C_out ? from + chunk : p.C_out;
     const T* const y = static_cast<const T*>(p.y) + tile.first * p.y_stride;
@@ -261,11 +260,11 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
         return;
     }
     // low's parts are added and, of 16-bit tensors, split, eight lanes a row
-    __shared__ float factor[kOutRows];
+    __shared__ float factor[kTileRows];
     {
         const float scale = p.scales ? p.scales[tile.s] : 1.f;
         const int r = threadIdx.x / 8, eighth = threadIdx.x % 8;
-        static_assert(kOutRows * 8 == 64 * kOutWaves, "a row of low for every eight threads");
+        static_assert(kTileRows * 8 == 64 * kOutWaves, "eight threads a row");
         const float* const source = static_cast<const float*>(p.work) + (tile.first + (r < tile.rows ? r : 0)) * K;
         auto values = [&](int c) {
             f32x4 v = *reinterpret_cast<const f32x4*>(source + c);
@@ -294,7 +293,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const T one = (T)rest[e];
-                    low[(n * kOutRows + r) * pitch + c + e] = one;
+                    low[(n * kTileRows + r) * pitch + c + e] = one;
                     rest[e] -= (float)one;
                 }
         }
@@ -351,7 +350,7 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
                 for (int t = 0; t < TS; ++t)
 #pragma unroll
                     for (int n = 0; n < PARTS; ++n) {
-                        const vec v = *reinterpret_cast<const vec*>(low + (n * kOutRows + 16 * t + m) * pitch + k0 + u * M::STEP + q * VEC);
+                        const vec v = *reinterpret_cast<const vec*>(low + (n * kTileRows + 16 * t + m) * pitch + k0 + u * M::STEP + q * VEC);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) acc[j][t] = M::multiply(bv[u][j], v, acc[j][t]);
                     }
@@ -526,14 +525,14 @@ bool whole_rows(const AdapterArgs& a, int ek)
     return factor <= kReadMost / row_chunks(a, kCUs) / rows;
 }
 
-unsigned die_groups(const AdapterArgs& a, int rows, int parts) { return (unsigned)((tile_places(a, rows) + kDies - 1) / kDies * kDies * parts); }
+unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
 
 constexpr int kChunks = 4;              // workgroups for a tile's output channels
 
 // Workgroups for a tile's input channels, where tiles are too few for the chip: at least 32 steps each.
 int low_parts(const AdapterArgs& a, int ek)
 {
-    const int64_t places = tile_places(a, kLowRows), steps = a.C_in / (ek == kElemF32 ? 16 : 32);
+    const int64_t places = tile_places(a), steps = a.C_in / (ek == kElemF32 ? 16 : 32);
     int64_t parts = kCUs / places;
     if (parts > steps / 32) parts = steps / 32;
     return (int)(parts < 1 ? 1 : parts);
@@ -542,10 +541,10 @@ int low_parts(const AdapterArgs& a, int ek)
 template <int EK, int NT, int W>
 hipError_t launch_low(const AdapterArgs& a, int64_t rows, int K, int parts, hipStream_t st)
 {
-    const size_t lds = sizeof(float) * W * kLowRows * (16 * NT + 1);
+    const size_t lds = sizeof(float) * W * kTileRows * (16 * NT + 1);
     static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_low_kernel<EK, NT, W>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (allowed != hipSuccess) return allowed;
-    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3(die_groups(a, kLowRows, parts)), dim3(64 * W), lds, st, a, rows, K, parts);
+    hipLaunchKernelGGL((adapters_low_kernel<EK, NT, W>), dim3(die_groups(a, parts)), dim3(64 * W), lds, st, a, rows, K, parts);
     return hipGetLastError();
 }
 
@@ -562,8 +561,8 @@ hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
     else err = launch_low<EK, 16, 4>(a, rows, K, parts, st);
     if (err != hipSuccess) return err;
     const int blocks = (a.C_out + 63) / 64, most = blocks < kChunks ? blocks : kChunks, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
-    const size_t lds = (size_t)kOutRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
-    const dim3 grid(die_groups(a, kOutRows, chunks)), block(64 * kOutWaves);
+    const size_t lds = (size_t)kTileRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
+    const dim3 grid(die_groups(a, chunks)), block(64 * kOutWaves);
     const int steps = K / Matrix<EK>::STEP;
     note_kernel("adapters_out_kernel", EK, a.rank);
     auto launch = [&](auto size, auto once, auto even) {
@@ -611,7 +610,7 @@ constexpr int64_t kThreadsMost = ((int64_t)1 << 32) - 1;
 bool adapters_fit(const AdapterArgs& a)
 {
     const int64_t rows = rows_of(a);
-    if (long_sequences(a)) return tile_places(a, kLowRows) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
+    if (long_sequences(a)) return tile_places(a) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
     return rows <= kThreadsMost / kRowThreads / 2 && rows <= kThreadsMost / (64 * ((a.rank + kRowRanks - 1) / kRowRanks)) - kRowThreads;
 }
 
