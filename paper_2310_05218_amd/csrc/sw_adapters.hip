@@ -201,12 +201,26 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
         for (; done < steps; ++done) add_pairs(std::integral_constant<int, 1>());
     if (run == runs - 1)
         for (int c = whole * 2 * M::STEP; c < p.C_in; c += M::STEP) {
+            // (elements from the last one's place, then zeros: looked at before each load the end would have it wait for the one before)
             typename R::vec xv[2], av[NT];
             const int at = c + q * R::VEC;
+            auto element = [&](int e) { return at + e < p.C_in ? at + e : p.C_in - 1; };
 #pragma unroll
-            for (int t = 0; t < 2; ++t) xv[t] = R::load(x + x_row(16 * t + m), at, p.C_in);
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) av[n] = R::load(a + a_row(16 * n + m), at, p.C_in);
+                for (int e = 0; e < R::VEC; ++e) xv[t][e] = x[x_row(16 * t + m) + element(e)];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < R::VEC; ++e) av[n][e] = a[a_row(16 * n + m) + element(e)];
+#pragma unroll
+            for (int e = 0; e < R::VEC; ++e) {
+                const bool there = at + e < p.C_in;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) xv[t][e] = there ? xv[t][e] : (T)0.f;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) av[n][e] = there ? av[n][e] : (T)0.f;
+            }
             add(xv, av);
         }
 #pragma unroll
@@ -228,11 +242,11 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
 }
 
 // out of a tile's rows and a run of output channels, 64 of them a wavefront at a time.  Output channels are the matrix's rows; what comes of the product goes
-// through LDS, so that y is read and out written in whole 128-byte lines.  ONCE: the rank is S steps.  EVEN: ranks and output channels are whole vectors.  A lane's places are 32-bit distances from the tile's first
+// through LDS, so that y is read and out written in whole 128-byte lines.  ONCE: the rank is S steps.  EVEN: a rank is whole vectors; WHOLE: so are the output channels.  A lane's places are 32-bit distances from the tile's first
 // row or the block's first row of b, which are the wavefront's: a block has 150 vector instructions beside its 48 products (rank 64), with 64-bit
 // addresses and rows' ends looked at everywhere it had 425, and waited for them more than for memory.
 constexpr int kOutWaves = 4, kOutPitch = 68;
-template <int EK, int S, bool ONCE, bool EVEN>
+template <int EK, int S, bool ONCE, bool EVEN, bool WHOLE>
 __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int parts, int chunks, int chunk)
 {
     typedef Matrix<EK> M;
@@ -315,11 +329,17 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
         const T *const y0 = y + c0, *const b0 = b + (int64_t)c0 * p.rank;
         vec yv[TS * PER];
         unsigned b_at[4];
-        const bool here = EVEN && column < left;
+        // (what is no whole vector is loaded an element at a time, those beyond the end from the last one's place: rows' ends looked at before each load would have it
+        // wait for the one before)
+        const bool here = column < left, vectors = WHOLE || left >= 64;
+        if (vectors) {
 #pragma unroll
-        for (int i = 0; i < TS * PER; ++i) {
-            if constexpr (EVEN) yv[i] = R::load(y0 + (here ? y_at[i] : y_at[i] - column));
-            else yv[i] = R::load(y0 + (y_at[i] - column), column, left);
+            for (int i = 0; i < TS * PER; ++i) yv[i] = R::load(y0 + (here ? y_at[i] : y_at[i] - column));
+        } else {
+#pragma unroll
+            for (int i = 0; i < TS * PER; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) yv[i][e] = y0[y_at[i] - column + (column + e < left ? column + e : left - 1)];
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) b_at[j] = (16 * j + m < left ? 16 * j + m : left - 1) * p.rank;
@@ -336,9 +356,18 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
                 for (int u = 0; u < S; ++u) {
                     const int k1 = k0 + u * M::STEP + q * VEC;
                     if constexpr (EVEN) bv[u][j] = R::load(b0 + b_at[j] + (k1 < p.rank ? k1 : 0));
-                    else bv[u][j] = R::load(b0 + b_at[j], k1, p.rank);
+                    else
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) bv[u][j][e] = b0[b_at[j] + (k1 + e < p.rank ? k1 + e : p.rank - 1)];
                 }
-            if (EVEN && k0 + S * M::STEP > p.rank)
+            if constexpr (!EVEN)
+#pragma unroll
+                for (int u = 0; u < S; ++u)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) bv[u][j][e] = k0 + u * M::STEP + q * VEC + e < p.rank ? bv[u][j][e] : (T)0.f;
+            else if (k0 + S * M::STEP > p.rank)
 #pragma unroll
                 for (int u = 0; u < S; ++u)
 #pragma unroll
@@ -373,8 +402,13 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
                     for (int k4 = 0; k4 < 4; ++k4) v[e + k4] = __builtin_fmaf(f[i], more[k4], v[e + k4]);
                 }
                 if (i * RUN + row < tile.rows) {
-                    if constexpr (!EVEN) R::store(out + c0 + (out_at[i] - column), column, left, v);
-                    else if (here) R::store(out + c0 + out_at[i], v);
+                    if (vectors) {
+                        if (here) R::store(out + c0 + out_at[i], v);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if (column + e < left) out[c0 + out_at[i] + e] = (T)v[e];
+                    }
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -527,7 +561,16 @@ bool whole_rows(const AdapterArgs& a, int ek)
 
 unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
 
-constexpr int kChunks = 4;              // workgroups for a tile's output channels
+// Workgroups for a tile's output channels: four, more where tiles are too few for the chip, at least a block for each wavefront.
+constexpr int kChunksMost = 64;
+int out_chunks(const AdapterArgs& a)
+{
+    const int64_t blocks = (a.C_out + 63) / 64, places = tile_places(a);
+    int64_t want = 2 * kCUs / places;
+    want = want < 4 ? 4 : want > kChunksMost ? kChunksMost : want;
+    const int64_t most = (blocks + kOutWaves - 1) / kOutWaves;
+    return (int)(want < most ? want : most);
+}
 
 // Workgroups for a tile's input channels, where tiles are too few for the chip: at least 32 steps each.
 int low_parts(const AdapterArgs& a, int ek)
@@ -560,26 +603,28 @@ hipError_t launch_tiles(const AdapterArgs& a, hipStream_t st)
     else if (a.rank <= 128) err = launch_low<EK, 8, 8>(a, rows, K, parts, st);
     else err = launch_low<EK, 16, 4>(a, rows, K, parts, st);
     if (err != hipSuccess) return err;
-    const int blocks = (a.C_out + 63) / 64, most = blocks < kChunks ? blocks : kChunks, chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
+    const int blocks = (a.C_out + 63) / 64, most = out_chunks(a), chunk = (blocks + most - 1) / most * 64, chunks = (a.C_out + chunk - 1) / chunk;
     const size_t lds = (size_t)kTileRows * Matrix<EK>::PARTS * (K + Row<EK>::VEC) * elem_size(EK);
     const dim3 grid(die_groups(a, chunks)), block(64 * kOutWaves);
     const int steps = K / Matrix<EK>::STEP;
     note_kernel("adapters_out_kernel", EK, a.rank);
-    auto launch = [&](auto size, auto once, auto even) {
-        static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_out_kernel<EK, size(), once(), even()>),
+    auto launch = [&](auto size, auto once, auto even, auto whole) {
+        static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(adapters_out_kernel<EK, size(), once(), even(), whole()>),
                                                               hipFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024);
         if (allowed != hipSuccess) return allowed;
-        hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even()>), grid, block, lds, st, a, rows, K, parts, chunks, chunk);
+        hipLaunchKernelGGL((adapters_out_kernel<EK, size(), once(), even(), whole()>), grid, block, lds, st, a, rows, K, parts, chunks, chunk);
         return hipGetLastError();
     };
     constexpr auto yes = std::true_type();
     constexpr auto no = std::false_type();
-    if (a.rank % Row<EK>::VEC || a.C_out % Row<EK>::VEC) return launch(std::integral_constant<int, 1>(), no, no);
-    if (steps == 1) return launch(std::integral_constant<int, 1>(), yes, yes);
-    if (steps == 2) return launch(std::integral_constant<int, 2>(), yes, yes);
-    if (steps == 4) return launch(std::integral_constant<int, 4>(), yes, yes);
-    if (steps % 2 == 0) return launch(std::integral_constant<int, 2>(), no, yes);
-    return launch(std::integral_constant<int, 1>(), no, yes);
+    constexpr auto one = std::integral_constant<int, 1>();
+    constexpr auto two = std::integral_constant<int, 2>();
+    if (a.rank % Row<EK>::VEC) return launch(one, no, no, no);
+    if (a.C_out % Row<EK>::VEC) return steps % 2 ? launch(one, no, yes, no) : launch(two, no, yes, no);
+    if (steps == 1) return launch(one, yes, yes, yes);
+    if (steps == 2) return launch(two, yes, yes, yes);
+    if (steps == 4) return launch(std::integral_constant<int, 4>(), yes, yes, yes);
+    return steps % 2 ? launch(one, no, yes, yes) : launch(two, no, yes, yes);
 }
 
 template <int EK>
@@ -610,7 +655,7 @@ constexpr int64_t kThreadsMost = ((int64_t)1 << 32) - 1;
 bool adapters_fit(const AdapterArgs& a)
 {
     const int64_t rows = rows_of(a);
-    if (long_sequences(a)) return tile_places(a) + kDies <= kThreadsMost / (kChunks * 64 * kOutWaves);
+    if (long_sequences(a)) return tile_places(a) + kDies <= kThreadsMost / (4 * 64 * kOutWaves);
     return rows <= kThreadsMost / kRowThreads / 2 && rows <= kThreadsMost / (64 * ((a.rank + kRowRanks - 1) / kRowRanks)) - kRowThreads;
 }
 
