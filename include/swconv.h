@@ -567,7 +567,7 @@ int sw_gated_recurrence_step(const void* x, const void* decay_gate, const void* 
  * for the `pairs` pairs (i, j) = (k, k + pairs) or, `interleaved`, (2k, 2k + 1); the elements from 2 * pairs on are not turned.
  * q, q_out: [B, T, heads, d], k, k_out: [B, T, kv_heads, d] (strides: of q, k, q_out, k_out); weights: [d] fp32 or NULL (ones), one for all
  * heads; frequencies: [pairs] fp32, radians a position, or NULL with pairs 0; positions: [B, T] int32, any value, contiguous, or NULL:
- * a token's place in its sequence.  The angle is taken in 64 bits: far positions lose nothing.  q_out may be q and k_out may be k
+ * a token's place in its sequence (T < 2^31 then, else SW_ERR_SHAPE).  The angle is taken in 64 bits: far positions lose nothing.  q_out may be q and k_out may be k
  * (same pointer and strides).  1 <= d <= 256, heads and kv_heads <= 65535 (SW_ERR_UNSUPPORTED beyond); eps >= 0 and finite;
  * 2 * pairs <= d.
  */
@@ -599,7 +599,7 @@ int64_t sw_head_norm_backward_workspace_bytes(const sw_head_norm_dims* dims);
  * (starts [B+1] int32, T rows in all).  a: [n, rank, C_in], b: [n, C_out, rank], of the same type, contiguous; scales: [n] fp32 or NULL
  * (ones); slots: [B] int32 (device) or NULL: sequence b has adapter b (n >= B then, else SW_ERR_SHAPE).  Several sequences may have one
  * adapter.  Rows of a sequence whose entry is outside 0 ... n-1, and rows in no sequence, are copied.  Products are added in fp32, a[s] x is
- * kept in fp32, and the result is rounded once.  out may be y (same pointer and stride); any other overlap is SW_ERR_ALIAS.
+ * kept in fp32, and the result is rounded once; what is not finite leaves infinities or NaNs, not always the same of the two, in the results that it reaches.  out may be y (same pointer and stride); any other overlap is SW_ERR_ALIAS.
  * 1 <= rank <= 256, C_in, C_out <= 2^20 (SW_ERR_UNSUPPORTED beyond); rows as far as a launch has threads (2^20 at any size, SW_ERR_SHAPE beyond that).
  */
 typedef struct {

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
                 if (packed.begins >> k & 1) begin(k, __builtin_amdgcn_readlane(packed.entry, k));
                 if (packed.outside >> k & 1)
 #pragma unroll
-                    for (int v = 0; v < V; ++v) b[k][v] = 0.f;
+                    for (int v = 0; v < V; ++v) a[k][v] = b[k][v] = 0.f;
             }
     } else if (first == 0) {
         const int entry = p.n.slots ? p.n.slots[of.batch] : (int)of.batch;
@@ -415,6 +415,8 @@ hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, h
         return launch_fold(FoldArgs{{{partial, parts, a.d_log_decay}, {nullptr, 0, nullptr}}, a.n.C}, st);
     });
 }
+
+bool recurrence_step_fits(const RecurrenceBatch& n) { return (n.C + kThreads - 1) / kThreads * n.B < ((int64_t)1 << 32) / kThreads; }
 
 hipError_t launch_recurrence_step(const RecurrenceStepArgs& a, int ek, hipStream_t st)
 {

@@ -56,6 +56,7 @@ struct RecurrenceStepArgs {
     RecurrenceBatch n;
 };
 bool       recurrence_fits(const RecurrenceBatch& n, bool packed, int ek);      // a launch has workgroups for it
+bool       recurrence_step_fits(const RecurrenceBatch& n);
 int64_t    recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek);
 int64_t    recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek);
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st);

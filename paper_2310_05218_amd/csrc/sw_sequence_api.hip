@@ -58,10 +58,10 @@ int check_recurrence(const sw_gated_recurrence_dims& d, bool packed)
     return recurrence_fits(batch_of(d, nullptr, nullptr, nullptr), packed, d.type) ? SW_OK : SW_ERR_SHAPE;
 }
 
-int check_heads(const sw_head_norm_dims& d)
+int check_heads(const sw_head_norm_dims& d, bool places = false)
 {
     if (d.B <= 0 || d.T <= 0 || d.heads <= 0 || d.kv_heads <= 0 || d.d <= 0 || d.pairs < 0 || 2 * (int64_t)d.pairs > d.d || !(d.eps >= 0.f) ||
-        !std::isfinite(d.eps) || d.T > kMaxExtent / d.B)
+        !std::isfinite(d.eps) || d.T > kMaxExtent / d.B || (places && d.pairs && d.T > 0x7fffffff))
         return SW_ERR_SHAPE;
     if (d.d > 256 || d.heads > 65535 || d.kv_heads > 65535 || !known(d.type)) return SW_ERR_UNSUPPORTED;
     if (d.B * d.T > kMaxExtent / ((int64_t)(d.heads + d.kv_heads) * d.d)) return SW_ERR_SHAPE;
@@ -184,7 +184,7 @@ int sw_gated_recurrence_step(const void* x, const void* decay_gate, const void* 
     if (const int rc = check_recurrence(d, false)) return rc;
     const int C = (int)d.C;
     Tensor4 tx, tr, ti, th;
-    if (d.T != 1 || !tx.set(x, strides, d.B, 1, 1, C, 1) || !tr.set(decay_gate, strides + 1, d.B, 1, 1, C, 1) ||
+    if (d.T != 1 || !recurrence_step_fits(batch_of(d, nullptr, nullptr, nullptr)) || !tx.set(x, strides, d.B, 1, 1, C, 1) || !tr.set(decay_gate, strides + 1, d.B, 1, 1, C, 1) ||
         !ti.set(input_gate, strides + 2, d.B, 1, 1, C, 1) || !th.set(h, strides + 3, d.B, 1, 1, C, 1, true) || d.n_states <= 0 ||
         (!slots && d.n_states < d.B))
         return SW_ERR_SHAPE;
@@ -207,7 +207,7 @@ int sw_head_norm(const void* q, const void* k, const float* q_weight, const floa
 {
     if (!q || !k || !q_out || !k_out || !dims || !strides || (dims->pairs > 0 && !frequencies)) return SW_ERR_NULL;
     const sw_head_norm_dims d = *dims;
-    if (const int rc = check_heads(d)) return rc;
+    if (const int rc = check_heads(d, !positions)) return rc;
     Tensor4 tq, tk, oq, ok;
     if (!tq.set(q, strides, d.B, d.T, d.heads, d.d, 1) || !tk.set(k, strides + 1, d.B, d.T, d.kv_heads, d.d, 1) ||
         !oq.set(q_out, strides + 2, d.B, d.T, d.heads, d.d, 1, true) || !ok.set(k_out, strides + 3, d.B, d.T, d.kv_heads, d.d, 1, true))
@@ -244,7 +244,7 @@ int sw_head_norm_backward(const void* dq, const void* dk, const void* q, const v
 {
     if (!dq || !dk || !q || !k || !q_grad || !k_grad || !dims || !strides || (dims->pairs > 0 && !frequencies)) return SW_ERR_NULL;
     const sw_head_norm_dims d = *dims;
-    if (const int rc = check_heads(d)) return rc;
+    if (const int rc = check_heads(d, !positions)) return rc;
     const void* const tensors[6] = {dq, dk, q, k, q_grad, k_grad};
     Tensor4 t[6];
     for (int i = 0; i < 6; ++i)

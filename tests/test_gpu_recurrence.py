@@ -162,6 +162,27 @@ def test_packed_without_states(sw):
         close(final[b], last, lm, None, 300)
 
 
+@pytest.mark.parametrize("before", [3, 300])
+def test_rows_in_no_sequence_are_not_looked_at(sw, before):
+    """Whatever they hold: padding around sequences, and between them and the next."""
+    n, C = 200, 70
+    T = before + n + 5
+    x, r, i, dh, ld, _, df = make(T, C, "bf16", 5)
+    starts = torch.tensor([before, before + n], dtype=torch.int32).cuda()
+    got = []
+    for fill in (0.0, float("nan")):
+        tensors = [v.clone() for v in (x, r, i, dh)]
+        for v in tensors:
+            v[:before] = v[before + n:] = fill
+        xs, rs, gs, dhs = (v.cuda() for v in tensors)
+        final = torch.empty(1, C, device="cuda")
+        h = sw.sw_gated_recurrence(xs, rs, gs, ld.cuda(), starts=starts, final_state=final)
+        grads = sw.sw_gated_recurrence_backward(dhs, xs, rs, gs, ld.cuda(), h, starts=starts, d_final_state=df[:1].cuda())
+        got.append((h, final, *grads))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert torch.all(got[1][0][:before] == 0) and torch.all(got[1][0][before + n:] == 0)
+
+
 @pytest.mark.parametrize("starts", [(-5, 3, 90), (0, 50, 20), (60, 10, 70), (0, 200, 300), (2000000000, -2000000000, 5)])
 def test_starts_out_of_range_stay_within(sw, starts):
     """Whatever starts holds, nothing outside of the tensors is written; in range and in order, every row has its sequence."""

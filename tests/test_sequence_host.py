@@ -98,7 +98,8 @@ def test_recurrence_step_refusals(L):
     for i in range(4):
         assert f(t=replaced(AT[:4], i, None)) == B.SW_ERR_NULL and f(t=replaced(AT[:4], i, AT[i] + 1)) == B.SW_ERR_ALIGN
     assert f(state=None) == f(g=None) == B.SW_ERR_NULL
-    for bad in BAD_EXTENTS[:7] + [dict(T=2), dict(n_states=0), dict(s=[(16, 0, 0)] * 3 + [(15, 0, 0)])]:
+    for bad in BAD_EXTENTS[:7] + [dict(T=2), dict(n_states=0), dict(s=[(16, 0, 0)] * 3 + [(15, 0, 0)]),
+                                  dict(B=1 << 24, n_states=1 << 24, t=[1 << 45, 2 << 45, 3 << 45, 4 << 45], g=5 << 45, state=6 << 45)]:
         assert f(**bad) == B.SW_ERR_SHAPE, bad
     for bad in (dict(t=replaced(AT[:4], 3, AT[0])), dict(state=AT[0]), dict(state=AT[3] + 64), dict(state=AT[4])):
         assert f(**bad) == B.SW_ERR_ALIAS, bad
@@ -118,7 +119,8 @@ def test_head_norm_refusals(L):
     for i in range(4):
         assert f(t=replaced(AT[:4], i, None)) == B.SW_ERR_NULL and f(t=replaced(AT[:4], i, AT[i] + 2)) == B.SW_ERR_ALIGN
     assert f(fr=None) == B.SW_ERR_NULL
-    for bad in BAD_HEADS + [dict(s=[SQ, SK, (640, 60, 16), SK]), dict(s=[SQ, SK, SQ, (320, 32, 8)]), dict(s=[(640, -64, 16), SK, SQ, SK])]:
+    for bad in BAD_HEADS + [dict(s=[SQ, SK, (640, 60, 16), SK]), dict(s=[SQ, SK, SQ, (320, 32, 8)]), dict(s=[(640, -64, 16), SK, SQ, SK]),
+                            dict(at=None, B=1, T=1 << 31, t=[1 << 45, 2 << 45, 3 << 45, 4 << 45])]:
         assert f(**bad) == B.SW_ERR_SHAPE, bad
     assert f(d=257, s=[(1 << 20, 1 << 16, 300)] * 4) == f(type=4) == f(heads=65536, s=[(1 << 30, 1 << 24, 16)] * 4) == B.SW_ERR_UNSUPPORTED
     for bad in (dict(w=(AT[4] + 1, AT[5])), dict(fr=AT[6] + 2), dict(at=AT[7] + 1)):
