@@ -561,7 +561,8 @@ bool whole_rows(const AdapterArgs& a, int ek)
 
 unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
 
-// Workgroups for a tile's output channels: four, more where tiles are too few for the chip, at least a block for each wavefront.
+// Workgroups for a tile's output channels: four, more where tiles are too few for the chip, at least a block for each wavefront (315 rows, fp32, 6201
+// channels, rank 32: 16 us, of four 28).
 constexpr int kChunksMost = 64;
 int out_chunks(const AdapterArgs& a)
 {
@@ -572,12 +573,15 @@ int out_chunks(const AdapterArgs& a)
     return (int)(want < most ? want : most);
 }
 
-// Workgroups for a tile's input channels, where tiles are too few for the chip: at least 32 steps each.
+// Workgroups for a tile's input channels, where tiles are too few for the chip: at least 8 steps each, a wavefront's least, and at most 8, whose sums every workgroup of
+// the second kernel adds up (32 rows, 4096 channels, rank 16: 9.6 us, of 32 steps each 10.5; 6000 rows of 1024: 10.0 and 11.4; 500 rows of 4096, rank 64: 17.5 and 17.2).
+constexpr int kPartsMost = 8;
 int low_parts(const AdapterArgs& a, int ek)
 {
     const int64_t places = tile_places(a), steps = a.C_in / (ek == kElemF32 ? 16 : 32);
     int64_t parts = kCUs / places;
-    if (parts > steps / 32) parts = steps / 32;
+    if (parts > steps / 8) parts = steps / 8;
+    if (parts > kPartsMost) parts = kPartsMost;
     return (int)(parts < 1 ? 1 : parts);
 }
 
