@@ -326,13 +326,15 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     return t;
 }
 
-// Workgroups of 8 wavefronts backwards, two on a CU (4 x 4096 x 2048 bf16: 133 us, of 16 wavefronts 152); of 16 where these have whole sequences, and where a long chain
-// alone takes the time (8192 x 512: 50 and 34, 8192 x 1000: 67 and 53).
+// Workgroups of 8 wavefronts backwards, two on a CU (4 x 4096 x 2048 bf16: 133 us, of 16 wavefronts 152); of 16 where these have whole sequences, where a long chain
+// alone takes the time (8192 x 512: 50 and 34, 8192 x 1000: 67 and 53), and where they are one for a CU at most but those of 8 more (2000 x 2000: 35 and 28; with fewer
+// of either, 1000 x 1000, 19 and 21.5).
 Tiles backward_tiles(const RecurrenceBatch& n, bool packed, int V)
 {
     const Tiles few = tiles_of(n, packed, V, kBackwardRows, 8), many = tiles_of(n, packed, V, kBackwardRows, 16);
     if (few.segments == 1) return few;
-    return many.segments == 1 || (few.segments > 32 && many.count() <= kResident) ? many : few;
+    const bool all = few.count() > kResident / 2 && many.count() <= kResident / 2;
+    return many.segments == 1 || all || (few.segments > 32 && many.count() <= kResident) ? many : few;
 }
 
 // Channels a lane has.  The last lane of an odd width shares one with its neighbour; where that would be another workgroup's, which may have written a state in place
