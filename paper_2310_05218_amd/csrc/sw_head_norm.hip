@@ -3,7 +3,7 @@
 // Both are bound by memory: a head is read once into the registers of a few lanes, folded there, turned and written once.  A lane has the two vectors
 // of 16 bytes whose elements turn with each other: no element changes its lane.  A turn is the same for all heads of a token: a group of lanes
 // has several heads of one, and takes sine and cosine once for them.  Queries and keys are workgroups of their own, so that the weights, and the sums of their gradients, stay in registers.
-// 8192 tokens of 32 and 8 heads of 128, bf16: 38 us, 4.4 TB/s; gradients of 16384 tokens of 16 and 16: 82 us, 4.9 TB/s, and 4.5 for the fold; vector instructions take 45 to 48 % of both.
+// 8192 tokens of 32 and 8 heads of 128, bf16: 36 us, 4.7 TB/s; gradients of 16384 tokens of 16 and 16: 82 us, 4.9 TB/s, and 4.5 for the fold; vector instructions take 45 to 48 % of both.
 #include <initializer_list>
 
 #include "sw_sequence.h"
@@ -20,9 +20,10 @@ namespace {
 __device__ __forceinline__ void turn(int position, double frequency, float* c, float* s)
 {
     constexpr double kQuarters = 0.6366197723675814, kQuartersLow = -3.935735335036497e-17;
-    const double f = (double)position * frequency, whole = __builtin_rint(f * kQuarters);
+    constexpr double kWhole = 6755399441055744.;                    // 3 * 2^51: what is added to it is rounded to a whole number, whose low word is the sum's
+    const double f = (double)position * frequency, sum = __builtin_fma(f, kQuarters, kWhole), whole = sum - kWhole;
     const float y = (float)__builtin_fma(f, kQuartersLow, __builtin_fma(f, kQuarters, -whole)), z = y * y;
-    const int q = (int)(unsigned)(long long)whole;
+    const unsigned q = (unsigned)__builtin_bit_cast(unsigned long long, sum);
     float sn = 1.60441185e-4f;                                      // (pi/2)^9 / 9!
     sn = __builtin_fmaf(sn, z, -4.68175414e-3f);
     sn = __builtin_fmaf(sn, z, 7.96926262e-2f);
@@ -362,7 +363,10 @@ hipError_t with_group(const HeadNormArgs& a, F&& f)
 
 constexpr int kForwardWaves = 8192, kBackwardGroups = 1024;
 
-// Heads of a row go to several groups of lanes as far as wavefronts are few, to one at most kHeads at a time otherwise; workgroups are what the chip holds.
+// Heads of a row go to several groups of lanes as far as wavefronts are few, kWavesLeast a side, to one at most kHeads at a time otherwise: those of one group share
+// their angles (gradients of 3001 tokens, 6 and 3 heads of 80 fp32: 12.2 us, with 4096 wavefronts 14.8; 4000 tokens, 6 heads of 198 half: 21.5 and 37.4); workgroups
+// are what the chip holds.
+constexpr int kWavesLeast = 512;
 HeadGroups head_groups(const HeadNormArgs& a, int lanes, int most_groups)
 {
     constexpr int kHeads = 8, kFew = 2;
@@ -372,7 +376,7 @@ HeadGroups head_groups(const HeadNormArgs& a, int lanes, int most_groups)
     int64_t want[2];
     for (int i = 0; i < 2; ++i) {
         const int heads = a.side[i].heads;
-        int64_t each = rows * heads * lanes / 64 / (kForwardWaves / 2);     // heads a group of lanes
+        int64_t each = rows * heads * lanes / 64 / kWavesLeast;     // heads a group of lanes
         each = each < 1 ? 1 : each > kHeads ? kHeads : each;
         g.chunks[i] = (int)((heads + each - 1) / each);
         want[i] = (rows * g.chunks[i] + per - 1) / per;
