@@ -32,12 +32,11 @@ constexpr int kForwardRows = 8, kForwardWaves = 16;
 
 // A tile of V channels a lane: decays and terms of its rows in registers, read once, the carry, then the rows' states.  Eight rows are what two workgroups a CU, 32
 // wavefronts, have registers for (64 each); two channels of 16 bits are a line of 256 bytes a row (one channel: 8192 x 4096 81 us, two 66).
-template <int EK, int V, bool PACKED>
-__global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per_eu(8))) void recurrence_kernel(RecurrenceArgs p, Tiles tiles)
+template <int EK, int V, bool PACKED, int R>
+__global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per_eu(64 / R))) void recurrence_kernel(RecurrenceArgs p, Tiles tiles)
 {
     typedef Lane<EK, V> L;
     typedef typename L::T T;
-    constexpr int R = kForwardRows;
     __shared__ float2 pairs[kForwardWaves][V][64], met[kForwardWaves][V][64];
     __shared__ unsigned ticket;
     const Chain chain{static_cast<Word*>(p.work), tiles.batches * p.n.C, tiles.segments, tiles.block};
@@ -319,6 +318,7 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     const int64_t most = (n.T + rows - 1) / rows;
     Tiles t;
     t.groups = (n.C + 64 * V - 1) / (64 * V);
+    t.rows = rows;
     t.waves = most < waves ? (int)most : waves;
     t.segments = (most + t.waves - 1) / t.waves;
     t.batches = packed ? 1 : n.B;
@@ -328,6 +328,18 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     // rows' bandwidth; others wait for their chain alone (bf16, 8192 tokens: 4096 channels 67.5 us with blocks of 4 and 71 with 16, 512 channels 30 and 22).
     t.block = t.count() > kResident ? 4 : waves;
     return t;
+}
+
+// Sequences that two workgroups of a chain would have are one's, of 16 rows a wavefront, as far as registers for half the wavefronts do: no words to clear, nothing to wait for
+// (8 x 256 x 4096 bf16: 16.7 us and 24.4; 64 of them, 2048 workgroups, 115 and 107).
+Tiles forward_tiles(const RecurrenceBatch& n, bool packed, int V)
+{
+    Tiles t = tiles_of(n, packed, V, kForwardRows, kForwardWaves);
+    // (short sequences share workgroups only as far as there are enough of these: 8 x 30 x 256 bf16 4.2 us, in one workgroup a group of channels 6.1)
+    while (t.per > 1 && t.count() < kResident) --t.per;
+    if (t.segments != 2) return t;
+    const Tiles whole = tiles_of(n, packed, V, 2 * kForwardRows, kForwardWaves);
+    return whole.count() <= kResident ? whole : t;
 }
 
 // Workgroups of 8 wavefronts backwards, two on a CU (4 x 4096 x 2048 bf16: 133 us, of 16 wavefronts 152); of 16 where these have whole sequences, where a long chain
@@ -341,9 +353,13 @@ Tiles backward_tiles(const RecurrenceBatch& n, bool packed, int V)
     return many.segments == 1 || all || (few.segments > 32 && many.count() <= kResident) ? many : few;
 }
 
-// Channels a lane has.  The last lane of an odd width shares one with its neighbour; where that would be another workgroup's, which may have written a state in place
-// that this one has not read, lanes have one channel.
-int lane_channels(const RecurrenceBatch& n, int ek) { return ek == kElemF32 || n.C % (64 * 2) == 1 ? 1 : 2; }
+// Channels a lane has: two of 16 bits, one where workgroups of two are for half of the CUs at most: a CU's arithmetic for 128 rows of two takes 6 us (256 x 4096 bf16:
+// 8.3 us, of two 11.6; gradients of 8 x 100 x 2048 13.5 and 16.5; 256 workgroups of two, 2000 x 2048, 16.7 and, of one, 19.4).  The last lane of an odd width shares one with its neighbour; where that would be
+// another workgroup's, which may have written a state in place that this one has not read, lanes have one channel.
+constexpr int kFew = 128;
+bool one_channel(const RecurrenceBatch& n, int ek) { return ek == kElemF32 || n.C % (64 * 2) == 1; }
+int forward_lanes(const RecurrenceBatch& n, bool packed, int ek) { return one_channel(n, ek) || forward_tiles(n, packed, 2).count() <= kFew ? 1 : 2; }
+int backward_lanes(const RecurrenceBatch& n, bool packed, int ek) { return one_channel(n, ek) || backward_tiles(n, packed, 2).count() <= kFew ? 1 : 2; }
 
 hipError_t clear_chain(void* work, int64_t words, hipStream_t st)
 {
@@ -369,31 +385,32 @@ int64_t chain_bytes(const Tiles& t, int C) { return (8 * chain_words(t, C) + 15)
 
 bool recurrence_fits(const RecurrenceBatch& n, bool packed, int ek)
 {
-    const int V = lane_channels(n, ek);
-    for (const Tiles& t : {tiles_of(n, packed, V, kForwardRows, kForwardWaves), backward_tiles(n, packed, V)})
+    for (const Tiles& t : {forward_tiles(n, packed, forward_lanes(n, packed, ek)), backward_tiles(n, packed, backward_lanes(n, packed, ek))})
         if (t.segments >= 1 << 22 || t.batches > ((int64_t)1 << 31) / t.segments || t.count() >= ((int64_t)1 << 26) / (t.waves * t.per)) return false;    // 2^32 threads
     return true;
 }
 
-int64_t recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek)
-{
-    return chain_bytes(tiles_of(n, packed, lane_channels(n, ek), kForwardRows, kForwardWaves), n.C);
-}
+int64_t recurrence_workspace(const RecurrenceBatch& n, bool packed, int ek) { return chain_bytes(forward_tiles(n, packed, forward_lanes(n, packed, ek)), n.C); }
 int64_t recurrence_backward_workspace(const RecurrenceBatch& n, bool packed, int ek)
 {
-    const Tiles t = backward_tiles(n, packed, lane_channels(n, ek));
+    const Tiles t = backward_tiles(n, packed, backward_lanes(n, packed, ek));
     return chain_bytes(t, n.C) + (t.segments * t.side() > 1 ? t.segments * t.side() * n.C * 4 : 0);
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 {
-    const int V = lane_channels(a.n, ek);
-    const Tiles tiles = tiles_of(a.n, a.n.starts != nullptr, V, kForwardRows, kForwardWaves);
+    const bool packed = a.n.starts != nullptr;
+    const int V = forward_lanes(a.n, packed, ek);
+    const Tiles tiles = forward_tiles(a.n, packed, V);
     if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
     return with_elem(ek, [&](auto e) {
-        note_kernel("recurrence_kernel", ek, V, a.n.starts != nullptr);
-        with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
-            hipLaunchKernelGGL((recurrence_kernel<e(), v(), packed()>), dim3((unsigned)tiles.count()), dim3(64 * tiles.waves * tiles.per), 0, st, a, tiles);
+        note_kernel("recurrence_kernel", ek, V, packed, tiles.rows);
+        with_lanes<e()>(V, packed, [&](auto v, auto pack) {
+            const dim3 grid((unsigned)tiles.count()), block(64 * tiles.waves * tiles.per);
+            if (tiles.rows == kForwardRows)
+                hipLaunchKernelGGL((recurrence_kernel<e(), v(), pack(), kForwardRows>), grid, block, 0, st, a, tiles);
+            else
+                hipLaunchKernelGGL((recurrence_kernel<e(), v(), pack(), 2 * kForwardRows>), grid, block, 0, st, a, tiles);
         });
         return hipGetLastError();
     });
@@ -401,20 +418,21 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int ek, hipStream_t st)
 
 hipError_t launch_recurrence_backward(const RecurrenceBackwardArgs& a, int ek, hipStream_t st)
 {
-    const int V = lane_channels(a.n, ek);
-    const Tiles tiles = backward_tiles(a.n, a.n.starts != nullptr, V);
+    const bool packed = a.n.starts != nullptr;
+    const int V = backward_lanes(a.n, packed, ek);
+    const Tiles tiles = backward_tiles(a.n, packed, V);
     if (const hipError_t err = clear_chain(a.work, chain_words(tiles, a.n.C), st)) return err;
     // (one row of sums needs no other launch)
     const int parts = (int)(tiles.segments * tiles.side());
     float* const partial = parts == 1 ? a.d_log_decay : reinterpret_cast<float*>(static_cast<char*>(a.work) + chain_bytes(tiles, a.n.C));
     return with_elem(ek, [&](auto e) {
-        note_kernel("recurrence_backward_kernel", ek, V, a.n.starts != nullptr, tiles.waves * tiles.per);
-        with_lanes<e()>(V, a.n.starts != nullptr, [&](auto v, auto packed) {
+        note_kernel("recurrence_backward_kernel", ek, V, packed, tiles.waves * tiles.per);
+        with_lanes<e()>(V, packed, [&](auto v, auto pack) {
             const dim3 grid((unsigned)tiles.count()), block(64 * tiles.waves * tiles.per);
             if (block.x > 8 * 64)
-                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed(), 16>), grid, block, 0, st, a, tiles, partial);
+                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), pack(), 16>), grid, block, 0, st, a, tiles, partial);
             else
-                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), packed(), 8>), grid, block, 0, st, a, tiles, partial);
+                hipLaunchKernelGGL((recurrence_backward_kernel<e(), v(), pack(), 8>), grid, block, 0, st, a, tiles, partial);
         });
         if (const hipError_t err = hipGetLastError()) return err;
         if (!a.d_log_decay || parts == 1) return hipSuccess;

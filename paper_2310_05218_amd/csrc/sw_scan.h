@@ -20,6 +20,7 @@ constexpr float kCut = -1.f;            // A of rows among which a sequence begi
 
 struct Tiles {
     int groups, waves, per;             // channel groups; wavefronts along a sequence; short sequences that a workgroup has side by side
+    int rows;                           // of a wavefront
     int block;                          // workgroups from one carry that is passed on to the next, at most W
     int64_t segments, batches;          // workgroups along a sequence; sequences (1: packed)
     __host__ __device__ int64_t side() const { return (batches + per - 1) / per; }

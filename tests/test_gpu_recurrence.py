@@ -97,7 +97,8 @@ def test_widths(sw, C, t):
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
-@pytest.mark.parametrize("B,T,C", [(1, 5000, 64), (2, 4100, 192), (40, 3, 512), (300, 1, 96), (5, 600, 1030)])
+@pytest.mark.parametrize("B,T,C", [(1, 5000, 64), (2, 4100, 192), (40, 3, 512), (300, 1, 96), (5, 600, 1030), (48, 300, 130), (48, 70, 131), (24, 200, 1030), (60, 200, 1030),
+                                   (700, 3, 130), (1201, 9, 64)])
 def test_larger(sw, B, T, C, t):
     check_sequences(sw, t, C, T, B, True, B + T)
 
@@ -106,9 +107,10 @@ def test_larger(sw, B, T, C, t):
 @pytest.mark.parametrize("lengths,before,after", [((5,), 0, 0), ((3, 0, 1, 60, 0), 0, 0), ((17, 0, 0, 33, 1, 1, 100), 3, 5), ((0, 0), 4, 4), ((1,) * 50, 1, 0),
                                                   ((700, 2, 333), 0, 40), ((0,) * 70 + (9, 0, 300) + (0,) * 70, 0, 1), ((256, 256, 16, 16), 0, 0)])
 @pytest.mark.parametrize("slots", [False, True])
-def test_packed(sw, lengths, before, after, slots, t):
+@pytest.mark.parametrize("C", [131])
+def test_packed(sw, lengths, before, after, slots, t, C):
     """Sequences one after the other, empty ones among them, rows of none around them; entries of a cache, some of them none."""
-    C, B, n = 131, len(lengths), sum(lengths)
+    B, n = len(lengths), sum(lengths)
     T = before + n + after
     x, r, i, dh, ld, s0, df = make(T, C, t, n + B, B + 3)
     starts = torch.tensor([before + sum(lengths[:k]) for k in range(B + 1)])
@@ -145,6 +147,12 @@ def test_packed(sw, lengths, before, after, slots, t):
     assert torch.all(final.cpu()[untouched] == 7.0) and torch.equal(in_place.cpu()[untouched], s0[untouched])
     assert torch.equal(in_place.cpu()[~untouched], final.cpu()[~untouched])
     close(grads[3], dl + torch.zeros(C), dlm + torch.zeros(C), None, n, GRADIENT + 512 * U)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("lengths,before,after", [((700, 2, 333), 0, 40), ((0, 129, 1, 0, 1000, 15), 3, 0)])
+def test_packed_on_many_workgroups(sw, lengths, before, after, t):
+    test_packed(sw, lengths, before, after, True, t, 2101)
 
 
 def test_packed_without_states(sw):
@@ -206,9 +214,10 @@ def test_starts_out_of_range_stay_within(sw, starts):
 
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("packed", [False, True])
-def test_slices_of_a_projection(sw, t, packed):
+@pytest.mark.parametrize("B", [2, 140])
+def test_slices_of_a_projection(sw, t, packed, B):
     """x and the gates as slices of one tensor's rows, the gradients into slices of another's; what lies beside them is not touched."""
-    B, T, C = 2, 150, 75
+    T, C = 150, 75
     g = torch.Generator().manual_seed(1)
     fused = torch.randn(B, T, 3 * C + 5, generator=g).to(TYPES[t])
     dh, ld = torch.randn(B, T, C, generator=g).to(TYPES[t]), -torch.rand(C, generator=g) - 1e-3
@@ -438,10 +447,11 @@ def test_offsets_beyond_32_bits(sw, t):
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("C", [1, 2, 3, 65, 127, 128, 129, 131, 255, 257, 385])
 @pytest.mark.parametrize("packed", [False, True])
-def test_states_in_place(sw, C, packed, t):
+@pytest.mark.parametrize("B", [6, 48])
+def test_states_in_place(sw, C, packed, t, B):
     """States and gradients of states that replace what they come from, at widths whose last channels are a lane's or a workgroup's of their own: several times over,
     the same bits as into tensors of their own."""
-    B, T = 6, 300
+    T = 300
     x, r, i, dh, ld, s0, df = make(B * T, C, t, C, B)
     shape = (lambda v: v.cuda()) if packed else (lambda v: v.reshape(B, T, C).cuda())
     args = shape(x), shape(r), shape(i), ld.cuda()
