@@ -548,9 +548,11 @@ bool in_tiles(const AdapterArgs& a)
 }
 
 // Single rows: workgroups for every CU, several a row where rows are few.  In one launch where every workgroup of a row reads its factor `a`, as long as that is little
-// in all (64 rows of rank 16 on 2048 channels bf16, 17 MB: 6.4 us, in two launches 7.2; fp32, 34 MB: 14 and 8.6).
+// in all (64 rows of rank 16 on 2048 channels bf16, 17 MB: 6.4 us, in two launches 7.2; fp32, 34 MB: 14 and 8.6) and for a CU (one row of 4096, rank 32, 256 KB: 6.5 and 7.4; rank 64:
+// 12.7 and 7.6), and ranks are few turns of its wavefronts (512 channels, rank 128: 9.2 and 7.3).
 constexpr int kCUs = 256;
-constexpr int64_t kReadMost = 1 << 24;
+constexpr int64_t kReadMost = 1 << 24, kFactorMost = 1 << 18;
+constexpr int kWholeRanks = 64;
 int row_chunks(const AdapterArgs& a, int groups)
 {
     const int64_t rows = rows_of(a), want = (groups + rows - 1) / rows, most = (a.C_out + kRowThreads - 1) / kRowThreads;
@@ -559,7 +561,7 @@ int row_chunks(const AdapterArgs& a, int groups)
 bool whole_rows(const AdapterArgs& a, int ek)
 {
     const int64_t factor = (int64_t)a.rank * a.C_in * elem_size(ek), rows = rows_of(a);
-    return factor <= kReadMost / row_chunks(a, kCUs) / rows;
+    return a.rank <= kWholeRanks && factor <= kFactorMost && factor <= kReadMost / row_chunks(a, kCUs) / rows;
 }
 
 unsigned die_groups(const AdapterArgs& a, int parts) { return (unsigned)((tile_places(a) + kDies - 1) / kDies * kDies * parts); }
