@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * W) void adapters_low_kernel(AdapterArgs p, int
 // through LDS, so that y is read and out written in whole 128-byte lines.  ONCE: the rank is S steps.  EVEN: a rank is whole vectors; WHOLE: so are the output channels.  A lane's places are 32-bit distances from the tile's first
 // row or the block's first row of b, which are the wavefront's: a block has 150 vector instructions beside its 48 products (rank 64), with 64-bit
 // addresses and rows' ends looked at everywhere it had 425, and waited for them more than for memory.
-constexpr int kOutWaves = 4, kOutPitch = 68;
+constexpr int kOutWaves = 4, kOutPitch = 68, kPartsMost = 8;      // kPartsMost: of `low` (low_parts)
 template <int EK, int S, bool ONCE, bool EVEN, bool WHOLE>
 __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArgs p, int64_t rows, int K, int parts, int chunks, int chunk)
 {
@@ -284,9 +284,14 @@ __global__ __launch_bounds__(64 * kOutWaves) void adapters_out_kernel(AdapterArg
         static_assert(kTileRows * 8 == 64 * kOutWaves, "eight threads a row");
         const float* const source = static_cast<const float*>(p.work) + (tile.first + (r < tile.rows ? r : 0)) * K;
         auto values = [&](int c) {
-            f32x4 v = *reinterpret_cast<const f32x4*>(source + c);
-            for (int n = 1; n < parts; ++n) v += *reinterpret_cast<const f32x4*>(source + n * rows * K + c);
-            return v;
+            if (parts == 1) return *reinterpret_cast<const f32x4*>(source + c);
+            // (all on their way at once; what is not there is the first again, and is not added)
+            f32x4 v[kPartsMost];
+#pragma unroll
+            for (int n = 0; n < kPartsMost; ++n) v[n] = *reinterpret_cast<const f32x4*>(source + (n < parts ? n : 0) * rows * K + c);
+#pragma unroll
+            for (int n = 1; n < kPartsMost; ++n) v[0] += n < parts ? v[n] : 0.f;
+            return v[0];
         };
         float back = 1.f, by = scale;
         if constexpr (EK == kElemF16) {
@@ -579,8 +584,7 @@ int out_chunks(const AdapterArgs& a)
 }
 
 // Workgroups for a tile's input channels, where tiles are too few for the chip: at least 8 steps each, a wavefront's least, and at most 8, whose sums every workgroup of
-// the second kernel adds up (32 rows, 4096 channels, rank 16: 9.6 us, of 32 steps each 10.5; 6000 rows of 1024: 10.0 and 11.4; 500 rows of 4096, rank 64: 17.5 and 17.2).
-constexpr int kPartsMost = 8;
+// the second kernel adds up (32 rows, 4096 channels, rank 16: 9.3 us, of 32 steps each 10.5; 6000 rows of 1024: 10.0 and 11.4; 24 of 1600, rank 26, 9.6 and 12.3).
 int low_parts(const AdapterArgs& a, int ek)
 {
     const int64_t places = tile_places(a), steps = a.C_in / (ek == kElemF32 ? 16 : 32);
