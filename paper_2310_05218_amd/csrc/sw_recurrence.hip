@@ -48,6 +48,8 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
     channel = channel < p.n.C - V ? channel : p.n.C - V;
     const int64_t first = of.first;
     const int rows = of.rows;
+    PackedFew few{0, 0, 0};
+    if constexpr (PACKED) few = packed_few(p.n);
     float log_decay[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]);
@@ -56,7 +58,7 @@ __global__ __launch_bounds__(64 * kForwardWaves) __attribute__((amdgpu_waves_per
     L::template load<R>(p.input_gate, of.batch, first, p.n.T, channel, i);
     L::template load<R>(p.x, of.batch, first, p.n.T, channel, x);
     PackedRows packed{0, 0, 0, 0, -1};
-    if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
+    if constexpr (PACKED) packed = packed_rows<R>(p.n, first, few);
     float a[R][V], b[R][V];
 #pragma unroll
     for (int k = 0; k < R; ++k)
@@ -154,6 +156,8 @@ __global__ __launch_bounds__(64 * W) void recurrence_backward_kernel(RecurrenceB
     channel = channel < p.n.C - V ? channel : p.n.C - V;
     const int64_t first = of.first;
     const int rows = of.rows;
+    PackedFew few{0, 0, 0};
+    if constexpr (PACKED) few = packed_few(p.n);
     float log_decay[V], sum[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) log_decay[v] = finite_decay(p.n.log_decay[channel + v]), sum[v] = 0.f;
@@ -164,7 +168,7 @@ __global__ __launch_bounds__(64 * W) void recurrence_backward_kernel(RecurrenceB
     L::template load<R>(p.x, of.batch, first, p.n.T, channel, x);
     L::template load<R>(p.h, of.batch, first - 1, p.n.T, channel, h);        // the state before each row
     PackedRows packed{0, 0, 0, 0, -1};
-    if constexpr (PACKED) packed = packed_rows<R>(p.n, first);
+    if constexpr (PACKED) packed = packed_rows<R>(p.n, first, few);
     float a[R][V], u[R][V];
 #pragma unroll
     for (int k = 0; k < R; ++k)
