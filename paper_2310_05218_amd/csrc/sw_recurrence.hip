@@ -334,16 +334,17 @@ Tiles tiles_of(const RecurrenceBatch& n, bool packed, int V, int rows, int waves
     return t;
 }
 
-// Sequences that two workgroups of a chain would have are one's, of 16 rows a wavefront, as far as registers for half the wavefronts do: no words to clear, nothing to wait for
-// (8 x 256 x 4096 bf16: 16.7 us and 24.4; 64 of them, 2048 workgroups, 115 and 107).
+// Twice the rows a wavefront, in registers of two: where a sequence is one workgroup's then, with no words to clear and nothing to wait for (8 x 256 x 4096 bf16: 16.7 us and
+// 24.4; 64 of them, 2048 workgroups, 115 and 107), and where a chain is half as long and CUs are busy all the same (8192 x 1000: 25.3 and 32.8, 2000 x 4096: 23.7 and
+// 26.8; of half as many workgroups, fp32 4000 x 512, 15.7 and 14.8; of more, 8192 x 4096, 69.6 and 66.3).
 Tiles forward_tiles(const RecurrenceBatch& n, bool packed, int V)
 {
     Tiles t = tiles_of(n, packed, V, kForwardRows, kForwardWaves);
     // (short sequences share workgroups only as far as there are enough of these: 8 x 30 x 256 bf16 4.2 us, in one workgroup a group of channels 6.1)
     while (t.per > 1 && t.count() < kResident) --t.per;
-    if (t.segments != 2) return t;
-    const Tiles whole = tiles_of(n, packed, V, 2 * kForwardRows, kForwardWaves);
-    return whole.count() <= kResident ? whole : t;
+    if (t.segments == 1 || (t.segments > 2 && t.count() <= kResident / 2)) return t;
+    const Tiles longer = tiles_of(n, packed, V, 2 * kForwardRows, kForwardWaves);
+    return longer.count() <= kResident ? longer : t;
 }
 
 // Workgroups of 8 wavefronts backwards, two on a CU (4 x 4096 x 2048 bf16: 133 us, of 16 wavefronts 152); of 16 where these have whole sequences, where a long chain

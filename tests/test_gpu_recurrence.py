@@ -151,8 +151,9 @@ def test_packed(sw, lengths, before, after, slots, t, C):
 
 @pytest.mark.parametrize("t", ["bf16", "f16"])
 @pytest.mark.parametrize("lengths,before,after", [((700, 2, 333), 0, 40), ((0, 129, 1, 0, 1000, 15), 3, 0)])
-def test_packed_on_many_workgroups(sw, lengths, before, after, t):
-    test_packed(sw, lengths, before, after, True, t, 2101)
+@pytest.mark.parametrize("C", [2101, 4101])
+def test_packed_on_many_workgroups(sw, C, lengths, before, after, t):
+    test_packed(sw, lengths, before, after, True, t, C)
 
 
 def test_packed_without_states(sw):
