@@ -361,7 +361,8 @@ hipError_t with_group(const HeadNormArgs& a, F&& f)
     return f(std::integral_constant<int, 0>());         // (256 elements in two ragged parts)
 }
 
-constexpr int kForwardWaves = 8192, kBackwardGroups = 1024;
+// kBackwardGroups: five workgroups a CU, as many as it has registers for (8192 tokens, 32 and 8 heads of 128 bf16: 56.5 us, of 1024 61.6; 30964 of 2 and 2: 35.6 and 33.5).
+constexpr int kForwardWaves = 8192, kBackwardGroups = 1280;
 
 // Heads of a row go to several groups of lanes as far as wavefronts are few, kWavesLeast a side, to one at most kHeads at a time otherwise: those of one group share
 // their angles (gradients of 3001 tokens, 6 and 3 heads of 80 fp32: 12.2 us, with 4096 wavefronts 14.8; 4000 tokens, 6 heads of 198 half: 21.5 and 37.4); workgroups
