@@ -3,7 +3,7 @@
 // Both are bound by memory: a head is read once into the registers of a few lanes, folded there, turned and written once.  A lane has the two vectors
 // of 16 bytes whose elements turn with each other: no element changes its lane.  A turn is the same for all heads of a token: a group of lanes
 // has several heads of one, and takes sine and cosine once for them.  Queries and keys are workgroups of their own, so that the weights, and the sums of their gradients, stay in registers.
-// 8192 tokens of 32 and 8 heads of 128, bf16: 36 us, 4.7 TB/s; gradients of 16384 tokens of 16 and 16: 82 us, 4.9 TB/s, and 4.5 for the fold; vector instructions take 45 to 48 % of both.
+// 8192 tokens of 32 and 8 heads of 128, bf16: 36 us, 4.7 TB/s; gradients of 16384 tokens of 16 and 16: 80 us, 5.0 TB/s, and 4.5 for the fold; vector instructions take 45 to 48 % of both.
 #include <initializer_list>
 
 #include "sw_sequence.h"
